@@ -492,6 +492,115 @@ ms_status ms_argmax(const float* x, int32_t T, int32_t n, int32_t* idx_out, void
 ms_status ms_embed(const int32_t* ids, const void* table, int32_t n_vocab, int32_t T, int32_t d, void* out,
                    void* stream);
 
+/* ---- an 8-bit key/value cache ----------------------------------------------
+ *
+ * The cache of ms_rope_kv in half its bytes, for batches of sequences and
+ * contexts of any length: what it leaves of a VRAM budget holds experts.
+ * Stateless calls like the ones above (caller-owned device memory on the
+ * current device, enqueued on `stream`, the same status codes; nothing is
+ * enqueued unless MS_OK or MS_E_HIP is returned).  No call allocates, waits or
+ * reads device memory on the host, so all of them can be captured into a
+ * graph.
+ *
+ * k, v: e4m3 codes (1 sign, 4 exponent and 3 mantissa bits, no infinities)
+ * [n_seqs][n_kv_heads][max_ctx][head_dim], 16-byte aligned; k_exp, v_exp: one
+ * byte x per 64 positions of a head, [n_seqs][n_kv_heads][max_ctx / 64]; a
+ * value is its code times 2^(x - 127).  head_dim is 64, 128 or 256
+ * (MS_E_UNSUPPORTED otherwise), max_ctx a multiple of 64.
+ *
+ * span_dev: NULL, and every sequence has T tokens at pos0 .. pos0 + T - 1, or
+ * device int32 [n_seqs][2] = (position of the first token, number of tokens):
+ * sequence s then uses the first span[s][1] of its T rows.  A sequence whose
+ * first position is not in [0, pos0] or whose count is not in [1, T] is not
+ * in use; its rows, and those past a sequence's count, are neither read nor
+ * written.  pos0 + T <= max_ctx either way (MS_E_INVALID). */
+typedef struct {
+  void* k;
+  void* v;
+  void* k_exp;
+  void* v_exp;
+  int32_t n_seqs;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t max_ctx;
+} ms_kv_cache_q;
+
+/* Rotary positions.  The first rot_dim (even, 0 .. head_dim) values of a head
+ * turn in pairs (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved; the
+ * rest stays.  Pair i turns by p f'_i at position p, cosine and sine times
+ * mscale (> 0; 1 where nothing is stretched).  f_i = base^(-2 i / rot_dim),
+ * base > 1.  factor >= 1 stretches positions: f'_i = f_i / factor if orig_ctx
+ * is 0, else f'_i = f_i ((1 - g) / factor + g) with g the position of the
+ * turns that pair i makes in the original context, orig_ctx f_i / (2 pi),
+ * between low and high (0 <= low < high; 0 below, 1 above). */
+typedef struct {
+  double base;
+  double factor;
+  double orig_ctx;
+  double low;
+  double high;
+  double mscale;
+  int32_t rot_dim;
+  int32_t interleaved;
+} ms_rope_desc;
+
+/* Rotary embedding and append.  qkv [n_seqs][T][(Hq + 2 Hkv) D] fp32 as in
+ * ms_rope_kv (Hkv = cache n_kv_heads, D = head_dim, Hq a multiple of Hkv;
+ * 16-byte aligned); q_out [n_seqs][T][Hq][D] bf16 (16-byte aligned); keys
+ * (turned) and values go into the cache at the tokens' positions, rounded to
+ * the nearest code, ties to even.  Angles are reduced in double precision.
+ *   The exponent e of 64 positions of a head is the least in [-40, 40] with
+ * the largest finite magnitude at most 448 * 2^e; larger finite values become
+ * the largest code, infinities and NaN the code of NaN.  An append that
+ * continues 64 positions keeps e at least what it was, and rounds the
+ * positions before pos0 again where e rises (exact but for codes below the
+ * least normal one); positions past the append are undefined then until they
+ * are written.  Two calls that write the same 64 positions must not overlap in
+ * time. */
+ms_status ms_rope_kv_q(const ms_kv_cache_q* cache, const ms_rope_desc* rope, const float* qkv, int32_t T, int32_t Hq,
+                       int32_t pos0, const int32_t* span_dev, void* q_out, void* stream);
+
+/* Positions pos0 .. pos0 + n - 1 (at most max_ctx) of every sequence and head
+ * as bf16 (exact): k_out, v_out [n_seqs][n_kv_heads][n][head_dim], 16-byte
+ * aligned. */
+ms_status ms_kv_read_q(const ms_kv_cache_q* cache, int32_t pos0, int32_t n, void* k_out, void* v_out, void* stream);
+
+/* What a score and the set of visible keys may have beside the causal order.
+ * Zero or NULL in a field: without.  For the query at position i and the key
+ * at position j of one sequence:
+ *   s = scale q.k (scale 0: 1 / sqrt(head_dim)); s = softcap tanh(s / softcap);
+ *   s = s - slopes_dev[query head] |i - j| (device fp32 [Hq]);
+ *   the key is seen if j <= i and i - j < window, or if j < prefix (earlier
+ *   and later queries alike), as far as the sequence has keys (its last token
+ *   of this call included), and, with docs_dev (device int32
+ *   [n_seqs][max_ctx]), only if docs_dev[i] == docs_dev[j] >= 0.
+ * A query that sees no key (a negative docs_dev[i]) gives zeros. */
+typedef struct {
+  float scale;
+  float softcap;
+  int32_t window;
+  int32_t prefix;
+  const float* slopes_dev;
+  const int32_t* docs_dev;
+} ms_attn_opts;
+
+/* Device bytes that ms_attention_q needs at workspace_dev for these sizes (0:
+ * none), whatever the options and spans; pure host arithmetic. */
+ms_status ms_attention_q_workspace(const ms_kv_cache_q* cache, int32_t T, int32_t Hq, int32_t pos0,
+                                   uint64_t* bytes_out);
+
+/* Grouped-query attention over the cache (which holds the call's own tokens:
+ * ms_rope_kv_q first): softmax in fp32 with the maximum subtracted.  q, out
+ * [n_seqs][T][Hq][D] bf16, 16-byte aligned (out may be q; other overlaps are
+ * MS_E_INVALID); Hq any multiple of n_kv_heads; opts NULL: causal.
+ * workspace_dev: 16-byte aligned, at least ms_attention_q_workspace bytes,
+ * used until the call has finished on `stream`; calls that may overlap in
+ * time need one each.  What masked keys and values hold (NaN included) does
+ * not reach a query. */
+ms_status ms_attention_q(const ms_kv_cache_q* cache, const void* q, int32_t T, int32_t Hq, int32_t pos0,
+                         const int32_t* span_dev, const ms_attn_opts* opts, void* out, void* workspace_dev,
+                         uint64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,7 +21,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libmoesplit.so")
 SAN_DIR = os.path.join(PKG, "_san")
-SOURCES = ["kernels.hip", "runtime.hip", "planner.cpp", "decoder.hip"]
+SOURCES = ["kernels.hip", "runtime.hip", "planner.cpp", "decoder.hip", "kvcache.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -60,6 +60,22 @@ class ms_plan_problem(ctypes.Structure):
                 ("hit", ctypes.c_void_p), ("pred", ctypes.c_void_p), ("pred_hit", ctypes.c_void_p)]
 
 
+class ms_kv_cache_q(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("max_ctx", ctypes.c_int32)]
+
+
+class ms_rope_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("base", "factor", "orig_ctx", "low", "high", "mscale")] + [
+        ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class ms_attn_opts(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("window", ctypes.c_int32),
+                ("prefix", ctypes.c_int32), ("slopes_dev", ctypes.c_void_p), ("docs_dev", ctypes.c_void_p)]
+
+
 MS_CACHE_STATIC, MS_CACHE_LCP, MS_CACHE_LRU, MS_CACHE_LFU, MS_CACHE_RND = range(5)
 MS_COPY_KERNEL, MS_COPY_DMA = range(2)
 
@@ -111,6 +127,10 @@ def _load():
         "ms_attention": [P, P, P, I32, I32, I32, I32, I32, I32, P, P],
         "ms_argmax": [P, I32, I32, P, P],
         "ms_embed": [P, P, I32, I32, I32, P, P],
+        "ms_rope_kv_q": [ctypes.POINTER(ms_kv_cache_q), ctypes.POINTER(ms_rope_desc), P, I32, I32, I32, P, P, P],
+        "ms_kv_read_q": [ctypes.POINTER(ms_kv_cache_q), I32, I32, P, P, P],
+        "ms_attention_q_workspace": [ctypes.POINTER(ms_kv_cache_q), I32, I32, I32, ctypes.POINTER(U64)],
+        "ms_attention_q": [ctypes.POINTER(ms_kv_cache_q), P, I32, I32, I32, P, ctypes.POINTER(ms_attn_opts), P, P, U64, P],
         "ms_timeline_begin": [P, P, I32],
         "ms_timeline_end": [P, ctypes.POINTER(ms_interval), I32, ctypes.POINTER(I32)],
     }
@@ -389,3 +409,75 @@ def ms_argmax(x, T, n, idx_out, stream=None):
 def ms_embed(ids, table, n_vocab, T, d, out, stream=None):
     _check(lib.ms_embed(_ptr(ids), _ptr(table), int(n_vocab), int(T), int(d), _ptr(out), _stream(stream)),
            what="ms_embed")
+
+
+# --------------------------------------------------- 8-bit key/value cache
+
+KV_BLOCK = 64  # positions that share a scale
+
+
+def kv_cache_q(k, v, k_exp, v_exp):
+    """ms_kv_cache_q of uint8 tensors: codes [n_seqs][Hkv][max_ctx][D] and
+    exponents [n_seqs][Hkv][max_ctx / 64] (new_kv_cache_q allocates them).  The
+    struct keeps the tensors alive."""
+    S, Hkv, ctx, D = k.shape
+    for x, shape in ((k, (S, Hkv, ctx, D)), (v, (S, Hkv, ctx, D)), (k_exp, (S, Hkv, ctx // KV_BLOCK)),
+                     (v_exp, (S, Hkv, ctx // KV_BLOCK))):
+        if tuple(x.shape) != shape or x.element_size() != 1:
+            raise ValueError("kv_cache_q: one-byte tensors of %r and %r expected" % ((S, Hkv, ctx, D),
+                                                                                 (S, Hkv, ctx // KV_BLOCK)))
+    c = ms_kv_cache_q(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), S, Hkv, D, ctx)
+    c.tensors = (k, v, k_exp, v_exp)
+    return c
+
+
+def new_kv_cache_q(n_seqs, n_kv_heads, head_dim, max_ctx, device="cuda"):
+    """A zeroed 8-bit cache (max_ctx a multiple of 64)."""
+    import torch
+    codes = [torch.zeros(n_seqs, n_kv_heads, max_ctx, head_dim, dtype=torch.uint8, device=device) for _ in range(2)]
+    exps = [torch.full((n_seqs, n_kv_heads, max_ctx // KV_BLOCK), 127, dtype=torch.uint8, device=device)
+            for _ in range(2)]
+    return kv_cache_q(*codes, *exps)
+
+
+def rope_desc(rot_dim, base, interleaved=False, factor=1.0, orig_ctx=0.0, low=1.0, high=32.0, mscale=1.0):
+    return ms_rope_desc(float(base), float(factor), float(orig_ctx), float(low), float(high), float(mscale),
+                        int(rot_dim), int(bool(interleaved)))
+
+
+def attn_opts(scale=0.0, softcap=0.0, window=0, prefix=0, slopes=None, doc=None):
+    """slopes: device fp32 [Hq]; doc: device int32 [n_seqs][max_ctx]."""
+    for x, name in ((slopes, "torch.float32"), (doc, "torch.int32")):
+        if x is not None and str(getattr(x, "dtype", name)) != name:
+            raise ValueError("attn_opts: %s expected" % name)
+    o = ms_attn_opts(float(scale), float(softcap), int(window), int(prefix), _ptr(slopes), _ptr(doc))
+    o.tensors = (slopes, doc)
+    return o
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def ms_rope_kv_q(cache, rope, qkv, T, Hq, pos0, q_out, span=None, stream=None):
+    _check(lib.ms_rope_kv_q(_ref(cache), _ref(rope), _ptr(qkv), int(T), int(Hq), int(pos0), _ptr(span), _ptr(q_out),
+                            _stream(stream)), what="ms_rope_kv_q")
+
+
+def ms_kv_read_q(cache, pos0, n, k_out, v_out, stream=None):
+    _check(lib.ms_kv_read_q(_ref(cache), int(pos0), int(n), _ptr(k_out), _ptr(v_out), _stream(stream)),
+           what="ms_kv_read_q")
+
+
+def ms_attention_q_workspace(cache, T, Hq, pos0):
+    n = ctypes.c_uint64()
+    _check(lib.ms_attention_q_workspace(_ref(cache), int(T), int(Hq), int(pos0), ctypes.byref(n)),
+           what="ms_attention_q_workspace")
+    return n.value
+
+
+def ms_attention_q(cache, q, T, Hq, pos0, out, workspace=None, opts=None, span=None, stream=None):
+    """workspace: a device tensor of at least ms_attention_q_workspace bytes."""
+    n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.ms_attention_q(_ref(cache), _ptr(q), int(T), int(Hq), int(pos0), _ptr(span), _ref(opts), _ptr(out),
+                              _ptr(workspace), n, _stream(stream)), what="ms_attention_q")

@@ -1,0 +1,475 @@
+"""GPU parity of the 8-bit key/value cache against its oracle: the append with
+rotary positions, the cache read back, attention over it, and a run of them as
+a decoder makes it, eager and captured."""
+import numpy as np
+import pytest
+
+import synth
+from oracle import kvcache as kv
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+def _ms():
+    from paper_2509_08342_amd import moesplit
+    return moesplit
+
+
+def _bf16(a):
+    from workload import to_device
+    raw, f = synth.storage(np.ascontiguousarray(a, np.float32), "bf16")
+    return to_device(raw, "bf16"), f.astype(np.float64)
+
+
+def _cache(ref):
+    """The oracle cache's codes and exponents on the GPU."""
+    return _ms().kv_cache_q(*[torch.from_numpy(x.copy()).cuda() for x in (ref.k, ref.v, ref.ke, ref.ve)])
+
+
+def _host(cache):
+    return [x.cpu().numpy() for x in cache.tensors]
+
+
+def _random_cache(rng, S, H, ctx, D, spread=3):
+    """Every code but NaN's, scales of neighbouring blocks up to 2^spread apart."""
+    c = kv.Cache(S, H, ctx, D)
+    for codes, exps in ((c.k, c.ke), (c.v, c.ve)):
+        x = rng.standard_normal(codes.shape)
+        codes[...] = kv.encode(x * 100)
+        exps[...] = kv.BIAS - 7 + rng.integers(-spread, spread + 1, exps.shape)
+    return c
+
+
+def _span(spans):
+    return torch.tensor(spans, dtype=torch.int32, device="cuda")
+
+
+# ------------------------------------------------------------------ append
+
+# every width; one token and many; starts and ends inside and at the ends of 64
+# positions; all, part (no multiple of 4, and of 8) and none of the head turned, in
+# either layout; stretched positions; sequences of their own spans
+@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0,rot,inter,factor,orig,spans", [
+    (1, 4, 2, 64, 1, 0, 64, False, 1.0, 0, None),
+    (1, 4, 2, 128, 1, 1499, 128, False, 1.0, 0, None),
+    (1, 8, 1, 256, 3, 62, 256, False, 4.0, 8192, None),
+    (3, 3, 1, 64, 70, 31, 32, True, 4.0, 0, None),
+    (2, 4, 4, 128, 64, 64, 44, False, 8.0, 512, None),
+    (2, 4, 2, 64, 129, 5, 18, False, 1.0, 0, None),
+    (1, 4, 2, 128, 200, 1, 6, True, 2.0, 100, None),
+    (1, 2, 2, 256, 65, 127, 0, False, 1.0, 0, None),
+    (4, 4, 2, 64, 5, 130, 64, True, 1.0, 0, [(130, 5), (0, 1), (61, 5), (128, 3)]),
+    (5, 4, 2, 128, 130, 100, 128, False, 1.0, 0, [(100, 130), (-1, 4), (3, 0), (101, 2), (37, 131)]),
+])
+def test_append(S, Hq, Hkv, D, T, pos0, rot, inter, factor, orig, spans):
+    ms = _ms()
+    rng = np.random.default_rng(T + pos0 + D)
+    ctx = -(-(pos0 + T) // 64) * 64 + 64
+    ref = _random_cache(rng, S, Hkv, ctx, D)
+    cache = _cache(ref)
+    before = _host(cache)
+    qkv = rng.standard_normal((S, T, Hq + 2 * Hkv, D)).astype(np.float32)
+    qkv[:, :, Hq] *= 37.0  # the first key head raises its scales, the others keep what is there or start anew
+    q = torch.full((S, T, Hq, D), -7.0, dtype=torch.bfloat16, device="cuda")
+    ms.ms_rope_kv_q(cache, ms.rope_desc(rot, 1e4, inter, factor, orig, 1.0, 8.0, 1.25), torch.from_numpy(qkv).cuda(), T, Hq,
+                    pos0, q, None if spans is None else _span(spans), torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    k, v, ke, ve = _host(cache)
+    qg = q.float().cpu().numpy()
+    f = kv.frequencies(rot, 1e4, factor, orig, 1.0, 8.0)
+    for s in range(S):
+        start, n = (pos0, T) if spans is None else spans[s]
+        if not (0 <= start <= pos0 and 1 <= n <= T):
+            start, n = 0, 0
+        x = qkv[s, :n].astype(np.float64)
+        turned = np.stack([kv.rope(x[t], start + t, rot, f, inter, 1.25) for t in range(n)]) if n else x
+        # two products and a sum in fp32, of a sine and cosine rounded to it: 8 half steps of the pair's size
+        err = 2.0 ** -21 * 1.25 * np.abs(x).max(axis=-1, initial=0, keepdims=True)
+        assert np.all(np.abs(qg[s, :n] - turned[:, :Hq]) <= 2.0 ** -8 * np.abs(turned[:, :Hq]) + err[:, :Hq])
+        assert np.all(qg[s, n:] == -7.0)
+        if n:
+            ref.append(s, start, turned[:, Hq:Hq + Hkv], x[:, Hq + Hkv:])
+        assert np.array_equal(ke[s], ref.ke[s]) and np.array_equal(ve[s], ref.ve[s])
+        rows = np.zeros(ctx, bool)
+        rows[start // 64 * 64:start + n] = n > 0
+        # values are not turned: the same codes.  Keys: half a step of the code and the turn's error
+        assert np.array_equal(v[s], ref.v[s])
+        got = kv.TABLE[k[s]] * np.repeat(np.exp2(ke[s].astype(float) - kv.BIAS), 64, axis=1)[..., None]
+        unit = np.repeat(np.exp2(ke[s].astype(float) - kv.BIAS), 64, axis=1)[:, start:start + n, None]
+        want = turned[:, Hq:Hq + Hkv].transpose(1, 0, 2)
+        half = np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10 * unit)
+        assert np.all(np.abs(got[:, start:start + n] - want) <= half * (1 + 2.0 ** -20) + err[:, Hq:Hq + Hkv].transpose(1, 0, 2))
+        assert np.array_equal(k[s][:, ~rows], before[0][s][:, ~rows]) and np.array_equal(v[s][:, ~rows], before[1][s][:, ~rows])
+        old = np.arange(ctx)
+        old = (old >= start // 64 * 64) & (old < start)
+        assert np.array_equal(k[s][:, old], ref.k[s][:, old])
+
+
+def test_append_token_by_token():
+    """A decode of 130 tokens, keys not turned: codes and scales are the oracle's, bit by bit, through every raised scale."""
+    ms = _ms()
+    rng = np.random.default_rng(11)
+    S, H, D, ctx = 2, 2, 64, 192
+    ref, cache = kv.Cache(S, H, ctx, D), ms.new_kv_cache_q(S, H, D, ctx)
+    q = torch.empty(S, 1, H, D, dtype=torch.bfloat16, device="cuda")
+    for p in range(130):
+        x = (rng.standard_normal((S, 1, 3 * H, D)) * 2.0 ** rng.integers(-6, 3)).astype(np.float32)
+        ms.ms_rope_kv_q(cache, ms.rope_desc(0, 1e4), torch.from_numpy(x).cuda(), 1, H, p, q)
+        for s in range(S):
+            ref.append(s, p, x[s, :, H:2 * H].astype(np.float64), x[s, :, 2 * H:].astype(np.float64))
+    torch.cuda.synchronize()
+    for got, want in zip(_host(cache), (ref.k, ref.v, ref.ke, ref.ve)):
+        assert np.array_equal(got, want)
+
+
+def test_append_of_extreme_values():
+    """Infinities and NaN become the NaN code and leave the scale to the finite values; magnitudes past the largest scale
+    saturate, those below the smallest vanish."""
+    ms = _ms()
+    H, D, T = 1, 64, 64
+    x = np.zeros((1, T, 3, D), np.float32)
+    x[0, :, 1] = np.linspace(-3, 3, T * D).reshape(T, D)
+    x[0, 5, 1, 7], x[0, 6, 1, 8], x[0, 7, 1, 9] = np.inf, -np.inf, np.nan
+    x[0, :, 2] = 1e-16 * np.linspace(-1, 1, T * D).reshape(T, D)
+    x[0, 9, 2, 3] = 3e38
+    x[0, 10, 2, 4] = 1e-45
+    ref, cache = kv.Cache(1, H, 64, D), ms.new_kv_cache_q(1, H, D, 64)
+    q = torch.empty(1, T, 1, D, dtype=torch.bfloat16, device="cuda")
+    ms.ms_rope_kv_q(cache, ms.rope_desc(0, 1e4), torch.from_numpy(x).cuda(), T, 1, 0, q)
+    ref.append(0, 0, x[0, :, 1:2].astype(np.float64), x[0, :, 2:].astype(np.float64))
+    torch.cuda.synchronize()
+    k, v, ke, ve = _host(cache)
+    assert np.array_equal(ke, ref.ke) and np.array_equal(ve, ref.ve) and ve[0, 0, 0] == kv.BIAS + kv.EMAX
+    for a, b in ((k, ref.k), (v, ref.v)):
+        assert np.array_equal(np.isnan(kv.TABLE[a]), np.isnan(kv.TABLE[b]))
+        fine = ~np.isnan(kv.TABLE[b])
+        assert np.array_equal(kv.TABLE[a][fine], kv.TABLE[b][fine])
+
+
+def test_far_positions_turn_by_exact_angles():
+    ms = _ms()
+    H, D, pos0 = 1, 128, (1 << 20) - 64
+    rng = np.random.default_rng(5)
+    x = rng.standard_normal((1, 3, 3, D)).astype(np.float32)
+    cache = ms.new_kv_cache_q(1, H, D, 1 << 20)
+    q = torch.empty(1, 3, 1, D, dtype=torch.bfloat16, device="cuda")
+    ms.ms_rope_kv_q(cache, ms.rope_desc(D, 1e4), torch.from_numpy(x).cuda(), 3, 1, pos0, q)
+    torch.cuda.synchronize()
+    want = np.stack([kv.rope(x[0, t, :1], pos0 + t, D, kv.frequencies(D, 1e4)) for t in range(3)])
+    assert np.all(np.abs(q[0].float().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -21 * np.abs(x).max())
+
+
+@pytest.mark.parametrize("S,H,D,ctx,pos0,n", [(1, 1, 64, 64, 0, 1), (2, 3, 64, 256, 63, 130), (1, 2, 128, 192, 0, 192),
+                                              (3, 1, 256, 128, 100, 28)])
+def test_read(S, H, D, ctx, pos0, n):
+    ms = _ms()
+    ref = _random_cache(np.random.default_rng(n), S, H, ctx, D, spread=30)
+    ref.k[0, 0, pos0, :3] = 0x7f, 0xff, 0x01
+    ref.ke[0, 0, pos0 // 64], ref.ve[0, 0, pos0 // 64] = kv.BIAS + kv.EMIN, kv.BIAS + kv.EMAX
+    cache = _cache(ref)
+    bufs = [torch.full((S * H * n * D + 8,), -7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    k, v = (b[:S * H * n * D].view(S, H, n, D) for b in bufs)
+    ms.ms_kv_read_q(cache, pos0, n, k, v, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for got, which, buf in ((k, "k", bufs[0]), (v, "v", bufs[1])):
+        want = ref.values(which)[:, :, pos0:pos0 + n]
+        assert np.array_equal(got.float().cpu().numpy().astype(np.float64), want, equal_nan=True)
+        assert np.all(buf[S * H * n * D:].float().cpu().numpy() == -7.0)
+
+
+# --------------------------------------------------------------- attention
+
+def _close(got, ref, mags, ds, n, vmax):
+    """The result's rounding to bf16; of every probability its fp16 half step and its score's error; and half the
+    smallest fp16 step of every key relative to 2^7, to which the largest probability is scaled."""
+    bound = 2.0 ** -8 * np.abs(ref) + mags * (2.0 ** -11 + 2 * ds[..., None] * 2.0 ** -24) * 1.01 + n * 2.0 ** -32 * vmax
+    bad = ~(np.abs(got - ref) <= bound)
+    assert not bad.any(), (np.argwhere(bad)[:4].tolist(), got[bad][:4], ref[bad][:4], bound[bad][:4])
+
+
+def _run(cache, q, T, Hq, pos0, opts=None, span=None, out=None, stream=None):
+    ms = _ms()
+    if out is None:
+        out = torch.full_like(q, -7.0)
+    need = ms.ms_attention_q_workspace(cache, T, Hq, pos0)
+    ws = torch.full((need + 64,), 0x7f, dtype=torch.uint8, device="cuda")  # fp32 of 3e38, past the end too
+    ms.ms_attention_q(cache, q, T, Hq, pos0, out, ws[:need] if need else None, opts, span,
+                      stream or torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert bool((ws[need:] == 0x7f).all())
+    return out
+
+
+def _check(ref, qf, got, pos0, spans, **kw):
+    """got [S][T][Hq][D] against the oracle; rows not in use keep -7."""
+    S, T = qf.shape[:2]
+    docs = kw.pop("docs", None)
+    vals = {w: ref.values(w) for w in "kv"}
+    for s in range(S):
+        start, n = (pos0, T) if spans is None else spans[s]
+        if not (0 <= start <= pos0 and 1 <= n <= T):
+            n = 0
+        assert np.all(got[s, n:] == -7.0)
+        if n:
+            o, mags, ds = kv.attention(qf[s, :n], vals["k"][s], vals["v"][s], start, docs=None if docs is None else docs[s], **kw)
+            _close(got[s, :n], o, mags, ds, start + n, np.abs(np.nan_to_num(vals["v"][s])).max())
+
+
+# (S, Hq, Hkv, D, T, pos0): one token, few, a block's worth, prompts; one query head
+# per key/value head, three, four, eight, sixteen and 71; contexts that end inside, at and
+# just past a tile; long ones that are split
+SHAPES = [(1, 1, 1, 64, 1, 0), (1, 4, 2, 64, 1, 63), (2, 4, 2, 64, 1, 64), (1, 32, 8, 128, 1, 1500), (3, 6, 2, 64, 1, 700),
+          (1, 8, 1, 256, 1, 333), (1, 16, 1, 128, 1, 4100), (2, 71, 1, 64, 1, 129), (1, 2, 2, 128, 1, 9000),
+          (1, 16, 2, 256, 1, 5003), (33, 4, 4, 64, 1, 77),
+          (1, 4, 2, 64, 3, 61), (2, 8, 2, 128, 5, 1000), (1, 3, 1, 64, 16, 0), (1, 8, 1, 256, 2, 190), (2, 6, 2, 64, 9, 4000),
+          (1, 4, 2, 64, 64, 0), (1, 4, 2, 64, 65, 0), (1, 8, 2, 128, 200, 0), (2, 3, 1, 64, 130, 33), (1, 4, 1, 128, 333, 1000),
+          (1, 8, 1, 256, 150, 20), (1, 5, 5, 64, 40, 6000), (1, 16, 16, 64, 257, 0), (1, 32, 2, 128, 600, 3)]
+
+
+@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", SHAPES)
+def test_attention(S, Hq, Hkv, D, T, pos0):
+    rng = np.random.default_rng(T + pos0 + D)
+    ctx = -(-(pos0 + T) // 64) * 64 + 64
+    ref = _random_cache(rng, S, Hkv, ctx, D)
+    q, qf = _bf16(2 * rng.standard_normal((S, T, Hq, D)))
+    _check(ref, qf, _run(_cache(ref), q, T, Hq, pos0).float().cpu().numpy(), pos0, None)
+
+
+# a cap, a bias, windows (one key, inside a tile, several tiles), prefixes (shorter and
+# longer than what is there), and all of them
+MASKS = [dict(softcap=5.0), dict(slopes=True), dict(window=1), dict(window=37), dict(window=200), dict(prefix=10),
+         dict(prefix=150), dict(prefix=100000), dict(window=70, prefix=5), dict(scale=0.25),
+         dict(softcap=20.0, slopes=True, window=130, prefix=70, scale=0.1)]
+
+
+@pytest.mark.parametrize("kw", MASKS, ids=[",".join(m) + str(list(m.values())[0]) for m in MASKS])
+@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", [(2, 4, 2, 64, 1, 700), (1, 6, 1, 128, 1, 3000), (1, 4, 2, 128, 7, 350),
+                                               (1, 4, 2, 64, 300, 0), (1, 8, 2, 128, 150, 260), (1, 8, 1, 256, 100, 90)])
+def test_attention_masks(S, Hq, Hkv, D, T, pos0, kw):
+    ms = _ms()
+    rng = np.random.default_rng(T + pos0)
+    ctx = -(-(pos0 + T) // 64) * 64
+    ref = _random_cache(rng, S, Hkv, ctx, D)
+    q, qf = _bf16(2 * rng.standard_normal((S, T, Hq, D)))
+    kw = dict(kw)
+    if "slopes" in kw:
+        kw["slopes"] = (0.5 ** np.arange(1, Hq + 1)).astype(np.float32)
+    opts = ms.attn_opts(**{k: torch.from_numpy(x).cuda() if k == "slopes" else x for k, x in kw.items()})
+    _check(ref, qf, _run(_cache(ref), q, T, Hq, pos0, opts).float().cpu().numpy(), pos0, None, **kw)
+
+
+@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", [(1, 4, 2, 64, 300, 0), (2, 4, 1, 128, 150, 100), (1, 8, 1, 256, 70, 3),
+                                               (3, 4, 2, 64, 1, 500), (1, 8, 2, 128, 5, 2000)])
+@pytest.mark.parametrize("length", [1, 50, 64, 130])
+@pytest.mark.parametrize("more", [{}, dict(window=40, prefix=90, softcap=10.0)])
+def test_attention_documents(S, Hq, Hkv, D, T, pos0, length, more):
+    """Packed documents, one of them in two places, padding whose queries see nothing (zeros)."""
+    ms = _ms()
+    rng = np.random.default_rng(length)
+    ctx = -(-(pos0 + T) // 64) * 64
+    ref = _random_cache(rng, S, Hkv, ctx, D)
+    q, qf = _bf16(2 * rng.standard_normal((S, T, Hq, D)))
+    docs = np.tile(np.arange(ctx, dtype=np.int32) // length, (S, 1))
+    docs[:, : min(20, pos0 + T - 1)] = docs[0, pos0 + T - 1]
+    docs[0, max(0, pos0 + T - T // 3):] = -1
+    docs[:, pos0 + T:] = docs[0, pos0]  # past the end: never seen
+    opts = ms.attn_opts(doc=torch.from_numpy(docs).cuda(), **more)
+    got = _run(_cache(ref), q, T, Hq, pos0, opts).float().cpu().numpy()
+    _check(ref, qf, got, pos0, None, docs=docs, **more)
+    if T >= 3:
+        assert not np.any(got[0, T - T // 3:])
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,T,pos0,spans", [
+    (4, 2, 64, 1, 900, [(900, 1), (0, 1), (63, 1), (64, 1), (-1, 1), (901, 1), (5, 0), (450, 1), (7, 2)]),
+    (8, 2, 128, 4, 3000, [(3000, 4), (1000, 1), (0, 3), (2999, 4), (-5, -5)]),
+    (4, 1, 64, 100, 500, [(500, 100), (0, 100), (321, 3), (2, 64), (600, 100)]),
+    (8, 1, 256, 40, 64, [(64, 40), (0, 1), (30, 33)])])
+@pytest.mark.parametrize("kw", [{}, dict(window=50, prefix=3)])
+def test_attention_spans(Hq, Hkv, D, T, pos0, spans, kw):
+    ms = _ms()
+    rng = np.random.default_rng(T)
+    S, ctx = len(spans), -(-(pos0 + T) // 64) * 64
+    ref = _random_cache(rng, S, Hkv, ctx, D)
+    q, qf = _bf16(2 * rng.standard_normal((S, T, Hq, D)))
+    got = _run(_cache(ref), q, T, Hq, pos0, ms.attn_opts(**kw), _span(spans)).float().cpu().numpy()
+    _check(ref, qf, got, pos0, spans, **kw)
+
+
+@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", [(1, 4, 2, 64, 1, 700), (1, 8, 2, 128, 1, 5000), (1, 4, 2, 128, 6, 350),
+                                               (1, 4, 2, 64, 300, 0), (1, 4, 1, 128, 200, 100), (1, 8, 1, 256, 90, 60)])
+def test_attention_does_not_see_what_is_masked(S, Hq, Hkv, D, T, pos0):
+    """NaN in the cache past the sequence, and in a key and a value of the call's own tokens: the former reach no query,
+    the latter those that see them only."""
+    rng = np.random.default_rng(T)
+    n = pos0 + T
+    ctx = -(-n // 64) * 64 + 64
+    ref = _random_cache(rng, S, Hkv, ctx, D)
+    ref.k[:, :, n:], ref.v[:, :, n:] = 0x7f, 0xff
+    q, qf = _bf16(2 * rng.standard_normal((S, T, Hq, D)))
+    _check(ref, qf, _run(_cache(ref), q, T, Hq, pos0).float().cpu().numpy(), pos0, None)
+    at, nan_key = pos0 + T // 2, pos0 + T - 1
+    clean = [w.copy() for w in (ref.k, ref.v)]
+    ref.v[:, :, at, 3] = 0x7f
+    ref.k[:, Hkv - 1, nan_key, 5] = 0x7f
+    got = _run(_cache(ref), q, T, Hq, pos0).float().cpu().numpy()
+    ref.k, ref.v = clean
+    vals = {w: ref.values(w) for w in "kv"}
+    o, mags, ds = kv.attention(qf[0], vals["k"][0], vals["v"][0], pos0)
+    i = np.arange(pos0, n)
+    want = np.zeros(o.shape, bool)
+    want[i >= at, :, 3] = True
+    want[i >= nan_key, (Hkv - 1) * (Hq // Hkv):] = True
+    assert np.array_equal(np.isnan(got[0]), want)
+    o, got0 = np.where(want, 0.0, o), np.where(want, 0.0, got[0])
+    _close(got0, o, mags, ds, n, np.abs(np.nan_to_num(vals["v"])).max())
+
+
+@pytest.mark.parametrize("T,pos0", [(1, 3000), (4, 500), (150, 200)])
+@pytest.mark.parametrize("far", [0, 10, 60])
+def test_attention_of_blocks_far_apart_in_scale(T, pos0, far):
+    """Values of some blocks 2^far times the others', probabilities that favour either: the small ones still count."""
+    rng = np.random.default_rng(far)
+    S, Hq, Hkv, D = 1, 8, 2, 128
+    ctx = -(-(pos0 + T) // 64) * 64
+    ref = _random_cache(rng, S, Hkv, ctx, D, spread=0)
+    ref.ve[:, :, ::2] = np.clip(ref.ve[:, :, ::2].astype(int) + far // 2, kv.BIAS + kv.EMIN, kv.BIAS + kv.EMAX)
+    ref.ve[:, :, 1::2] = np.clip(ref.ve[:, :, 1::2].astype(int) - (far - far // 2), kv.BIAS + kv.EMIN, kv.BIAS + kv.EMAX)
+    for name, sign in (("even", 1.0), ("odd", -1.0)):
+        # the first value of a key says which blocks it belongs to; the query's turns that into a score of 0 or -50
+        ref.k[:, :, :, 0] = kv.encode(np.where(np.arange(ctx) // 64 % 2 == 0, 100.0, -100.0))
+        ref.ke[:, :, :] = kv.BIAS - 7
+        qv = 0.5 * rng.standard_normal((S, T, Hq, D))
+        qv[..., 0] = sign * 25.0 * np.sqrt(D) / (100.0 / 128)
+        q, qf = _bf16(qv)
+        _check(ref, qf, _run(_cache(ref), q, T, Hq, pos0).float().cpu().numpy(), pos0, None)
+
+
+@pytest.mark.parametrize("T,pos0", [(1, 700), (5, 100), (150, 64)])
+@pytest.mark.parametrize("exponent", [20, 36, 60])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_attention_large_scores(T, pos0, exponent, sign):
+    """Scores of 1e6 to 1e18, three distinct and exact ones: the largest keys share the weight."""
+    rng = np.random.default_rng(T + exponent)
+    S, Hq, Hkv, D = 1, 4, 1, 64
+    ctx = -(-(pos0 + T) // 64) * 64
+    ref = _random_cache(rng, S, Hkv, ctx, D)
+    ref.k[...] = kv.encode(sign * (1.25 + rng.integers(0, 3, (S, Hkv, ctx, 1)) / 8.0) * np.ones(D))
+    ref.ke[...] = kv.BIAS + exponent - exponent // 2
+    q, qf = _bf16(np.full((S, T, Hq, D), 1.5 * 2.0 ** (exponent // 2)))
+    got = _run(_cache(ref), q, T, Hq, pos0).float().cpu().numpy()
+    o, mags, _ = kv.attention(qf[0], ref.values("k")[0], ref.values("v")[0], pos0)
+    _close(got[0], o, mags, np.zeros(o.shape[:2]), ctx, np.abs(ref.values("v")).max())
+
+
+def test_attention_in_place_and_on_another_stream():
+    rng = np.random.default_rng(1)
+    for S, Hq, Hkv, D, T, pos0 in [(1, 8, 2, 128, 1, 4000), (2, 4, 2, 64, 5, 300), (1, 4, 2, 64, 200, 100)]:
+        ref = _random_cache(rng, S, Hkv, -(-(pos0 + T) // 64) * 64, D)
+        q, qf = _bf16(rng.standard_normal((S, T, Hq, D)))
+        cache, stream = _cache(ref), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        _check(ref, qf, _run(cache, q, T, Hq, pos0, out=q, stream=stream).float().cpu().numpy(), pos0, None)
+
+
+def test_long_caches_pass_32_bits():
+    """The second head of a cache of 5 GiB: offsets past 2^32."""
+    ms = _ms()
+    D, ctx = 256, 10 << 20
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("needs 12 GiB")
+    cache = ms.new_kv_cache_q(1, 2, D, ctx)
+    rng = np.random.default_rng(2)
+    pos0, T = ctx - 70, 70
+    x = rng.standard_normal((1, T, 6, D)).astype(np.float32)
+    q = torch.empty(1, T, 2, D, dtype=torch.bfloat16, device="cuda")
+    ms.ms_rope_kv_q(cache, ms.rope_desc(0, 1e4), torch.from_numpy(x).cuda(), T, 2, pos0, q)
+    k, v = (torch.empty(1, 2, T, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ms.ms_kv_read_q(cache, pos0, T, k, v)
+    out = _run(cache, q, T, 2, pos0, ms.attn_opts(window=50)).float().cpu().numpy()
+    ref = kv.Cache(1, 2, 128, D)  # the last 128 positions: 58 keys before the call's own, more than the window
+    ref.append(0, 58, x[0, :, 2:4].astype(np.float64), x[0, :, 4:].astype(np.float64))
+    assert np.array_equal(k[0].float().cpu().numpy().astype(np.float64), ref.values("k")[0][:, 58:])
+    assert np.array_equal(v[0].float().cpu().numpy().astype(np.float64), ref.values("v")[0][:, 58:])
+    qf = q.float().cpu().numpy().astype(np.float64)
+    o, mags, ds = kv.attention(qf[0], ref.values("k")[0], ref.values("v")[0], 58, window=50)
+    _close(out[0], o, mags, ds, 128, np.abs(ref.values("v")).max())
+
+
+# ------------------------------------------------------------ used together
+
+def _steps(ms, cache, qkv, q, out, ws, desc, opts, span, T, Hq, pos0, stream):
+    ms.ms_rope_kv_q(cache, desc, qkv, T, Hq, pos0, q, span, stream)
+    ms.ms_attention_q(cache, q, T, Hq, pos0, out, ws, opts, span, stream)
+
+
+def test_prompt_then_decode_eager_and_captured():
+    """Three sequences of different prompt lengths, then six tokens each: the eager calls against the oracle, and the same
+    decode captured once and replayed with positions that change on the device."""
+    ms = _ms()
+    rng = np.random.default_rng(8)
+    S, Hq, Hkv, D, ctx, P, n_dec = 3, 6, 2, 64, 512, 150, 6
+    desc = ms.rope_desc(48, 1e4, True, 4.0, 128, 1.0, 8.0, 1.1)
+    kw = dict(softcap=30.0, window=100, prefix=4)
+    opts = ms.attn_opts(**kw)
+    lens = [150, 64, 97]
+    prompt = rng.standard_normal((S, P, Hq + 2 * Hkv, D)).astype(np.float32)
+    toks = rng.standard_normal((n_dec, S, 1, Hq + 2 * Hkv, D)).astype(np.float32)
+    stream = torch.cuda.Stream()
+    results = []
+    for captured in (False, True):
+        cache = ms.new_kv_cache_q(S, Hkv, D, ctx)
+        q, out = (torch.zeros(S, P, Hq, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        q1, out1 = (torch.zeros(S, 1, Hq, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        need = max(ms.ms_attention_q_workspace(cache, P, Hq, 0), ms.ms_attention_q_workspace(cache, 1, Hq, ctx - 1), 16)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        span = _span([(0, n) for n in lens])
+        x, x1 = torch.from_numpy(prompt).cuda(), torch.zeros(S, 1, Hq + 2 * Hkv, D, device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            _steps(ms, cache, x, q, out, ws, desc, opts, span, P, Hq, 0, stream)
+            got = [out.clone()]
+            span.copy_(_span([(n, 1) for n in lens]))
+            stream.synchronize()
+            graph = None
+            if captured:
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph, stream=stream):
+                    _steps(ms, cache, x1, q1, out1, ws, desc, opts, span, 1, Hq, ctx - 1, stream)
+            for i in range(n_dec):
+                x1.copy_(torch.from_numpy(toks[i]))
+                if graph is not None:
+                    graph.replay()
+                else:
+                    _steps(ms, cache, x1, q1, out1, ws, desc, opts, span, 1, Hq, ctx - 1, stream)
+                got.append(out1.clone())
+                span[:, 0] += 1
+            stream.synchronize()
+        results.append([g.float().cpu().numpy() for g in got] + _host(cache))
+    for a, b in zip(*results):
+        assert np.array_equal(a, b)
+    f = kv.frequencies(48, 1e4, 4.0, 128, 1.0, 8.0)
+    got, (k, v, ke, ve) = results[0][:1 + n_dec], results[0][1 + n_dec:]
+    final = kv.Cache(S, Hkv, ctx, D)
+    final.k, final.v, final.ke, final.ve = k, v, ke, ve
+    for s in range(S):
+        # values are not turned: the append in pieces is the oracle's; attention over the cache as it was left
+        ref = kv.Cache(1, Hkv, ctx, D)
+        z = np.zeros((lens[s], Hkv, D))
+        ref.append(0, 0, z, prompt[s, :lens[s], Hq + Hkv:].astype(np.float64))
+        for i in range(n_dec):
+            ref.append(0, lens[s] + i, z[:1], toks[i, s, :, Hq + Hkv:].astype(np.float64))
+        n = lens[s] + n_dec
+        assert np.array_equal(v[s, :, :n], ref.v[0, :, :n]) and np.array_equal(ve[s], ref.ve[0])
+        pos = lens[s] + n_dec - 1
+        qf = kv.rope(toks[-1, s, :, :Hq].astype(np.float64), pos, 48, f, True, 1.1)
+        qf = _bf16(qf)[1]
+        o, mags, ds = kv.attention(qf, final.values("k")[s], final.values("v")[s], pos, **kw)
+        vmax = np.abs(final.values("v")[s]).max()
+        # a query's own rounding to bf16 may differ by a step where its turn is rounded: one step of one value's
+        # product, 2^-7 |q k| / sqrt(D), in a capped score
+        K = np.abs(final.values("k")[s]).max()
+        ds = ds + 2.0 ** 24 * 2.0 ** -7 * np.abs(qf).max() * K / np.sqrt(D)
+        _close(got[-1][s], o, mags, ds, n, vmax)
