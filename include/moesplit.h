@@ -573,7 +573,7 @@ ms_status ms_kv_read_q(const ms_kv_cache_q* cache, int32_t pos0, int32_t n, void
  *   the key is seen if j <= i and i - j < window, or if j < prefix (earlier
  *   and later queries alike), as far as the sequence has keys (its last token
  *   of this call included), and, with docs_dev (device int32
- *   [n_seqs][max_ctx]), only if docs_dev[i] == docs_dev[j] >= 0.
+ *   [n_seqs][max_ctx], 16-byte aligned), only if docs_dev[i] == docs_dev[j] >= 0.
  * A query that sees no key (a negative docs_dev[i]) gives zeros. */
 typedef struct {
   float scale;

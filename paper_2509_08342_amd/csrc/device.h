@@ -78,4 +78,14 @@ __device__ __forceinline__ v4i16_t lds_read_tr16(const unsigned char* p) {
       (__attribute__((address_space(3))) v4i16_t*)((const __attribute__((address_space(3))) unsigned char*)(p)));
 }
 
+// The same for 8-bit values (ds_read_b64_tr_b8): in each 16-lane group, lanes
+// 2 r and 2 r + 1 give row r of an 8 x 16 tile and lane i receives its column i,
+// row 0 in the lowest byte.
+typedef int v2i32_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint2 lds_read_tr8(const unsigned char* p) {
+  const v2i32_t v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+      (__attribute__((address_space(3))) v2i32_t*)((const __attribute__((address_space(3))) unsigned char*)(p)));
+  return make_uint2(static_cast<uint32_t>(v[0]), static_cast<uint32_t>(v[1]));
+}
+
 }  // namespace msk

@@ -247,9 +247,11 @@ struct AttArgs {
   const float* slopes;
   const int32_t* docs;
   uint16_t* out;
-  int T, Hq, Hkv, G, max_ctx, pos0;
+  float* part;  // splits > 1: [rows][splits][D] results of a share of the keys
+  float2* ml;   // [rows][splits] their maxima and sums
+  int T, Hq, Hkv, G, max_ctx, pos0, heads, splits;  // heads: key/value heads of all sequences
   int window, prefix;
-  float scale, cap;
+  float pre, cap, mul;  // score = pre q.k, capped and biased; weight = 2^(mul (score - maximum))
 };
 
 // Tiles of 64 keys that queries at positions p0 .. p1 of a sequence of n keys
@@ -278,7 +280,7 @@ __device__ __forceinline__ float tanh_of(float x) {
   return fabsf(x) < 0.25f ? series : copysignf(far, x);
 }
 
-// Whether the query at position i (document di) sees key j of n (document dj).
+// Whether the query at position i sees key j of n (document di, dj).
 __device__ __forceinline__ bool sees(const AttArgs& a, int i, int j, int n, int di, int dj) {
   const int d = i - j;
   bool s = (d >= 0 && (a.window <= 0 || d < a.window)) || j < a.prefix;
@@ -287,26 +289,39 @@ __device__ __forceinline__ bool sees(const AttArgs& a, int i, int j, int n, int 
   return s;
 }
 
-// One query row by one wave: lane j of a tile has key j's score, then D / 64
-// columns of the output.  Every value is read for the rows that see it only.
+__device__ __forceinline__ size_t kv_row(const AttArgs& a, int head) { return static_cast<size_t>(head) * a.max_ctx; }
+__device__ __forceinline__ size_t exp_row(const AttArgs& a, int head) {
+  return static_cast<size_t>(head) * (a.max_ctx / kKvBlock);
+}
+// row r (token r / G, query head r % G of the group) of a key/value head: its place in q and out, and in part
+__device__ __forceinline__ size_t q_row(const AttArgs& a, int head, int r) {
+  return (static_cast<size_t>(head / a.Hkv) * a.T + r / a.G) * a.Hq + head % a.Hkv * a.G + r % a.G;
+}
+__device__ __forceinline__ size_t part_row(const AttArgs& a, int head, int r, int z) {
+  return (static_cast<size_t>(head) * a.T * a.G + r) * a.splits + z;
+}
+
+// One query row over the tiles [i0, i1) of `tl`, by one wave: lane j of a tile
+// has key j's score, then D / 64 columns of the output.  Reads no value that
+// the row does not see, so it is what a work-group falls back to when a result
+// is not finite (qs: D floats of LDS of the wave's own).
 template <int D>
-__device__ __forceinline__ void attend_row(const AttArgs& a, int seq, const Span& sp, int g, int t, int h, float* qs) {
+__device__ __forceinline__ void attend_row(const AttArgs& a, int head, const Span& sp, int r, const Tiles& tl, int i0, int i1,
+                                           int z, float* qs) {
   constexpr int CPL = D / 64;
   const int lane = threadIdx.x & 63;
-  const int pos = sp.start + t, n = sp.start + sp.count, head = g * a.G + h;
-  const size_t row = (static_cast<size_t>(seq) * a.T + t) * a.Hq + head;
+  const int pos = sp.start + r / a.G, n = sp.start + sp.count, seq = head / a.Hkv;
+  const size_t row = q_row(a, head, r);
 #pragma unroll
   for (int c = 0; c < CPL; ++c) qs[CPL * lane + c] = __uint_as_float(static_cast<uint32_t>(a.q[row * D + CPL * lane + c]) << 16);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's own row
-  const size_t kv = static_cast<size_t>(seq) * a.Hkv + g;
-  const uint8_t *K = a.k + kv * a.max_ctx * D, *V = a.v + kv * a.max_ctx * D;
-  const uint8_t *ke = a.k_exp + kv * (a.max_ctx / kKvBlock), *ve = a.v_exp + kv * (a.max_ctx / kKvBlock);
+  const uint8_t *K = a.k + kv_row(a, head) * D, *V = a.v + kv_row(a, head) * D;
+  const uint8_t *ke = a.k_exp + exp_row(a, head), *ve = a.v_exp + exp_row(a, head);
   const int32_t* docs = a.docs ? a.docs + static_cast<size_t>(seq) * a.max_ctx : nullptr;
   const int di = docs ? docs[pos] : 0;
-  const float slope = a.slopes ? a.slopes[head] : 0.0f;
-  const Tiles tl = tiles_of(a, pos, pos, n);
+  const float slope = a.slopes ? a.slopes[head % a.Hkv * a.G + r % a.G] : 0.0f;
   float m = -INFINITY, l = 0.0f, o[CPL] = {};
-  for (int i = 0; i < tl.count(); ++i) {
+  for (int i = i0; i < i1; ++i) {
     const int tile = tl.at(i), j = tile * kKvBlock + lane;
     const bool see = sees(a, pos, j, n, di, docs ? docs[j] : 0);
     float s = -INFINITY;
@@ -323,7 +338,7 @@ __device__ __forceinline__ void attend_row(const AttArgs& a, int seq, const Span
           for (int f = 0; f < 4; ++f) d = fmaf(qs[c + 4 * e + f], v[f], d);
         }
       }
-      s = d * pow2(exponent(ke[tile])) * a.scale;
+      s = d * pow2(exponent(ke[tile])) * a.pre;
       if (a.cap > 0.0f) s = a.cap * tanh_of(s / a.cap);
       s -= slope * fabsf(static_cast<float>(pos - j));
     }
@@ -335,8 +350,8 @@ __device__ __forceinline__ void attend_row(const AttArgs& a, int seq, const Span
     }
     const float next = top != top || m != m ? __uint_as_float(0x7fc00000u) : fmaxf(m, top);
     if (next == -INFINITY) continue;  // nothing seen yet
-    const float f = m == next ? 1.0f : expf(m - next);
-    const float p = see ? expf(s - next) : 0.0f;
+    const float f = m == next ? 1.0f : exp2f((m - next) * a.mul);
+    const float p = see ? exp2f((s - next) * a.mul) : 0.0f;
     float sum = p;
 #pragma unroll
     for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x, 64);
@@ -354,23 +369,686 @@ __device__ __forceinline__ void attend_row(const AttArgs& a, int seq, const Span
       for (int c = 0; c < CPL; ++c) o[c] = fmaf(px, __builtin_amdgcn_cvt_f32_fp8(vr[c], 0), o[c]);
     }
   }
+  const size_t pr = part_row(a, head, r, z);
 #pragma unroll
-  for (int c = 0; c < CPL; ++c)
-    a.out[row * D + CPL * lane + c] = static_cast<uint16_t>(f32_to_bf16_bits(l == 0.0f ? 0.0f : o[c] / l));
+  for (int c = 0; c < CPL; ++c) {
+    const float v = l == 0.0f ? 0.0f : o[c] / l;
+    if (a.splits == 1)
+      a.out[row * D + CPL * lane + c] = static_cast<uint16_t>(f32_to_bf16_bits(v));
+    else
+      a.part[pr * D + CPL * lane + c] = v;
+  }
+  if (a.splits > 1 && lane == 0) a.ml[pr] = make_float2(m, l);
 }
 
-constexpr int kRowThreads = 256;
+// ---- one step of the softmax, shared by the two matrix-core kernels
+//
+// S^T = K Q^T on the matrix cores: A = 16 keys, B = 16 rows, so that lane (n =
+// lane % 16, g = lane / 16) ends with row n's scores of keys 16 b + 4 g + r of
+// key block b; O^T += V^T P^T takes the probabilities where they are, as fp16
+// pairs, contraction slot 4 h + r of lane group g being key 16 h + 4 g + r of 32.
+//
+// Scales: a key block's 2^ek multiplies the raw score (exact), a value block's
+// 2^ev goes into the probability's exponent.  A row keeps its maximum m (in
+// scores before `mul`, subtracted before the exponent is scaled: the largest
+// key gets an exact power of two however large its score) and its sum l relative
+// to m, and an exponent R with O = sum 2^(mul (s - m) + ev - R) code.  R keeps
+// the fp16 probabilities below 2^15, its aim is 2^7 for the largest: half a step
+// is 2^-11 of a probability and the smallest step 2^-31 of the largest weight.
+// One fp16 part is enough here: the 3-bit mantissa of the codes it meets is
+// 2^-4 off already.  m and R move only when they have to (kGrow), so most tiles
+// rescale nothing.
+constexpr float kAim = 7.0f, kMost = 15.0f, kGrow = 40.0f;
+
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+
+// maximum over the lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float group_max(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+template <int DB>
+struct RowState {
+  float m = -INFINITY, l = 0.0f, R = 0.0f;
+  msk::f32x4_t O[DB];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int c = 0; c < DB; ++c) O[c] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+};
+
+// Scores of NB key blocks (NB / 2 fragments of P) into probabilities.  ks: the
+// keys' scale; mul, ev as above.
+template <int NB, int DB>
+__device__ __forceinline__ void softmax_step(RowState<DB>& st, const msk::f32x4_t (&S)[NB], float ks, float mul, float ev,
+                                             f16x8_t (&P)[NB / 2]) {
+  float top = S[0][0];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) top = fmaxf(top, S[b][r]);
+  top = group_max(top) * ks;
+  const float dx = (top - st.m) * mul;
+  if (__any(dx > kGrow || dx + ev - st.R > kMost)) {
+    const float next = fmaxf(st.m, top);
+    if (next != -INFINITY) {
+      const float dl = st.m == next ? 0.0f : (st.m - next) * mul;
+      const float was = st.R + dl;  // R relative to the new maximum
+      const float R = fmaxf(was, (top - next) * mul + ev - kAim);
+      const float f = __builtin_amdgcn_exp2f(was - R);
+      st.l *= __builtin_amdgcn_exp2f(dl);
+#pragma unroll
+      for (int c = 0; c < DB; ++c) st.O[c] *= f;
+      st.m = next;
+      st.R = R;
+    }
+  }
+  const float base = st.m == -INFINITY ? 0.0f : st.m, off = ev - st.R;
+  float sum = 0.0f;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    float p[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(fmaf(S[b][r], ks, -base), mul, off));
+    sum += (p[0] + p[1]) + (p[2] + p[3]);
+    const f16x2_t lo = __builtin_convertvector(f32x2_t{p[0], p[1]}, f16x2_t);
+    const f16x2_t hi = __builtin_convertvector(f32x2_t{p[2], p[3]}, f16x2_t);
+    f16x8_t& d = P[b / 2];
+    const int o = 4 * (b % 2);
+    d[o] = lo[0], d[o + 1] = lo[1], d[o + 2] = hi[0], d[o + 3] = hi[1];
+  }
+  st.l = fmaf(sum, __builtin_amdgcn_exp2f(-off), st.l);
+}
+
+// A lane's row: what its scores and masks depend on.
+struct Row {
+  int pos, doc;
+  float slope;
+};
+__device__ __forceinline__ Row row_of(const AttArgs& a, int head, const Span& sp, int r) {
+  Row w;
+  w.pos = sp.start + r / a.G;
+  w.doc = a.docs ? a.docs[static_cast<size_t>(head / a.Hkv) * a.max_ctx + w.pos] : 0;
+  w.slope = a.slopes ? a.slopes[head % a.Hkv * a.G + r % a.G] : 0.0f;
+  return w;
+}
+
+// Raw scores of NB key blocks from key k0 on to scores: scaled, capped, biased
+// and masked (`masked`: some row of the wave may not see some of the keys).
+template <int NB>
+__device__ __forceinline__ void modify(const AttArgs& a, const Row& w, const int32_t* docs, int k0, int n, float ks, bool masked,
+                                       msk::f32x4_t (&S)[NB]) {
+  const int g4 = (threadIdx.x & 63) >> 4;
+  const float f = ks * a.pre, inv_cap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int j0 = k0 + 16 * b + 4 * g4;
+    S[b] *= f;
+    if (a.cap > 0.0f) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) S[b][r] = a.cap * tanh_of(S[b][r] * inv_cap);
+    }
+    if (a.slopes) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) S[b][r] -= w.slope * fabsf(static_cast<float>(w.pos - j0 - r));
+    }
+    if (masked) {
+      int4 dj = make_int4(0, 0, 0, 0);
+      if (docs) dj = *reinterpret_cast<const int4*>(docs + j0);
+      const int d[4] = {dj.x, dj.y, dj.z, dj.w};
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (!sees(a, w.pos, j0 + r, n, w.doc, d[r])) S[b][r] = -INFINITY;
+    }
+  }
+}
+
+__device__ __forceinline__ msk::bf16x8_t codes_bf16(uint32_t lo, uint32_t hi) {
+  const uint2 a = codes_to_bf16(lo, 1.0f), b = codes_to_bf16(hi, 1.0f);
+  return msk::as_bf16x8(make_uint4(a.x, a.y, b.x, b.y));
+}
+__device__ __forceinline__ uint2 codes_to_f16(uint32_t c) {
+  return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(c), 1.0f, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(c), 1.0f, true)));
+}
+__device__ __forceinline__ msk::f32x4_t mfma_f16(f16x8_t a, f16x8_t b, msk::f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Whether v holds in any thread of WAVES waves; flags: WAVES ints of LDS that no
+// one else uses until the next barrier.
+template <int WAVES>
+__device__ __forceinline__ bool any_thread(bool v, int* flags) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const bool mine = __any(v);
+  if (lane == 0) flags[wave] = mine;
+  __syncthreads();
+  int r = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) r |= flags[w];
+  return r != 0;
+}
+
+// ---- few rows: one token, or a few
+//
+// At most 16 rows per key/value head (tokens x query heads of the group).  A
+// work-group takes a head and a share of its tiles, a wave the steps (32 keys)
+// w, w + NW, ... of the share, from a ring of its own (no barrier in the loop),
+// and the waves' results are merged at the end.  Codes come to LDS by direct
+// loads and become matrix operands when they are read: keys by 16-byte reads,
+// values by transposing reads of eight keys of a column each.  16-byte piece p of
+// row u sits in slot p ^ key_slot(u) or p ^ value_slot(u), so that the lanes
+// which LDS serves together meet 16 different slots of 256 bytes.
+constexpr int kStep = 32;
+
 template <int D>
-__global__ __launch_bounds__(kRowThreads) void attention_q_kernel(AttArgs a, int seqs) {
-  __shared__ float qs[kRowThreads / 64][D];
-  const int wave = threadIdx.x >> 6;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * (kRowThreads / 64) + wave;
-  const int t = static_cast<int>(row / a.Hq % a.T), head = static_cast<int>(row % a.Hq);
-  const int64_t seq = row / a.Hq / a.T;
-  if (seq >= seqs) return;
-  const Span sp = span_of(a.span, static_cast<int>(seq), a.pos0, a.T);
-  if (t >= sp.count) return;
-  attend_row<D>(a, static_cast<int>(seq), sp, head / a.G, t, head % a.G, qs[wave]);
+__device__ __forceinline__ int key_slot(int u) { return (u / (256 / D)) & (D / 16 - 1); }
+template <int D>
+__device__ __forceinline__ int value_slot(int u) { return (((u & 7) | ((u >> 1) & 8)) / (256 / D)) & (D / 16 - 1); }
+
+constexpr int few_waves(int D) { return D == 256 ? 4 : 8; }
+constexpr int few_stages(int D) { return D == 64 ? 4 : 2; }
+
+template <int D, bool MODS>
+__global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttArgs a) {
+  constexpr int NW = few_waves(D), NST = few_stages(D), KS = D / 32, DB = D / 16;
+  constexpr int PIECES = D / 16, RPL = 64 / PIECES;  // 16-byte pieces of a row, rows per load
+  constexpr int KB = kStep * D, SB = 2 * KB, NK = KB / 1024, NL = 2 * NK;
+  constexpr int PP = D + 4;                          // floats of a merged row
+  static_assert((NST - 2) * NL < 64 && NW * NST * SB <= 160 * 1024, "rings");
+  static_assert(NW * 16 * (PP + 3) * 4 + 64 <= NW * NST * SB, "the merge fits the rings");
+  extern __shared__ __align__(16) unsigned char kv_lds[];
+  const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = blockIdx.x % a.heads, z = blockIdx.x / a.heads, seq = head / a.Hkv;
+  const Span sp = span_of(a.span, seq, a.pos0, a.T);
+  if (sp.count == 0) return;
+  const int rows = sp.count * a.G, n = sp.start + sp.count;
+  const Tiles tl = tiles_of(a, sp.start, n - 1, n);
+  const int total = tl.count(), share = (total + a.splits - 1) / a.splits;
+  const int i0 = min(z * share, total), i1 = min(i0 + share, total);
+  if (i0 == i1) {
+    if (static_cast<int>(threadIdx.x) < rows) a.ml[part_row(a, head, threadIdx.x, z)] = make_float2(-INFINITY, 0.0f);
+    return;
+  }
+  // the last tile's second half may be past the end
+  const int steps = 2 * (i1 - i0) - (tl.at(i1 - 1) * kKvBlock + kStep >= n);
+  const uint8_t *K = a.k + kv_row(a, head) * D, *V = a.v + kv_row(a, head) * D;
+  const uint8_t *ke = a.k_exp + exp_row(a, head), *ve = a.v_exp + exp_row(a, head);
+  const int32_t* docs = a.docs ? a.docs + static_cast<size_t>(seq) * a.max_ctx : nullptr;
+  unsigned char* ring = kv_lds + wave * NST * SB;
+  const uint32_t lbase = msk::lds_address(ring);
+  const int lrow = lane / PIECES, slot = lane % PIECES;
+  auto key0 = [&](int s) { return tl.at(i0 + (s >> 1)) * kKvBlock + (s & 1) * kStep; };
+  int kexp[2], vexp[2];  // of this step and the next
+  auto issue = [&](int s, int buf) {  // steps past the wave's last reload the share's last one (never read)
+    const int k0 = key0(min(s, steps - 1));
+#pragma unroll
+    for (int j = 0; j < NK; ++j) {
+      const int u = j * RPL + lrow;
+      const size_t at = static_cast<size_t>(k0 + u) * D;
+      msk::lds_load16(K + at + 16 * (slot ^ key_slot<D>(u)), lbase + buf * SB + 1024 * j);
+      msk::lds_load16(V + at + 16 * (slot ^ value_slot<D>(u)), lbase + buf * SB + KB + 1024 * j);
+    }
+  };
+  const int r = min(n16, rows - 1);
+  const Row w = row_of(a, head, sp, r);
+  msk::bf16x8_t Q[KS];
+  {
+    const uint16_t* qr = a.q + q_row(a, head, r) * D + 16 * g4;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) Q[s] = msk::as_bf16x8(*reinterpret_cast<const uint4*>(qr + 64 * (s >> 1) + 8 * (s & 1)));
+  }
+#pragma unroll
+  for (int p = 0; p < NST - 1; ++p) issue(wave + NW * p, p);
+  auto load_exps = [&](int s, int at) {
+    const int tile = tl.at(i0 + (min(s, steps - 1) >> 1));
+    kexp[at] = ke[tile];
+    vexp[at] = ve[tile];
+  };
+  load_exps(wave, 0);
+  int va;  // this lane's 8 bytes of column block 0
+  {
+    const int x = (lane >> 1) & 7, u = (x < 4 ? 0 : 12) + 4 * g4 + x;  // x >= 4: key 16 + 4 g + x - 4
+    va = KB + u * D + 8 * (lane & 1);
+  }
+  const int vswz = value_slot<D>(((lane >> 1) & 7) < 4 ? 4 * g4 + ((lane >> 1) & 7) : 12 + 4 * g4 + ((lane >> 1) & 7));
+  RowState<DB> st;
+  st.clear();
+  int cur = 0, nxt = NST - 1;
+  for (int s = wave; s < steps; s += NW) {
+    load_exps(s + NW, 1);
+    msk::wait_vm<(NST - 2) * NL>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    issue(s + NW * (NST - 1), nxt);
+    const unsigned char* sg = ring + cur * SB;
+    cur = cur + 1 == NST ? 0 : cur + 1;
+    nxt = nxt + 1 == NST ? 0 : nxt + 1;
+    const int k0 = key0(s);
+    msk::f32x4_t S[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      S[b] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const int u = 16 * b + n16;
+#pragma unroll
+      for (int x = 0; x < KS / 2; ++x) {
+        const uint4 c = *reinterpret_cast<const uint4*>(sg + u * D + 16 * ((4 * x + g4) ^ key_slot<D>(u)));
+        S[b] = msk::mfma16(codes_bf16(c.x, c.y), Q[2 * x], S[b]);
+        S[b] = msk::mfma16(codes_bf16(c.z, c.w), Q[2 * x + 1], S[b]);
+      }
+    }
+    const bool last = k0 + kStep > n;
+    const float ks = pow2(exponent(static_cast<uint8_t>(kexp[0]))), ev = static_cast<float>(exponent(static_cast<uint8_t>(vexp[0])));
+    kexp[0] = kexp[1];
+    vexp[0] = vexp[1];
+    f16x8_t P[1];
+    if constexpr (MODS) {
+      modify(a, w, docs, k0, n, ks, true, S);
+      softmax_step(st, S, 1.0f, a.mul, ev, P);
+    } else {
+      if (k0 + kStep > sp.start + 1) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (k0 + 16 * b + 4 * g4 + x > w.pos) S[b][x] = -INFINITY;
+      }
+      softmax_step(st, S, ks, a.mul, ev, P);
+    }
+#pragma unroll
+    for (int c = 0; c < DB; ++c) {
+      uint2 t = msk::lds_read_tr8(sg + va + 16 * (c ^ vswz));
+      if (last) {  // what lies past the end may be anything: code 0
+        auto keep = [&](uint32_t x, int j) {
+          const int m = n - j;
+          return m >= 4 ? x : m <= 0 ? 0u : x & ((1u << (8 * m)) - 1);
+        };
+        t.x = keep(t.x, k0 + 4 * g4);
+        t.y = keep(t.y, k0 + 16 + 4 * g4);
+      }
+      const uint2 lo = codes_to_f16(t.x), hi = codes_to_f16(t.y);
+      st.O[c] = mfma_f16(__builtin_bit_cast(f16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y)), P[0], st.O[c]);
+    }
+  }
+  msk::wait_vm<0>();  // the reloads past the last step have landed
+  __syncthreads();    // every wave is done with its ring
+  float l = st.l;
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  float* part = reinterpret_cast<float*>(kv_lds);  // [NW][16][PP]
+  float* mx = part + NW * 16 * PP;                 // [NW][16], and the sums and exponents
+  float *sm = mx + NW * 16, *rx = sm + NW * 16;
+  int* flags = reinterpret_cast<int*>(rx + NW * 16);
+  if (n16 < rows) {
+    if (g4 == 0) {
+      mx[wave * 16 + n16] = st.m;
+      sm[wave * 16 + n16] = l;
+      rx[wave * 16 + n16] = st.R;
+    }
+#pragma unroll
+    for (int c = 0; c < DB; ++c)
+      *reinterpret_cast<float4*>(part + (wave * 16 + n16) * PP + 16 * c + 4 * g4) =
+          make_float4(st.O[c][0], st.O[c][1], st.O[c][2], st.O[c][3]);
+  }
+  __syncthreads();
+  const int used = min(NW, steps);  // waves with a step
+  constexpr int NV = 16 * D / (64 * NW);
+  float val[NV];
+  bool bad = false;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int i = k * 64 * NW + threadIdx.x, row = i / D, col = i % D;
+    val[k] = 0.0f;
+    if (row >= rows) continue;
+    float top = mx[row];
+    for (int x = 1; x < used; ++x) top = fmaxf(top, mx[x * 16 + row]);
+    float num = 0.0f, den = 0.0f;
+    for (int x = 0; x < used; ++x) {
+      const float m = mx[x * 16 + row], d = m == top ? 0.0f : (m - top) * a.mul;
+      den += sm[x * 16 + row] * __builtin_amdgcn_exp2f(d);
+      num += part[(x * 16 + row) * PP + col] * __builtin_amdgcn_exp2f(rx[x * 16 + row] + d);
+    }
+    val[k] = den == 0.0f ? 0.0f : num / den;
+    bad |= !isfinite(val[k]) || !isfinite(den);
+    if (a.splits > 1 && col == 0) a.ml[part_row(a, head, row, z)] = make_float2(top, den);
+  }
+  if (any_thread<NW>(bad, flags)) {  // nothing of out is written yet: it may be q
+    for (int row = wave; row < rows; row += NW) attend_row<D>(a, head, sp, row, tl, i0, i1, z, part + wave * D);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int i = k * 64 * NW + threadIdx.x, row = i / D, col = i % D;
+    if (row >= rows) continue;
+    if (a.splits == 1)
+      a.out[q_row(a, head, row) * D + col] = static_cast<uint16_t>(f32_to_bf16_bits(val[k]));
+    else
+      a.part[part_row(a, head, row, z) * D + col] = val[k];
+  }
+}
+
+// ---- prompts
+//
+// A work-group takes 64 QB rows of one key/value head, a wave 16 QB of them, over
+// its share of the tiles of 64 keys.  A tile's codes go through registers, where
+// they become bf16 keys and fp16 values once for all waves, into LDS, two stages: the
+// loads of the tile after next are in flight while a tile is computed.  16-byte
+// piece p of key row u sits in slot p ^ tile_key_slot(u), of value row u in p ^
+// tile_value_slot(u), free of bank conflicts for the reads.
+constexpr int kTileThreads = 256;
+
+template <int D>
+__device__ __forceinline__ int tile_key_slot(int u) { return (D == 64 ? u >> 1 : u) & (D == 64 ? 7 : 15); }
+template <int D>
+__device__ __forceinline__ int tile_value_slot(int u) { return 2 * ((D == 64 ? u >> 1 : u) & (D == 64 ? 3 : 7)); }
+
+template <int D, int QB, bool MODS>
+__global__ __launch_bounds__(kTileThreads, D == 256 ? 1 : 2) void attention_q_tile_kernel(AttArgs a, int blocks) {
+  constexpr int ROWS = 64 * QB, KS = D / 32, DB = D / 16;
+  constexpr int PITCH = 2 * D, TILE = kKvBlock * PITCH;  // bytes of a converted row and tile
+  constexpr int PIECES = D / 16, NP = kKvBlock * PIECES / kTileThreads;
+  extern __shared__ __align__(16) unsigned char kv_lds[];
+  const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = blockIdx.x % a.heads, zj = blockIdx.x / a.heads, j = zj % blocks, z = zj / blocks, seq = head / a.Hkv;
+  const Span sp = span_of(a.span, seq, a.pos0, a.T);
+  const int rows = sp.count * a.G, n = sp.start + sp.count;
+  // the longest row blocks first, the second half shortest first: two work-groups
+  // that share a CU add up to about the same work
+  const int first = (blocks + 1) / 2, r0 = (j < first ? blocks - 1 - j : j - first) * ROWS;
+  if (r0 >= rows) return;
+  const int r1 = min(r0 + ROWS, rows);  // the work-group's rows
+  const Tiles tl = tiles_of(a, sp.start + r0 / a.G, sp.start + (r1 - 1) / a.G, n);
+  const int total = tl.count(), share = (total + a.splits - 1) / a.splits;
+  const int i0 = min(z * share, total), i1 = min(i0 + share, total);
+  if (i0 == i1) {
+    if (r0 + static_cast<int>(threadIdx.x) < r1) a.ml[part_row(a, head, r0 + threadIdx.x, z)] = make_float2(-INFINITY, 0.0f);
+    return;
+  }
+  const uint8_t *K = a.k + kv_row(a, head) * D, *V = a.v + kv_row(a, head) * D;
+  const uint8_t *ke = a.k_exp + exp_row(a, head), *ve = a.v_exp + exp_row(a, head);
+  const int32_t* docs = a.docs ? a.docs + static_cast<size_t>(seq) * a.max_ctx : nullptr;
+
+  uint4 kr[NP], vr[NP];  // codes of the tile to stage
+  int kexp, vexp;
+  auto load = [&](int i) {
+    const int tile = tl.at(min(i, i1 - 1));
+    const size_t at = static_cast<size_t>(tile) * kKvBlock * D + 16 * threadIdx.x;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      kr[p] = *reinterpret_cast<const uint4*>(K + at + p * kTileThreads * 16);
+      vr[p] = *reinterpret_cast<const uint4*>(V + at + p * kTileThreads * 16);
+    }
+    kexp = ke[tile];
+    vexp = ve[tile];
+  };
+  auto stage = [&](int i, unsigned char* to) {
+    const int k0 = tl.at(min(i, i1 - 1)) * kKvBlock;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int id = p * kTileThreads + threadIdx.x, u = id / PIECES, c = id % PIECES;
+      unsigned char* row = to + u * PITCH;
+      const int sk = tile_key_slot<D>(u), sv = tile_value_slot<D>(u);
+      *reinterpret_cast<uint4*>(row + 16 * ((2 * c) ^ sk)) = __builtin_bit_cast(uint4, codes_bf16(kr[p].x, kr[p].y));
+      *reinterpret_cast<uint4*>(row + 16 * ((2 * c + 1) ^ sk)) = __builtin_bit_cast(uint4, codes_bf16(kr[p].z, kr[p].w));
+      if (k0 + u >= n) vr[p] = make_uint4(0, 0, 0, 0);  // past the end may be anything
+      const uint2 a0 = codes_to_f16(vr[p].x), a1 = codes_to_f16(vr[p].y), a2 = codes_to_f16(vr[p].z), a3 = codes_to_f16(vr[p].w);
+      *reinterpret_cast<uint4*>(row + TILE + 16 * ((2 * c) ^ sv)) = make_uint4(a0.x, a0.y, a1.x, a1.y);
+      *reinterpret_cast<uint4*>(row + TILE + 16 * ((2 * c + 1) ^ sv)) = make_uint4(a2.x, a2.y, a3.x, a3.y);
+    }
+  };
+  load(i0);
+  Row w[QB];
+  msk::bf16x8_t Q[QB][KS];
+#pragma unroll
+  for (int b = 0; b < QB; ++b) {
+    const int r = min(r0 + (wave * QB + b) * 16 + n16, r1 - 1);  // rows past the last repeat it (never stored)
+    w[b] = row_of(a, head, sp, r);
+    const uint16_t* qr = a.q + q_row(a, head, r) * D + 8 * g4;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) Q[b][s] = msk::as_bf16x8(*reinterpret_cast<const uint4*>(qr + 32 * s));
+  }
+  // positions of the wave's first and last rows
+  const int p_min = sp.start + min(r0 + wave * QB * 16, r1 - 1) / a.G;
+  const int p_max = sp.start + min(r0 + (wave + 1) * QB * 16 - 1, r1 - 1) / a.G;
+  int ka[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) ka[s] = n16 * PITCH + 16 * ((4 * s + g4) ^ tile_key_slot<D>(n16));
+  const int vrow = 4 * g4 + ((lane >> 2) & 3), vj = lane & 3;
+  const int va = TILE + vrow * PITCH + 8 * (vj & 1), vswz = tile_value_slot<D>(vrow);
+  RowState<DB> st[QB];
+#pragma unroll
+  for (int b = 0; b < QB; ++b) st[b].clear();
+
+  int ks_c = kexp, ev_c = vexp;  // of the tile to compute
+  stage(i0, kv_lds);
+  load(i0 + 1);
+  msk::bare_barrier();
+  for (int i = i0; i < i1; ++i) {
+    unsigned char* sg = kv_lds + ((i - i0) & 1) * 2 * TILE;
+    const float ks = pow2(exponent(static_cast<uint8_t>(ks_c))), ev = static_cast<float>(exponent(static_cast<uint8_t>(ev_c)));
+    if (i + 1 < i1) {
+      ks_c = kexp;
+      ev_c = vexp;
+      stage(i + 1, kv_lds + ((i + 1 - i0) & 1) * 2 * TILE);
+      load(i + 2);
+    }
+    const int k0 = tl.at(i) * kKvBlock;
+    bool skip, masked;  // whether no row of the wave sees the tile, and whether each sees all of it
+    if constexpr (MODS) {
+      skip = !((k0 <= p_max && (a.window <= 0 || k0 + kKvBlock - 1 > p_min - a.window)) || k0 < a.prefix);
+      masked = docs || !((k0 + kKvBlock - 1 <= p_min && (a.window <= 0 || p_max - k0 < a.window)) ||
+                         (k0 + kKvBlock <= a.prefix && k0 + kKvBlock <= n));
+    } else {
+      skip = k0 > p_max;
+      masked = k0 + kKvBlock - 1 > p_min;
+    }
+    if (!skip) {
+      msk::f32x4_t S[QB][4];
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) {
+        msk::bf16x8_t A[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) A[s] = msk::lds_frag(sg + kb * 16 * PITCH + ka[s]);
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+          S[b][kb] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < KS; ++s) S[b][kb] = msk::mfma16(A[s], Q[b][s], S[b][kb]);
+        }
+      }
+      f16x8_t P[QB][2];
+#pragma unroll
+      for (int b = 0; b < QB; ++b) {
+        if constexpr (MODS) {
+          modify(a, w[b], docs, k0, n, ks, masked, S[b]);
+          softmax_step(st[b], S[b], 1.0f, a.mul, ev, P[b]);
+        } else {
+          if (masked) {
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+              for (int x = 0; x < 4; ++x)
+                if (k0 + 16 * kb + 4 * g4 + x > w[b].pos) S[b][kb][x] = -INFINITY;
+          }
+          softmax_step(st[b], S[b], ks, a.mul, ev, P[b]);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < DB; ++c) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const unsigned char* p = sg + va + 32 * x * PITCH + 16 * ((2 * c + (vj >> 1)) ^ vswz);
+          const msk::v4i16_t v0 = msk::lds_read_tr16(p), v1 = msk::lds_read_tr16(p + 16 * PITCH);
+          const f16x8_t A = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int b = 0; b < QB; ++b) st[b].O[c] = mfma_f16(A, P[b][x], st[b].O[c]);
+        }
+      }
+    }
+    msk::bare_barrier();  // the tile is read, the next one staged
+  }
+  bool bad = false;
+#pragma unroll
+  for (int b = 0; b < QB; ++b) {
+    st[b].l += __shfl_xor(st[b].l, 16, 64);
+    st[b].l += __shfl_xor(st[b].l, 32, 64);
+    const float f = st[b].l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(st[b].R) / st[b].l;
+    bad |= !isfinite(st[b].l);
+#pragma unroll
+    for (int c = 0; c < DB; ++c)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        st[b].O[c][x] *= f;
+        bad |= !isfinite(st[b].O[c][x]);
+      }
+  }
+  if (any_thread<kTileThreads / 64>(bad, reinterpret_cast<int*>(kv_lds))) {  // nothing of out is written yet: it may be q
+    __syncthreads();  // the flags are read
+    for (int r = r0 + wave; r < r1; r += kTileThreads / 64)
+      attend_row<D>(a, head, sp, r, tl, i0, i1, z, reinterpret_cast<float*>(kv_lds) + wave * D);
+    return;
+  }
+#pragma unroll
+  for (int b = 0; b < QB; ++b) {
+    const int r = r0 + (wave * QB + b) * 16 + n16;
+    if (r >= r1) continue;
+    if (a.splits == 1) {
+      uint16_t* dst = a.out + q_row(a, head, r) * D + 4 * g4;
+#pragma unroll
+      for (int c = 0; c < DB; ++c)
+        *reinterpret_cast<uint2*>(dst + 16 * c) =
+            make_uint2(f32_to_bf16_bits(st[b].O[c][0]) | f32_to_bf16_bits(st[b].O[c][1]) << 16,
+                       f32_to_bf16_bits(st[b].O[c][2]) | f32_to_bf16_bits(st[b].O[c][3]) << 16);
+    } else {
+      const size_t pr = part_row(a, head, r, z);
+#pragma unroll
+      for (int c = 0; c < DB; ++c)
+        *reinterpret_cast<float4*>(a.part + pr * D + 16 * c + 4 * g4) =
+            make_float4(st[b].O[c][0], st[b].O[c][1], st[b].O[c][2], st[b].O[c][3]);
+      if (g4 == 0) a.ml[pr] = make_float2(st[b].m, st[b].l);
+    }
+  }
+}
+
+// ---- the splits of a row, joined
+//
+// Work-group: one row.  Every wave weighs the splits (lane = split), groups of D / 4
+// threads add up every NG-th of them.
+constexpr int kMostSplits = 64;
+constexpr int kJoinThreads = 256;
+
+template <int D>
+__global__ __launch_bounds__(kJoinThreads) void attention_q_join_kernel(AttArgs a) {
+  constexpr int COLS = D / 4, NG = kJoinThreads / COLS;
+  __shared__ float ws[kMostSplits];
+  __shared__ __align__(16) float sums[NG][D];
+  const int per = a.T * a.G, head = blockIdx.x / per, r = blockIdx.x % per;
+  const Span sp = span_of(a.span, head / a.Hkv, a.pos0, a.T);
+  if (r >= sp.count * a.G) return;
+  const size_t pr = part_row(a, head, r, 0);
+  const int lane = threadIdx.x & 63;
+  const float2 ml = lane < a.splits ? a.ml[pr + lane] : make_float2(-INFINITY, 0.0f);
+  float top = ml.x;
+#pragma unroll
+  for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+  const float w = ml.x == top ? ml.y : ml.y * __builtin_amdgcn_exp2f((ml.x - top) * a.mul);
+  float total = w;
+#pragma unroll
+  for (int x = 32; x >= 1; x >>= 1) total += __shfl_xor(total, x, 64);
+  if (threadIdx.x < 64) ws[lane] = w;
+  __syncthreads();
+  const int c = threadIdx.x % COLS, g = threadIdx.x / COLS;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int z = g; z < a.splits; z += NG) {
+    const float f = ws[z];
+    if (f == 0.0f && a.ml[pr + z].y == 0.0f) continue;  // a share without keys: nothing was written
+    const float4 x = *reinterpret_cast<const float4*>(a.part + (pr + z) * D + 4 * c);
+    v.x = fmaf(f, x.x, v.x), v.y = fmaf(f, x.y, v.y), v.z = fmaf(f, x.z, v.z), v.w = fmaf(f, x.w, v.w);
+  }
+  *reinterpret_cast<float4*>(&sums[g][4 * c]) = v;
+  __syncthreads();
+  if (threadIdx.x < COLS) {
+#pragma unroll
+    for (int x = 1; x < NG; ++x) {
+      const float4 y = *reinterpret_cast<const float4*>(&sums[x][4 * c]);
+      v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
+    }
+    const float f = total == 0.0f ? 0.0f : 1.0f / total;
+    *reinterpret_cast<uint2*>(a.out + q_row(a, head, r) * D + 4 * c) =
+        make_uint2(f32_to_bf16_bits(v.x * f) | f32_to_bf16_bits(v.y * f) << 16,
+                   f32_to_bf16_bits(v.z * f) | f32_to_bf16_bits(v.w * f) << 16);
+  }
+}
+
+// How a call is run.
+struct Plan {
+  bool few;        // attention_q_few_kernel
+  int qb, blocks;  // row blocks of 64 qb otherwise
+  int splits;      // shares of a row's tiles
+};
+
+Plan plan_of(int64_t heads, int T, int G, int D, int pos0, int window, int prefix) {
+  Plan p;
+  const int64_t rows = static_cast<int64_t>(T) * G;
+  int64_t tiles = (static_cast<int64_t>(pos0) + T + kKvBlock - 1) / kKvBlock;
+  p.few = rows <= 16;
+  p.qb = 1;
+  p.blocks = 1;
+  if (!p.few) {
+    p.qb = heads * ((rows + 127) / 128) >= 512 ? 2 : 1;
+    p.blocks = static_cast<int>((rows + 64 * p.qb - 1) / (64 * p.qb));
+  }
+  if (window > 0) {
+    const int64_t tokens = p.few ? T : std::min<int64_t>(T, 64 * p.qb / G + 2);
+    tiles = std::min<int64_t>(tiles, (static_cast<int64_t>(window) + tokens) / kKvBlock + 2 + prefix / kKvBlock + 1);
+  }
+  const int64_t wgs = heads * p.blocks;
+  const int64_t target = p.few ? 512 : 512, least = p.few ? 4 : 4;
+  p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({target / wgs, tiles / least, kMostSplits})));
+  return p;
+}
+
+template <int D>
+ms_status launch_attention_q(const AttArgs& a, const Plan& p, bool mods, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.heads) * p.blocks * p.splits));
+  if (p.few) {
+    constexpr size_t lds = static_cast<size_t>(few_waves(D)) * few_stages(D) * 2 * kStep * D;
+    if (mods)
+      hipLaunchKernelGGL((attention_q_few_kernel<D, true>), grid, dim3(64 * few_waves(D)), lds, s, a);
+    else
+      hipLaunchKernelGGL((attention_q_few_kernel<D, false>), grid, dim3(64 * few_waves(D)), lds, s, a);
+  } else {
+    constexpr size_t lds = size_t{4} * kKvBlock * 2 * D;
+    const dim3 block(kTileThreads);
+    if (p.qb == 2) {
+      if (mods)
+        hipLaunchKernelGGL((attention_q_tile_kernel<D, 2, true>), grid, block, lds, s, a, p.blocks);
+      else
+        hipLaunchKernelGGL((attention_q_tile_kernel<D, 2, false>), grid, block, lds, s, a, p.blocks);
+    } else {
+      if (mods)
+        hipLaunchKernelGGL((attention_q_tile_kernel<D, 1, true>), grid, block, lds, s, a, p.blocks);
+      else
+        hipLaunchKernelGGL((attention_q_tile_kernel<D, 1, false>), grid, block, lds, s, a, p.blocks);
+    }
+  }
+  if (p.splits > 1)
+    hipLaunchKernelGGL(attention_q_join_kernel<D>, dim3(static_cast<unsigned>(a.heads) * a.T * a.G), dim3(kJoinThreads), 0, s, a);
+  return hipGetLastError() == hipSuccess ? MS_OK : MS_E_HIP;
+}
+
+// rows of all sequences that a call may have: grids and row numbers stay in 31 bits
+constexpr int64_t kMostRows = int64_t{1} << 22;
+
+// [rows][splits] results of D floats, maxima and sums
+uint64_t workspace_of(int64_t rows, int splits, int D) {
+  return static_cast<uint64_t>(rows) * splits * (D + 2) * sizeof(float);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -467,6 +1145,13 @@ ms_status ms_attention_q_workspace(const ms_kv_cache_q* cache, int32_t T, int32_
       static_cast<int64_t>(pos0) + T > cache->max_ctx)
     return MS_E_INVALID;
   *bytes_out = 0;
+  if (T == 0) return MS_OK;
+  const int64_t rows = static_cast<int64_t>(T) * Hq;
+  if (rows > kMostRows || rows * cache->n_seqs > kMostRows) return MS_E_UNSUPPORTED;
+  // without a window, which only makes the splits fewer
+  const Plan p = plan_of(static_cast<int64_t>(cache->n_seqs) * cache->n_kv_heads, T, Hq / cache->n_kv_heads, cache->head_dim,
+                         pos0, 0, 0);
+  if (p.splits > 1) *bytes_out = workspace_of(rows * cache->n_seqs, p.splits, cache->head_dim);
   return MS_OK;
 }
 
@@ -476,16 +1161,14 @@ ms_status ms_attention_q(const ms_kv_cache_q* cache, const void* q, int32_t T, i
   uint64_t need = 0;
   if (const ms_status st = ms_attention_q_workspace(cache, T, Hq, pos0, &need); st != MS_OK) return st;
   if (opts && (!(opts->scale >= 0.0f) || !std::isfinite(opts->scale) || !(opts->softcap >= 0.0f) ||
-               !std::isfinite(opts->softcap) || opts->window < 0 || opts->prefix < 0))
+               !std::isfinite(opts->softcap) || opts->window < 0 || opts->prefix < 0 || !aligned16(opts->docs_dev)))
     return MS_E_INVALID;
   if (T == 0) return MS_OK;
   if (!cache_pointers(cache) || !q || !out || !aligned16(q) || !aligned16(out)) return MS_E_INVALID;
   if (need > 0 && (!workspace_dev || !aligned16(workspace_dev) || workspace_bytes < need)) return MS_E_INVALID;
   const int D = cache->head_dim;
-  const int64_t rows = static_cast<int64_t>(T) * Hq;  // of a sequence
-  constexpr int64_t kMostRows = int64_t{1} << 31;
-  if (rows > kMostRows || rows * cache->n_seqs > kMostRows) return MS_E_UNSUPPORTED;
-  const uint64_t bytes = static_cast<uint64_t>(rows) * cache->n_seqs * D * sizeof(uint16_t);
+  const int64_t rows = static_cast<int64_t>(T) * Hq * cache->n_seqs;  // at most kMostRows
+  const uint64_t bytes = static_cast<uint64_t>(rows) * D * sizeof(uint16_t);
   const auto qa = reinterpret_cast<uintptr_t>(q), oa = reinterpret_cast<uintptr_t>(out);
   if (qa != oa && qa < oa + bytes && oa < qa + bytes) return MS_E_INVALID;
   AttArgs a;
@@ -504,22 +1187,23 @@ ms_status ms_attention_q(const ms_kv_cache_q* cache, const void* q, int32_t T, i
   a.G = Hq / cache->n_kv_heads;
   a.max_ctx = cache->max_ctx;
   a.pos0 = pos0;
+  a.heads = cache->n_seqs * cache->n_kv_heads;
   a.window = opts ? opts->window : 0;
   a.prefix = opts ? opts->prefix : 0;
-  a.scale = opts && opts->scale > 0.0f ? opts->scale : 1.0f / std::sqrt(static_cast<float>(D));
   a.cap = opts ? opts->softcap : 0.0f;
-  constexpr int kWaves = kRowThreads / 64;
-  const int64_t wgs = (rows * cache->n_seqs + kWaves - 1) / kWaves;
-  if (wgs > UINT32_MAX / kRowThreads) return MS_E_UNSUPPORTED;
-  const dim3 grid(static_cast<unsigned>(wgs)), block(kRowThreads);
+  const float scale = opts && opts->scale > 0.0f ? opts->scale : 1.0f / std::sqrt(static_cast<float>(D));
+  const bool scores = a.cap > 0.0f || a.slopes;  // more than the product's scale
+  a.pre = scores ? scale : 1.0f;
+  a.mul = scores ? kLog2e : scale * kLog2e;
+  const Plan p = plan_of(a.heads, T, a.G, D, pos0, a.window, a.prefix);
+  a.splits = p.splits;
+  a.part = static_cast<float*>(workspace_dev);
+  a.ml = reinterpret_cast<float2*>(a.part + rows * p.splits * D);
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (D == 64)
-    hipLaunchKernelGGL(attention_q_kernel<64>, grid, block, 0, s, a, cache->n_seqs);
-  else if (D == 128)
-    hipLaunchKernelGGL(attention_q_kernel<128>, grid, block, 0, s, a, cache->n_seqs);
-  else
-    hipLaunchKernelGGL(attention_q_kernel<256>, grid, block, 0, s, a, cache->n_seqs);
-  return launched();
+  const bool mods = scores || a.window > 0 || a.prefix > 0 || a.docs;
+  if (D == 64) return launch_attention_q<64>(a, p, mods, s);
+  if (D == 128) return launch_attention_q<128>(a, p, mods, s);
+  return launch_attention_q<256>(a, p, mods, s);
 }
 
 }  // extern "C"
