@@ -31,9 +31,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ uint32_t f32_to_bf16_bits(float f) {
-  const uint32_t u = __float_as_uint(f);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return (u >> 16) | 0x40u;  // NaN stays NaN
-  return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f));  // to nearest even, NaN stays NaN
 }
 
 // 2^e, e in [-126, 127]
@@ -248,7 +246,7 @@ struct AttArgs {
   const int32_t* docs;
   uint16_t* out;
   float* part;  // splits > 1: [rows][splits][D] results of a share of the keys
-  float2* ml;   // [rows][splits] their maxima and sums
+  float2* ml;   // [rows][splits] the exponent that their sums are relative to (-inf: no key), and the sums
   int T, Hq, Hkv, G, max_ctx, pos0, heads, splits;  // heads: key/value heads of all sequences
   int window, prefix;
   float pre, cap, mul;  // score = pre q.k, capped and biased; weight = 2^(mul (score - maximum))
@@ -300,6 +298,24 @@ __device__ __forceinline__ size_t q_row(const AttArgs& a, int head, int r) {
 __device__ __forceinline__ size_t part_row(const AttArgs& a, int head, int r, int z) {
   return (static_cast<size_t>(head) * a.T * a.G + r) * a.splits + z;
 }
+
+// The scales' exponents of 64 list places of a share [i0, i1), one per lane: read
+// in the loop by lane, so that no load of theirs makes the loop wait for others.
+struct Exps {
+  int chunk = -1, both = 0;
+  __device__ __forceinline__ void at(const Tiles& tl, int i0, int i1, int i, const uint8_t* ke, const uint8_t* ve, int& ek,
+                                     int& ev) {
+    const int d = i - i0;
+    if (d / 64 != chunk) {
+      chunk = d / 64;
+      const int tile = tl.at(min(i0 + 64 * chunk + static_cast<int>(threadIdx.x & 63), i1 - 1));
+      both = exponent(ke[tile]) << 16 | (exponent(ve[tile]) & 0xffff);
+    }
+    const int x = __builtin_amdgcn_readlane(both, d & 63);
+    ek = x >> 16;
+    ev = static_cast<int16_t>(x);
+  }
+};
 
 // One query row over the tiles [i0, i1) of `tl`, by one wave: lane j of a tile
 // has key j's score, then D / 64 columns of the output.  Reads no value that
@@ -378,7 +394,7 @@ __device__ __forceinline__ void attend_row(const AttArgs& a, int head, const Spa
     else
       a.part[pr * D + CPL * lane + c] = v;
   }
-  if (a.splits > 1 && lane == 0) a.ml[pr] = make_float2(m, l);
+  if (a.splits > 1 && lane == 0) a.ml[pr] = make_float2(m * a.mul, l);
 }
 
 // ---- one step of the softmax, shared by the two matrix-core kernels
@@ -388,80 +404,87 @@ __device__ __forceinline__ void attend_row(const AttArgs& a, int head, const Spa
 // key block b; O^T += V^T P^T takes the probabilities where they are, as fp16
 // pairs, contraction slot 4 h + r of lane group g being key 16 h + 4 g + r of 32.
 //
-// Scales: a key block's 2^ek multiplies the raw score (exact), a value block's
-// 2^ev goes into the probability's exponent.  A row keeps its maximum m (in
-// scores before `mul`, subtracted before the exponent is scaled: the largest
-// key gets an exact power of two however large its score) and its sum l relative
-// to m, and an exponent R with O = sum 2^(mul (s - m) + ev - R) code.  R keeps
-// the fp16 probabilities below 2^15, its aim is 2^7 for the largest: half a step
-// is 2^-11 of a probability and the smallest step 2^-31 of the largest weight.
-// One fp16 part is enough here: the 3-bit mantissa of the codes it meets is
-// 2^-4 off already.  m and R move only when they have to (kGrow), so most tiles
-// rescale nothing.
+// A score's exponent is y = c S, c = mul times the key block's scale.  A row keeps
+// its sum l = sum 2^(y - L) and O = sum 2^(y + ev - A) code, ev the value block's
+// exponent; L and A are whole numbers, so that c S - A is one fma that rounds once
+// whatever their size, and rescaling by their changes is exact.  A keeps the fp16
+// probabilities below 2^15 with the largest at 2^6 to 2^7 when it is set: half a
+// step is 2^-11 of a probability and the smallest step 2^-30 of the largest
+// weight or less.  One fp16 part is enough here: the 3-bit mantissa of the codes
+// that it meets is 2^-4 off already.  The sum is taken of the same fp16
+// probabilities by the matrix cores (a column of ones), in 32 bits.  L and A move
+// only when they have to, so most tiles rescale nothing.  Exponents past 2^24
+// (kHuge), where whole numbers are no longer exact, leave the row to attend_row.
 constexpr float kAim = 7.0f, kMost = 15.0f, kGrow = 40.0f;
+constexpr float kNone = -1073741824.0f;  // L and A of a row without keys
+constexpr float kHuge = 16777216.0f;
 
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
+__device__ __forceinline__ msk::f32x4_t mfma_f16(f16x8_t a, f16x8_t b, msk::f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// maximum, NaN if one is
+__device__ __forceinline__ float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 // maximum over the lanes l, l ^ 16, l ^ 32, l ^ 48
 __device__ __forceinline__ float group_max(float v) {
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  v = max_of(__uint_as_float(a[0]), __uint_as_float(a[1]));
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+  return max_of(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 template <int DB>
 struct RowState {
-  float m = -INFINITY, l = 0.0f, R = 0.0f;
+  float l = 0.0f, L = kNone, A = kNone, best = -INFINITY;  // best: the largest exponent
   msk::f32x4_t O[DB];
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int c = 0; c < DB; ++c) O[c] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
+  // whether the row has to be left to attend_row
+  __device__ __forceinline__ bool lost() const { return !isfinite(l) || (fabsf(best) > kHuge && best != -INFINITY); }
 };
 
-// Scores of NB key blocks (NB / 2 fragments of P) into probabilities.  ks: the
-// keys' scale; mul, ev as above.
+// The largest of a row's scores of NB key blocks, and what it moves.
 template <int NB, int DB>
-__device__ __forceinline__ void softmax_step(RowState<DB>& st, const msk::f32x4_t (&S)[NB], float ks, float mul, float ev,
-                                             f16x8_t (&P)[NB / 2]) {
+__device__ __forceinline__ void softmax_max(RowState<DB>& st, const msk::f32x4_t (&S)[NB], float c, float ev) {
   float top = S[0][0];
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) top = fmaxf(top, S[b][r]);
-  top = group_max(top) * ks;
-  const float dx = (top - st.m) * mul;
-  if (__any(dx > kGrow || dx + ev - st.R > kMost)) {
-    const float next = fmaxf(st.m, top);
-    if (next != -INFINITY) {
-      const float dl = st.m == next ? 0.0f : (st.m - next) * mul;
-      const float was = st.R + dl;  // R relative to the new maximum
-      const float R = fmaxf(was, (top - next) * mul + ev - kAim);
-      const float f = __builtin_amdgcn_exp2f(was - R);
-      st.l *= __builtin_amdgcn_exp2f(dl);
+    for (int r = 0; r < 4; ++r) top = max_of(top, S[b][r]);
+  const float y = group_max(top) * c;
+  st.best = fmaxf(st.best, y);
+  if (__any(y - st.L > kGrow || y + ev - st.A > kMost)) {
+    const float up = ceilf(y);  // -inf where the row sees nothing
+    const float L = fmaxf(st.L, up), A = fmaxf(st.A, up + ev - kAim);
+    st.l *= __builtin_amdgcn_exp2f(st.L - L);
+    const float f = __builtin_amdgcn_exp2f(st.A - A);
 #pragma unroll
-      for (int c = 0; c < DB; ++c) st.O[c] *= f;
-      st.m = next;
-      st.R = R;
-    }
+    for (int x = 0; x < DB; ++x) st.O[x] *= f;
+    st.L = L;
+    st.A = A;
   }
-  const float base = st.m == -INFINITY ? 0.0f : st.m, off = ev - st.R;
-  float sum = 0.0f;
+}
+
+// Two probabilities: those of the scores s0 and s1.
+__device__ __forceinline__ uint32_t softmax_pair(float s0, float s1, float c, float off) {
+  const f32x2_t p = {__builtin_amdgcn_exp2f(fmaf(s0, c, off)), __builtin_amdgcn_exp2f(fmaf(s1, c, off))};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(p, f16x2_t));
+}
+
+// Adds the probabilities' sum.
+template <int NP, int DB>
+__device__ __forceinline__ void softmax_sum(RowState<DB>& st, const f16x8_t (&P)[NP], float ev) {
+  const f16x8_t ones = {1, 1, 1, 1, 1, 1, 1, 1};
+  msk::f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    float p[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(fmaf(S[b][r], ks, -base), mul, off));
-    sum += (p[0] + p[1]) + (p[2] + p[3]);
-    const f16x2_t lo = __builtin_convertvector(f32x2_t{p[0], p[1]}, f16x2_t);
-    const f16x2_t hi = __builtin_convertvector(f32x2_t{p[2], p[3]}, f16x2_t);
-    f16x8_t& d = P[b / 2];
-    const int o = 4 * (b % 2);
-    d[o] = lo[0], d[o + 1] = lo[1], d[o + 2] = hi[0], d[o + 3] = hi[1];
-  }
-  st.l = fmaf(sum, __builtin_amdgcn_exp2f(-off), st.l);
+  for (int x = 0; x < NP; ++x) sum = mfma_f16(ones, P[x], sum);
+  st.l = fmaf(sum[0], __builtin_amdgcn_exp2f(st.A - ev - st.L), st.l);
 }
 
 // A lane's row: what its scores and masks depend on.
@@ -515,8 +538,9 @@ __device__ __forceinline__ uint2 codes_to_f16(uint32_t c) {
   return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(c), 1.0f, false)),
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(c), 1.0f, true)));
 }
-__device__ __forceinline__ msk::f32x4_t mfma_f16(f16x8_t a, f16x8_t b, msk::f32x4_t c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+__device__ __forceinline__ uint4 codes_f16(uint32_t lo, uint32_t hi) {
+  const uint2 a = codes_to_f16(lo), b = codes_to_f16(hi);
+  return make_uint4(a.x, a.y, b.x, b.y);
 }
 
 // Whether v holds in any thread of WAVES waves; flags: WAVES ints of LDS that no
@@ -584,7 +608,6 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
   const uint32_t lbase = msk::lds_address(ring);
   const int lrow = lane / PIECES, slot = lane % PIECES;
   auto key0 = [&](int s) { return tl.at(i0 + (s >> 1)) * kKvBlock + (s & 1) * kStep; };
-  int kexp[2], vexp[2];  // of this step and the next
   auto issue = [&](int s, int buf) {  // steps past the wave's last reload the share's last one (never read)
     const int k0 = key0(min(s, steps - 1));
 #pragma unroll
@@ -605,12 +628,7 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
   }
 #pragma unroll
   for (int p = 0; p < NST - 1; ++p) issue(wave + NW * p, p);
-  auto load_exps = [&](int s, int at) {
-    const int tile = tl.at(i0 + (min(s, steps - 1) >> 1));
-    kexp[at] = ke[tile];
-    vexp[at] = ve[tile];
-  };
-  load_exps(wave, 0);
+  Exps exps;
   int va;  // this lane's 8 bytes of column block 0
   {
     const int x = (lane >> 1) & 7, u = (x < 4 ? 0 : 12) + 4 * g4 + x;  // x >= 4: key 16 + 4 g + x - 4
@@ -621,7 +639,8 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
   st.clear();
   int cur = 0, nxt = NST - 1;
   for (int s = wave; s < steps; s += NW) {
-    load_exps(s + NW, 1);
+    int ek, ve_s;
+    exps.at(tl, i0, i1, i0 + (s >> 1), ke, ve, ek, ve_s);
     msk::wait_vm<(NST - 2) * NL>();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     issue(s + NW * (NST - 1), nxt);
@@ -642,23 +661,23 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
       }
     }
     const bool last = k0 + kStep > n;
-    const float ks = pow2(exponent(static_cast<uint8_t>(kexp[0]))), ev = static_cast<float>(exponent(static_cast<uint8_t>(vexp[0])));
-    kexp[0] = kexp[1];
-    vexp[0] = vexp[1];
+    const float ks = pow2(ek), ev = static_cast<float>(ve_s);
     f16x8_t P[1];
+    const float c = MODS ? a.mul : a.mul * ks;
     if constexpr (MODS) {
       modify(a, w, docs, k0, n, ks, true, S);
-      softmax_step(st, S, 1.0f, a.mul, ev, P);
-    } else {
-      if (k0 + kStep > sp.start + 1) {
+    } else if (k0 + kStep > sp.start + 1) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
-            if (k0 + 16 * b + 4 * g4 + x > w.pos) S[b][x] = -INFINITY;
-      }
-      softmax_step(st, S, ks, a.mul, ev, P);
+        for (int x = 0; x < 4; ++x)
+          if (k0 + 16 * b + 4 * g4 + x > w.pos) S[b][x] = -INFINITY;
     }
+    softmax_max(st, S, c, ev);
+    const float off = ev - st.A;
+    P[0] = __builtin_bit_cast(f16x8_t, make_uint4(softmax_pair(S[0][0], S[0][1], c, off), softmax_pair(S[0][2], S[0][3], c, off),
+                                                  softmax_pair(S[1][0], S[1][1], c, off), softmax_pair(S[1][2], S[1][3], c, off)));
+    softmax_sum(st, P, ev);
 #pragma unroll
     for (int c = 0; c < DB; ++c) {
       uint2 t = msk::lds_read_tr8(sg + va + 16 * (c ^ vswz));
@@ -676,18 +695,16 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
   }
   msk::wait_vm<0>();  // the reloads past the last step have landed
   __syncthreads();    // every wave is done with its ring
-  float l = st.l;
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
   float* part = reinterpret_cast<float*>(kv_lds);  // [NW][16][PP]
-  float* mx = part + NW * 16 * PP;                 // [NW][16], and the sums and exponents
+  float* mx = part + NW * 16 * PP;                 // [NW][16] L, then l and A
   float *sm = mx + NW * 16, *rx = sm + NW * 16;
   int* flags = reinterpret_cast<int*>(rx + NW * 16);
+  bool bad = n16 < rows && st.lost();
   if (n16 < rows) {
     if (g4 == 0) {
-      mx[wave * 16 + n16] = st.m;
-      sm[wave * 16 + n16] = l;
-      rx[wave * 16 + n16] = st.R;
+      mx[wave * 16 + n16] = st.L;
+      sm[wave * 16 + n16] = st.l;
+      rx[wave * 16 + n16] = st.A;
     }
 #pragma unroll
     for (int c = 0; c < DB; ++c)
@@ -698,7 +715,6 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
   const int used = min(NW, steps);  // waves with a step
   constexpr int NV = 16 * D / (64 * NW);
   float val[NV];
-  bool bad = false;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int i = k * 64 * NW + threadIdx.x, row = i / D, col = i % D;
@@ -708,13 +724,12 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
     for (int x = 1; x < used; ++x) top = fmaxf(top, mx[x * 16 + row]);
     float num = 0.0f, den = 0.0f;
     for (int x = 0; x < used; ++x) {
-      const float m = mx[x * 16 + row], d = m == top ? 0.0f : (m - top) * a.mul;
-      den += sm[x * 16 + row] * __builtin_amdgcn_exp2f(d);
-      num += part[(x * 16 + row) * PP + col] * __builtin_amdgcn_exp2f(rx[x * 16 + row] + d);
+      den += sm[x * 16 + row] * __builtin_amdgcn_exp2f(mx[x * 16 + row] - top);
+      num += part[(x * 16 + row) * PP + col] * __builtin_amdgcn_exp2f(rx[x * 16 + row] - top);
     }
     val[k] = den == 0.0f ? 0.0f : num / den;
-    bad |= !isfinite(val[k]) || !isfinite(den);
-    if (a.splits > 1 && col == 0) a.ml[part_row(a, head, row, z)] = make_float2(top, den);
+    bad |= !isfinite(val[k]);
+    if (a.splits > 1 && col == 0) a.ml[part_row(a, head, row, z)] = make_float2(den == 0.0f ? -INFINITY : top, den);
   }
   if (any_thread<NW>(bad, flags)) {  // nothing of out is written yet: it may be q
     for (int row = wave; row < rows; row += NW) attend_row<D>(a, head, sp, row, tl, i0, i1, z, part + wave * D);
@@ -734,24 +749,19 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
 // ---- prompts
 //
 // A work-group takes 64 QB rows of one key/value head, a wave 16 QB of them, over
-// its share of the tiles of 64 keys.  A tile's codes go through registers, where
-// they become bf16 keys and fp16 values once for all waves, into LDS, two stages: the
-// loads of the tile after next are in flight while a tile is computed.  16-byte
-// piece p of key row u sits in slot p ^ tile_key_slot(u), of value row u in p ^
-// tile_value_slot(u), free of bank conflicts for the reads.
-constexpr int kTileThreads = 256;
-
-template <int D>
-__device__ __forceinline__ int tile_key_slot(int u) { return (D == 64 ? u >> 1 : u) & (D == 64 ? 7 : 15); }
-template <int D>
-__device__ __forceinline__ int tile_value_slot(int u) { return 2 * ((D == 64 ? u >> 1 : u) & (D == 64 ? 3 : 7)); }
-
-template <int D, int QB, bool MODS>
-__global__ __launch_bounds__(kTileThreads, D == 256 ? 1 : 2) void attention_q_tile_kernel(AttArgs a, int blocks) {
-  constexpr int ROWS = 64 * QB, KS = D / 32, DB = D / 16;
-  constexpr int PITCH = 2 * D, TILE = kKvBlock * PITCH;  // bytes of a converted row and tile
-  constexpr int PIECES = D / 16, NP = kKvBlock * PIECES / kTileThreads;
-  extern __shared__ __align__(16) unsigned char kv_lds[];
+// its share of the tiles of 64 keys.  Codes come to LDS by direct loads, a tile
+// ahead, and become operands when a wave reads them, as above: the conversions
+// run beside the matrix instructions, and LDS holds and moves a byte per value.
+template <int D, int QB, int NW, bool MODS>
+__global__ __launch_bounds__(64 * NW, NW / 2) void attention_q_tile_kernel(AttArgs a, int blocks) {
+  constexpr int kTileThreads = 64 * NW;
+  constexpr int ROWS = 16 * NW * QB, KS = D / 32, DB = D / 16;
+  constexpr int PIECES = D / 16, RPL = 64 / PIECES;  // 16-byte pieces of a row, rows per load
+  constexpr int TILE = kKvBlock * D, NL = TILE / 1024 / NW;  // bytes of a tile's keys (or values), their loads per wave
+  static_assert(NL >= 1 && NL * NW * 1024 == TILE, "loads");
+  extern __shared__ __align__(16) unsigned char kv_lds[];  // two stages of a tile's keys and values
+  __shared__ int doc_s[2 * kTileThreads / 64];
+  __shared__ uint32_t near_s[4];
   const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = blockIdx.x % a.heads, zj = blockIdx.x / a.heads, j = zj % blocks, z = zj / blocks, seq = head / a.Hkv;
@@ -771,74 +781,131 @@ __global__ __launch_bounds__(kTileThreads, D == 256 ? 1 : 2) void attention_q_ti
   }
   const uint8_t *K = a.k + kv_row(a, head) * D, *V = a.v + kv_row(a, head) * D;
   const uint8_t *ke = a.k_exp + exp_row(a, head), *ve = a.v_exp + exp_row(a, head);
-  const int32_t* docs = a.docs ? a.docs + static_cast<size_t>(seq) * a.max_ctx : nullptr;
+  const int32_t* docs = MODS && a.docs ? a.docs + static_cast<size_t>(seq) * a.max_ctx : nullptr;
 
-  uint4 kr[NP], vr[NP];  // codes of the tile to stage
-  int kexp, vexp;
-  auto load = [&](int i) {
-    const int tile = tl.at(min(i, i1 - 1));
-    const size_t at = static_cast<size_t>(tile) * kKvBlock * D + 16 * threadIdx.x;
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      kr[p] = *reinterpret_cast<const uint4*>(K + at + p * kTileThreads * 16);
-      vr[p] = *reinterpret_cast<const uint4*>(V + at + p * kTileThreads * 16);
-    }
-    kexp = ke[tile];
-    vexp = ve[tile];
-  };
-  auto stage = [&](int i, unsigned char* to) {
-    const int k0 = tl.at(min(i, i1 - 1)) * kKvBlock;
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      const int id = p * kTileThreads + threadIdx.x, u = id / PIECES, c = id % PIECES;
-      unsigned char* row = to + u * PITCH;
-      const int sk = tile_key_slot<D>(u), sv = tile_value_slot<D>(u);
-      *reinterpret_cast<uint4*>(row + 16 * ((2 * c) ^ sk)) = __builtin_bit_cast(uint4, codes_bf16(kr[p].x, kr[p].y));
-      *reinterpret_cast<uint4*>(row + 16 * ((2 * c + 1) ^ sk)) = __builtin_bit_cast(uint4, codes_bf16(kr[p].z, kr[p].w));
-      if (k0 + u >= n) vr[p] = make_uint4(0, 0, 0, 0);  // past the end may be anything
-      const uint2 a0 = codes_to_f16(vr[p].x), a1 = codes_to_f16(vr[p].y), a2 = codes_to_f16(vr[p].z), a3 = codes_to_f16(vr[p].w);
-      *reinterpret_cast<uint4*>(row + TILE + 16 * ((2 * c) ^ sv)) = make_uint4(a0.x, a0.y, a1.x, a1.y);
-      *reinterpret_cast<uint4*>(row + TILE + 16 * ((2 * c + 1) ^ sv)) = make_uint4(a2.x, a2.y, a3.x, a3.y);
-    }
-  };
-  load(i0);
   Row w[QB];
   msk::bf16x8_t Q[QB][KS];
 #pragma unroll
   for (int b = 0; b < QB; ++b) {
     const int r = min(r0 + (wave * QB + b) * 16 + n16, r1 - 1);  // rows past the last repeat it (never stored)
     w[b] = row_of(a, head, sp, r);
-    const uint16_t* qr = a.q + q_row(a, head, r) * D + 8 * g4;
+    const uint16_t* qr = a.q + q_row(a, head, r) * D + 16 * g4;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) Q[b][s] = msk::as_bf16x8(*reinterpret_cast<const uint4*>(qr + 32 * s));
+    for (int s = 0; s < KS; ++s) Q[b][s] = msk::as_bf16x8(*reinterpret_cast<const uint4*>(qr + 64 * (s >> 1) + 8 * (s & 1)));
   }
+
+  // documents: only tiles with a key of a document between the rows' least and
+  // largest are visited; 64 tiles are looked at at a time
+  int d_min = INT32_MAX, d_max = -1, chunk = -1;
+  uint64_t near = ~uint64_t{0};
+  if constexpr (MODS) {
+    if (docs) {
+#pragma unroll
+      for (int b = 0; b < QB; ++b)
+        if (w[b].doc >= 0) {
+          d_min = min(d_min, w[b].doc);
+          d_max = max(d_max, w[b].doc);
+        }
+#pragma unroll
+      for (int x = 8; x >= 1; x >>= 1) {
+        d_min = min(d_min, __shfl_xor(d_min, x, 64));
+        d_max = max(d_max, __shfl_xor(d_max, x, 64));
+      }
+      if (lane == 0) {
+        doc_s[wave] = d_min;
+        doc_s[kTileThreads / 64 + wave] = d_max;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int x = 0; x < kTileThreads / 64; ++x) {
+        d_min = min(d_min, doc_s[x]);
+        d_max = max(d_max, doc_s[kTileThreads / 64 + x]);
+      }
+    }
+  }
+  // the first tile to visit from i on (the same in every thread)
+  auto advance = [&](int i) {
+    if constexpr (MODS) {
+      if (docs) {
+        while (i < i1) {
+          if ((i - i0) / 64 != chunk) {  // wave: 16 tiles, lane: a quarter of one
+            chunk = (i - i0) / 64;
+            const int t = i0 + 64 * chunk + 16 * wave + (lane >> 2);
+            bool hit = false;
+            if (wave < 4 && t < i1) {
+              const int4* d = reinterpret_cast<const int4*>(docs + tl.at(t) * kKvBlock + 16 * (lane & 3));
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const int4 v = d[x];
+                hit |= (v.x >= d_min && v.x <= d_max) || (v.y >= d_min && v.y <= d_max) || (v.z >= d_min && v.z <= d_max) ||
+                       (v.w >= d_min && v.w <= d_max);
+              }
+            }
+            uint64_t h = __ballot(hit);
+            h |= h >> 1;
+            h |= h >> 2;  // bit 4 k: tile k
+            uint32_t bits = 0;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) bits |= static_cast<uint32_t>((h >> (4 * x)) & 1) << x;
+            __syncthreads();  // the chunk before is read
+            if (lane == 0 && wave < 4) near_s[wave] = bits;
+            __syncthreads();
+            near = 0;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) near |= static_cast<uint64_t>(near_s[x]) << (16 * x);
+          }
+          const uint64_t rest = near >> ((i - i0) & 63);
+          if (rest) return i + static_cast<int>(__builtin_ctzll(rest));
+          i = i0 + 64 * (chunk + 1);
+        }
+        return i1;
+      }
+    }
+    return min(i, i1);
+  };
+
+  int at_k[NL], at_v[NL];  // this lane's bytes of its wave's loads
+  uint32_t to[NL];
+#pragma unroll
+  for (int x = 0; x < NL; ++x) {
+    const int u = (wave + NW * x) * RPL + lane / PIECES;
+    at_k[x] = u * D + 16 * (lane % PIECES ^ key_slot<D>(u));
+    at_v[x] = u * D + 16 * (lane % PIECES ^ value_slot<D>(u));
+    to[x] = msk::lds_address(kv_lds) + (wave + NW * x) * 1024;
+  }
+  auto issue = [&](int i, int buf) {  // past the last tile: that one again (never read)
+    const size_t k0 = static_cast<size_t>(tl.at(min(i, i1 - 1))) * kKvBlock * D;
+#pragma unroll
+    for (int x = 0; x < NL; ++x) {
+      msk::lds_load16(K + k0 + at_k[x], to[x] + buf * 2 * TILE);
+      msk::lds_load16(V + k0 + at_v[x], to[x] + buf * 2 * TILE + TILE);
+    }
+  };
   // positions of the wave's first and last rows
   const int p_min = sp.start + min(r0 + wave * QB * 16, r1 - 1) / a.G;
   const int p_max = sp.start + min(r0 + (wave + 1) * QB * 16 - 1, r1 - 1) / a.G;
-  int ka[KS];
+  const unsigned char* ka[KS / 2];  // this lane's 16 bytes of keys 0 .. 15
 #pragma unroll
-  for (int s = 0; s < KS; ++s) ka[s] = n16 * PITCH + 16 * ((4 * s + g4) ^ tile_key_slot<D>(n16));
-  const int vrow = 4 * g4 + ((lane >> 2) & 3), vj = lane & 3;
-  const int va = TILE + vrow * PITCH + 8 * (vj & 1), vswz = tile_value_slot<D>(vrow);
+  for (int x = 0; x < KS / 2; ++x) ka[x] = kv_lds + n16 * D + 16 * ((4 * x + g4) ^ key_slot<D>(n16));
+  const int vx = (lane >> 1) & 7, vrow = (vx < 4 ? 0 : 12) + 4 * g4 + vx;  // vx >= 4: key 16 + 4 g + vx - 4
+  const unsigned char* const va = kv_lds + TILE + vrow * D + 8 * (lane & 1);
+  const int vswz = value_slot<D>(vrow);
   RowState<DB> st[QB];
 #pragma unroll
   for (int b = 0; b < QB; ++b) st[b].clear();
 
-  int ks_c = kexp, ev_c = vexp;  // of the tile to compute
-  stage(i0, kv_lds);
-  load(i0 + 1);
-  msk::bare_barrier();
-  for (int i = i0; i < i1; ++i) {
-    unsigned char* sg = kv_lds + ((i - i0) & 1) * 2 * TILE;
-    const float ks = pow2(exponent(static_cast<uint8_t>(ks_c))), ev = static_cast<float>(exponent(static_cast<uint8_t>(ev_c)));
-    if (i + 1 < i1) {
-      ks_c = kexp;
-      ev_c = vexp;
-      stage(i + 1, kv_lds + ((i + 1 - i0) & 1) * 2 * TILE);
-      load(i + 2);
-    }
-    const int k0 = tl.at(i) * kKvBlock;
-    bool skip, masked;  // whether no row of the wave sees the tile, and whether each sees all of it
+  int it = advance(i0), nx = advance(it + 1);  // this tile and the next
+  Exps exps;
+  // A tile in pieces whose order is kept (sched_barrier), so that matrix
+  // instructions run beside vector work: conversions, and the second half's
+  // exponentials beside the first half's values.  Codes are read three pieces ahead.
+  auto step = [&](int p) {
+    const int k0 = tl.at(it) * kKvBlock;
+    int ek, ve_it;
+    exps.at(tl, i0, i1, it, ke, ve, ek, ve_it);
+    const float ks = pow2(ek), ev = static_cast<float>(ve_it);
+    const float c = MODS ? a.mul : a.mul * ks;
+    bool skip, masked;  // whether no row of the wave sees the tile, and whether some do not see all of it
     if constexpr (MODS) {
       skip = !((k0 <= p_max && (a.window <= 0 || k0 + kKvBlock - 1 > p_min - a.window)) || k0 < a.prefix);
       masked = docs || !((k0 + kKvBlock - 1 <= p_min && (a.window <= 0 || p_max - k0 < a.window)) ||
@@ -847,58 +914,106 @@ __global__ __launch_bounds__(kTileThreads, D == 256 ? 1 : 2) void attention_q_ti
       skip = k0 > p_max;
       masked = k0 + kKvBlock - 1 > p_min;
     }
+    const int after = advance(nx + 1);
+    msk::wait_vm<0>();
+    msk::bare_barrier();  // the tile is staged, the other stage is read
+    issue(nx, p ^ 1);
+    if (n - k0 < kKvBlock) {  // values past the end may be anything: code 0
+      for (int x = (n - k0) * D + 16 * threadIdx.x; x < TILE; x += 16 * kTileThreads)
+        *reinterpret_cast<uint4*>(kv_lds + p * 2 * TILE + TILE + x) = make_uint4(0, 0, 0, 0);
+      msk::bare_barrier();
+    }
     if (!skip) {
       msk::f32x4_t S[QB][4];
+      {
+        uint4 A[3];
+        auto key = [&](int f) { return *reinterpret_cast<const uint4*>(ka[f / 4] + p * 2 * TILE + f % 4 * 16 * D); };
 #pragma unroll
-      for (int kb = 0; kb < 4; ++kb) {
-        msk::bf16x8_t A[KS];
+        for (int f = 0; f < 2; ++f) A[f] = key(f);
 #pragma unroll
-        for (int s = 0; s < KS; ++s) A[s] = msk::lds_frag(sg + kb * 16 * PITCH + ka[s]);
+        for (int f = 0; f < 2 * KS; ++f) {
+          if (f + 2 < 2 * KS) A[(f + 2) % 3] = key(f + 2);
+          const uint4 c = A[f % 3];
+          const msk::bf16x8_t lo = codes_bf16(c.x, c.y), hi = codes_bf16(c.z, c.w);
 #pragma unroll
-        for (int b = 0; b < QB; ++b) {
-          S[b][kb] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
+          for (int b = 0; b < QB; ++b)
+            S[b][f % 4] = msk::mfma16(lo, Q[b][f / 4 * 2], f < 4 ? msk::f32x4_t{0.f, 0.f, 0.f, 0.f} : S[b][f % 4]);
 #pragma unroll
-          for (int s = 0; s < KS; ++s) S[b][kb] = msk::mfma16(A[s], Q[b][s], S[b][kb]);
+          for (int b = 0; b < QB; ++b) S[b][f % 4] = msk::mfma16(hi, Q[b][f / 4 * 2 + 1], S[b][f % 4]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
-      f16x8_t P[QB][2];
 #pragma unroll
       for (int b = 0; b < QB; ++b) {
         if constexpr (MODS) {
           modify(a, w[b], docs, k0, n, ks, masked, S[b]);
-          softmax_step(st[b], S[b], 1.0f, a.mul, ev, P[b]);
-        } else {
-          if (masked) {
+        } else if (masked) {
 #pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
+          for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-              for (int x = 0; x < 4; ++x)
-                if (k0 + 16 * kb + 4 * g4 + x > w[b].pos) S[b][kb][x] = -INFINITY;
-          }
-          softmax_step(st[b], S[b], ks, a.mul, ev, P[b]);
+            for (int x = 0; x < 4; ++x)
+              if (k0 + 16 * kb + 4 * g4 + x > w[b].pos) S[b][kb][x] = -INFINITY;
         }
+        softmax_max(st[b], S[b], c, ev);
+      }
+      uint32_t P[QB][2][4];
+      float off[QB];
+#pragma unroll
+      for (int b = 0; b < QB; ++b) off[b] = ev - st[b].A;
+      auto pair = [&](int b, int h, int i) {
+        const msk::f32x4_t& v = S[b][2 * h + i / 2];
+        P[b][h][i] = softmax_pair(v[2 * (i % 2)], v[2 * (i % 2) + 1], c, off[b]);
+      };
+      auto operand = [&](int b, int h) {
+        return __builtin_bit_cast(f16x8_t, make_uint4(P[b][h][0], P[b][h][1], P[b][h][2], P[b][h][3]));
+      };
+      auto value = [&](int f) {  // 16 columns of 32 keys
+        return msk::lds_read_tr8(va + p * 2 * TILE + 32 * (f / DB) * D + 16 * ((f % DB) ^ vswz));
+      };
+      uint2 A[4];
+#pragma unroll
+      for (int f = 0; f < 3; ++f) A[f] = value(f);
+#pragma unroll
+      for (int b = 0; b < QB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pair(b, 0, i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int f = 0; f < 2 * DB; ++f) {
+        if (f + 3 < 2 * DB) A[(f + 3) % 4] = value(f + 3);
+        const f16x8_t v = __builtin_bit_cast(f16x8_t, codes_f16(A[f % 4].x, A[f % 4].y));
+#pragma unroll
+        for (int b = 0; b < QB; ++b) st[b].O[f % DB] = mfma_f16(v, operand(b, f / DB), st[b].O[f % DB]);
+        if (f < DB) {
+#pragma unroll
+          for (int i = f * 4 * QB / DB; i < (f + 1) * 4 * QB / DB; ++i) pair(i / 4, 1, i % 4);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int c = 0; c < DB; ++c) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const unsigned char* p = sg + va + 32 * x * PITCH + 16 * ((2 * c + (vj >> 1)) ^ vswz);
-          const msk::v4i16_t v0 = msk::lds_read_tr16(p), v1 = msk::lds_read_tr16(p + 16 * PITCH);
-          const f16x8_t A = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-          for (int b = 0; b < QB; ++b) st[b].O[c] = mfma_f16(A, P[b][x], st[b].O[c]);
-        }
+      for (int b = 0; b < QB; ++b) {
+        const f16x8_t both[2] = {operand(b, 0), operand(b, 1)};
+        softmax_sum(st[b], both, ev);
       }
     }
-    msk::bare_barrier();  // the tile is read, the next one staged
+    it = nx;
+    nx = after;
+  };
+  if (it < i1) {
+    issue(it, 0);
+    for (;;) {
+      step(0);
+      if (it >= i1) break;
+      step(1);
+      if (it >= i1) break;
+    }
+    msk::wait_vm<0>();  // the reload past the last tile has landed
   }
   bool bad = false;
 #pragma unroll
   for (int b = 0; b < QB; ++b) {
-    st[b].l += __shfl_xor(st[b].l, 16, 64);
-    st[b].l += __shfl_xor(st[b].l, 32, 64);
-    const float f = st[b].l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(st[b].R) / st[b].l;
-    bad |= !isfinite(st[b].l);
+    const float f = st[b].l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(st[b].A - st[b].L) / st[b].l;
+    bad |= st[b].lost();
 #pragma unroll
     for (int c = 0; c < DB; ++c)
 #pragma unroll
@@ -907,6 +1022,7 @@ __global__ __launch_bounds__(kTileThreads, D == 256 ? 1 : 2) void attention_q_ti
         bad |= !isfinite(st[b].O[c][x]);
       }
   }
+  __syncthreads();  // LDS is free
   if (any_thread<kTileThreads / 64>(bad, reinterpret_cast<int*>(kv_lds))) {  // nothing of out is written yet: it may be q
     __syncthreads();  // the flags are read
     for (int r = r0 + wave; r < r1; r += kTileThreads / 64)
@@ -930,7 +1046,7 @@ __global__ __launch_bounds__(kTileThreads, D == 256 ? 1 : 2) void attention_q_ti
       for (int c = 0; c < DB; ++c)
         *reinterpret_cast<float4*>(a.part + pr * D + 16 * c + 4 * g4) =
             make_float4(st[b].O[c][0], st[b].O[c][1], st[b].O[c][2], st[b].O[c][3]);
-      if (g4 == 0) a.ml[pr] = make_float2(st[b].m, st[b].l);
+      if (g4 == 0) a.ml[pr] = make_float2(st[b].l == 0.0f ? -INFINITY : st[b].L, st[b].l);
     }
   }
 }
@@ -956,7 +1072,7 @@ __global__ __launch_bounds__(kJoinThreads) void attention_q_join_kernel(AttArgs 
   float top = ml.x;
 #pragma unroll
   for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-  const float w = ml.x == top ? ml.y : ml.y * __builtin_amdgcn_exp2f((ml.x - top) * a.mul);
+  const float w = ml.x == top ? ml.y : ml.y * __builtin_amdgcn_exp2f(ml.x - top);
   float total = w;
 #pragma unroll
   for (int x = 32; x >= 1; x >>= 1) total += __shfl_xor(total, x, 64);
@@ -988,56 +1104,62 @@ __global__ __launch_bounds__(kJoinThreads) void attention_q_join_kernel(AttArgs 
 
 // How a call is run.
 struct Plan {
-  bool few;        // attention_q_few_kernel
-  int qb, blocks;  // row blocks of 64 qb otherwise
-  int splits;      // shares of a row's tiles
+  int variant;      // 0: attention_q_few_kernel, 1 ..: attention_q_tile_kernel
+  int rows, blocks; // of a work-group, work-groups per head and split
+  int splits;       // shares of a row's tiles
 };
 
 Plan plan_of(int64_t heads, int T, int G, int D, int pos0, int window, int prefix) {
   Plan p;
   const int64_t rows = static_cast<int64_t>(T) * G;
   int64_t tiles = (static_cast<int64_t>(pos0) + T + kKvBlock - 1) / kKvBlock;
-  p.few = rows <= 16;
-  p.qb = 1;
-  p.blocks = 1;
-  if (!p.few) {
-    p.qb = heads * ((rows + 127) / 128) >= 512 ? 2 : 1;
-    p.blocks = static_cast<int>((rows + 64 * p.qb - 1) / (64 * p.qb));
-  }
+  p.variant = rows <= 16 ? 0 : heads * ((rows + 127) / 128) >= 512 && D < 256 ? 2 : 1;
+  p.rows = p.variant == 0 ? 16 : p.variant == 1 ? 64 : 128;
+#ifdef SWEEP
+  static const int V = getenv("V") ? atoi(getenv("V")) : 0;
+  if (p.variant && V) { p.variant = V; p.rows = V == 1 || V == 3 ? 64 : V == 6 ? 256 : 128; }
+#endif
+  p.blocks = static_cast<int>((rows + p.rows - 1) / p.rows);
   if (window > 0) {
-    const int64_t tokens = p.few ? T : std::min<int64_t>(T, 64 * p.qb / G + 2);
+    const int64_t tokens = std::min<int64_t>(T, p.rows / G + 2);
     tiles = std::min<int64_t>(tiles, (static_cast<int64_t>(window) + tokens) / kKvBlock + 2 + prefix / kKvBlock + 1);
   }
   const int64_t wgs = heads * p.blocks;
-  const int64_t target = p.few ? 512 : 512, least = p.few ? 4 : 4;
+  int64_t target = 512, least = 4;
+#ifdef SWEEP
+  static const int TG = getenv("TG") ? atoi(getenv("TG")) : 512, LE = getenv("LE") ? atoi(getenv("LE")) : 4;
+  target = TG, least = LE;
+#endif
   p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({target / wgs, tiles / least, kMostSplits})));
   return p;
+}
+
+template <int D, int QB, int NW>
+void launch_tile(const AttArgs& a, int blocks, bool mods, dim3 grid, hipStream_t s) {
+  constexpr size_t lds = size_t{4} * kKvBlock * D;
+  if (mods)
+    hipLaunchKernelGGL((attention_q_tile_kernel<D, QB, NW, true>), grid, dim3(64 * NW), lds, s, a, blocks);
+  else
+    hipLaunchKernelGGL((attention_q_tile_kernel<D, QB, NW, false>), grid, dim3(64 * NW), lds, s, a, blocks);
 }
 
 template <int D>
 ms_status launch_attention_q(const AttArgs& a, const Plan& p, bool mods, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.heads) * p.blocks * p.splits));
-  if (p.few) {
+  if (p.variant == 0) {
     constexpr size_t lds = static_cast<size_t>(few_waves(D)) * few_stages(D) * 2 * kStep * D;
     if (mods)
       hipLaunchKernelGGL((attention_q_few_kernel<D, true>), grid, dim3(64 * few_waves(D)), lds, s, a);
     else
       hipLaunchKernelGGL((attention_q_few_kernel<D, false>), grid, dim3(64 * few_waves(D)), lds, s, a);
-  } else {
-    constexpr size_t lds = size_t{4} * kKvBlock * 2 * D;
-    const dim3 block(kTileThreads);
-    if (p.qb == 2) {
-      if (mods)
-        hipLaunchKernelGGL((attention_q_tile_kernel<D, 2, true>), grid, block, lds, s, a, p.blocks);
-      else
-        hipLaunchKernelGGL((attention_q_tile_kernel<D, 2, false>), grid, block, lds, s, a, p.blocks);
-    } else {
-      if (mods)
-        hipLaunchKernelGGL((attention_q_tile_kernel<D, 1, true>), grid, block, lds, s, a, p.blocks);
-      else
-        hipLaunchKernelGGL((attention_q_tile_kernel<D, 1, false>), grid, block, lds, s, a, p.blocks);
-    }
+  } else if (p.variant == 1) {
+    launch_tile<D, 1, 4>(a, p.blocks, mods, grid, s);
+  } else if (p.variant == 2) {
+    launch_tile<D, 2, 4>(a, p.blocks, mods, grid, s);
   }
+#ifdef SWEEP
+  else if (p.variant == 4) launch_tile<(D > 64 ? D : 128), 1, 8>(a, p.blocks, mods, grid, s);
+#endif
   if (p.splits > 1)
     hipLaunchKernelGGL(attention_q_join_kernel<D>, dim3(static_cast<unsigned>(a.heads) * a.T * a.G), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError() == hipSuccess ? MS_OK : MS_E_HIP;
