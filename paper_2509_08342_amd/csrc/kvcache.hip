@@ -247,8 +247,10 @@ struct AttArgs {
   uint16_t* out;
   float* part;  // splits > 1: [rows][splits][D] results of a share of the keys
   float2* ml;   // [rows][splits] the exponent that their sums are relative to (-inf: no key), and the sums
-  int T, Hq, Hkv, G, max_ctx, pos0, heads, splits;  // heads: key/value heads of all sequences
+  int T, Hq, Hkv, G, max_ctx, pos0;
+  int heads, splits, share;  // key/value heads of all sequences, shares of a row's tiles, and tiles of a share (few rows)
   int window, prefix;
+  int scores;           // whether scores are capped or biased
   float pre, cap, mul;  // score = pre q.k, capped and biased; weight = 2^(mul (score - maximum))
 };
 
@@ -397,30 +399,36 @@ __device__ __forceinline__ void attend_row(const AttArgs& a, int head, const Spa
   if (a.splits > 1 && lane == 0) a.ml[pr] = make_float2(m * a.mul, l);
 }
 
-// ---- one step of the softmax, shared by the two matrix-core kernels
+// ---- scores and softmax, shared by the two matrix-core kernels
 //
 // S^T = K Q^T on the matrix cores: A = 16 keys, B = 16 rows, so that lane (n =
-// lane % 16, g = lane / 16) ends with row n's scores of keys 16 b + 4 g + r of
-// key block b; O^T += V^T P^T takes the probabilities where they are, as fp16
-// pairs, contraction slot 4 h + r of lane group g being key 16 h + 4 g + r of 32.
+// lane % 16, g = lane / 16) ends with row n's scores of keys 16 b + 4 g + r of key
+// block b.  Codes are converted to bf16 (exact); the keys' scale 2^ek multiplies the
+// sums.  (The 8-bit matrix instructions would take the codes as they are, but align
+// the products of a sum to 2^-14 or so of the largest.)
+//   O^T += V^T P^T takes the probabilities where they are, as fp16 pairs,
+// contraction slot 4 h + r of lane group g being key 16 h + 4 g + r of 32, and codes
+// converted to fp16 (exact).  A value block's 2^ev goes into the probability's
+// exponent.
 //
-// A score's exponent is y = c S, c = mul times the key block's scale.  A row keeps
-// its sum l = sum 2^(y - L) and O = sum 2^(y + ev - A) code, ev the value block's
-// exponent; L and A are whole numbers, so that c S - A is one fma that rounds once
-// whatever their size, and rescaling by their changes is exact.  A keeps the fp16
-// probabilities below 2^15 with the largest at 2^6 to 2^7 when it is set: half a
-// step is 2^-11 of a probability and the smallest step 2^-30 of the largest
-// weight or less.  One fp16 part is enough here: the 3-bit mantissa of the codes
-// that it meets is 2^-4 off already.  The sum is taken of the same fp16
-// probabilities by the matrix cores (a column of ones), in 32 bits.  L and A move
-// only when they have to, so most tiles rescale nothing.  Exponents past 2^24
-// (kHuge), where whole numbers are no longer exact, leave the row to attend_row.
-constexpr float kAim = 7.0f, kMost = 15.0f, kGrow = 40.0f;
-constexpr float kNone = -1073741824.0f;  // L and A of a row without keys
+// A score's exponent is y = c S, c = mul 2^ek.  A row keeps its sum l = sum 2^(y - L) and O = sum
+// 2^(y + ev - A) code; L and A are whole numbers, so that c S + ev - A is one fma
+// that rounds once whatever their size, and rescaling by their changes is exact.  A
+// makes the largest probability 2^6 to 2^7 when it is set: half an fp16 step is 2^-11
+// of a probability, and the smallest step 2^-30 of the largest weight or less.  One
+// fp16 part is enough here: the 3-bit mantissa of the codes that it meets is 2^-4
+// off already.  The sum is taken of the same fp16 probabilities by the matrix cores
+// (a row of ones), in 32 bits.  Only if it overflows (a probability past fp16: 2^9
+// above the last maximum; the first keys of a row) is the maximum looked for, and L
+// and A moved.  Exponents past 2^24 (kHuge), where whole numbers are no longer exact,
+// leave the row to attend_row.
+constexpr float kAim = 7.0f;
+constexpr float kNone = -3e38f;  // L and A of a row without keys
 constexpr float kHuge = 16777216.0f;
 
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ msk::f32x4_t mfma_f16(f16x8_t a, f16x8_t b, msk::f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -437,39 +445,38 @@ __device__ __forceinline__ float group_max(float v) {
   return max_of(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// The 16-byte pieces of a key row that a lane of group g holds, two contraction
+// steps each.
+constexpr int key_pieces(int D) { return D / 64; }
+__device__ __forceinline__ int key_piece(int x, int g) { return 4 * x + g; }
+
+__device__ __forceinline__ msk::bf16x8_t codes_bf16(uint32_t lo, uint32_t hi) {
+  const uint2 a = codes_to_bf16(lo, 1.0f), b = codes_to_bf16(hi, 1.0f);
+  return msk::as_bf16x8(make_uint4(a.x, a.y, b.x, b.y));
+}
+
+// A row of q as matrix operands, in the order of the pieces.
+template <int D>
+struct Query {
+  msk::bf16x8_t part[2 * key_pieces(D)];
+  __device__ __forceinline__ void load(const uint16_t* q, int g) {
+#pragma unroll
+    for (int x = 0; x < 2 * key_pieces(D); ++x)
+      part[x] = msk::as_bf16x8(*reinterpret_cast<const uint4*>(q + 16 * key_piece(x / 2, g) + 8 * (x % 2)));
+  }
+};
+
 template <int DB>
 struct RowState {
-  float l = 0.0f, L = kNone, A = kNone, best = -INFINITY;  // best: the largest exponent
+  float l = 0.0f, L = kNone, A = kNone;
   msk::f32x4_t O[DB];
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int c = 0; c < DB; ++c) O[c] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
   // whether the row has to be left to attend_row
-  __device__ __forceinline__ bool lost() const { return !isfinite(l) || (fabsf(best) > kHuge && best != -INFINITY); }
+  __device__ __forceinline__ bool lost() const { return !isfinite(l) || (A != kNone && fabsf(A) > kHuge); }
 };
-
-// The largest of a row's scores of NB key blocks, and what it moves.
-template <int NB, int DB>
-__device__ __forceinline__ void softmax_max(RowState<DB>& st, const msk::f32x4_t (&S)[NB], float c, float ev) {
-  float top = S[0][0];
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) top = max_of(top, S[b][r]);
-  const float y = group_max(top) * c;
-  st.best = fmaxf(st.best, y);
-  if (__any(y - st.L > kGrow || y + ev - st.A > kMost)) {
-    const float up = ceilf(y);  // -inf where the row sees nothing
-    const float L = fmaxf(st.L, up), A = fmaxf(st.A, up + ev - kAim);
-    st.l *= __builtin_amdgcn_exp2f(st.L - L);
-    const float f = __builtin_amdgcn_exp2f(st.A - A);
-#pragma unroll
-    for (int x = 0; x < DB; ++x) st.O[x] *= f;
-    st.L = L;
-    st.A = A;
-  }
-}
 
 // Two probabilities: those of the scores s0 and s1.
 __device__ __forceinline__ uint32_t softmax_pair(float s0, float s1, float c, float off) {
@@ -477,14 +484,49 @@ __device__ __forceinline__ uint32_t softmax_pair(float s0, float s1, float c, fl
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(p, f16x2_t));
 }
 
-// Adds the probabilities' sum.
-template <int NP, int DB>
-__device__ __forceinline__ void softmax_sum(RowState<DB>& st, const f16x8_t (&P)[NP], float ev) {
+// The probabilities of 2 H key blocks, H operands, and their sum for every row
+// (all four values alike).
+template <int H>
+__device__ __forceinline__ msk::f32x4_t probabilities(const msk::f32x4_t (&S)[2 * H], float c, float off, f16x8_t (&P)[H]) {
   const f16x8_t ones = {1, 1, 1, 1, 1, 1, 1, 1};
   msk::f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int x = 0; x < NP; ++x) sum = mfma_f16(ones, P[x], sum);
-  st.l = fmaf(sum[0], __builtin_amdgcn_exp2f(st.A - ev - st.L), st.l);
+  for (int h = 0; h < H; ++h) {
+    P[h] = __builtin_bit_cast(
+        f16x8_t, make_uint4(softmax_pair(S[2 * h][0], S[2 * h][1], c, off), softmax_pair(S[2 * h][2], S[2 * h][3], c, off),
+                            softmax_pair(S[2 * h + 1][0], S[2 * h + 1][1], c, off),
+                            softmax_pair(S[2 * h + 1][2], S[2 * h + 1][3], c, off)));
+    sum = mfma_f16(ones, P[h], sum);
+  }
+  return sum;
+}
+
+// Softmax of QB rows' scores S of 2 H key blocks: their operands P, and what l, L, A
+// and O become.
+template <int QB, int DB, int H>
+__device__ __forceinline__ void softmax_step(RowState<DB> (&st)[QB], const msk::f32x4_t (&S)[QB][2 * H], float c, float ev,
+                                             f16x8_t (&P)[QB][H]) {
+#pragma unroll
+  for (int b = 0; b < QB; ++b) {
+    msk::f32x4_t sum = probabilities<H>(S[b], c, ev - st[b].A, P[b]);
+    if (__any(!(sum[0] < INFINITY))) {
+      float top = S[b][0][0];
+#pragma unroll
+      for (int k = 0; k < 2 * H; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = max_of(top, S[b][k][r]);
+      const float up = ceilf(group_max(top) * c);  // -inf where the row sees nothing
+      const float L = fmaxf(st[b].L, up), A = fmaxf(st[b].A, up + ev - kAim);
+      st[b].l *= __builtin_amdgcn_exp2f(st[b].L - L);
+      const float f = __builtin_amdgcn_exp2f(st[b].A - A);
+#pragma unroll
+      for (int x = 0; x < DB; ++x) st[b].O[x] *= f;
+      st[b].L = L;
+      st[b].A = A;
+      sum = probabilities<H>(S[b], c, ev - A, P[b]);
+    }
+    st[b].l = fmaf(sum[0], __builtin_amdgcn_exp2f(st[b].A - ev - st[b].L), st[b].l);
+  }
 }
 
 // A lane's row: what its scores and masks depend on.
@@ -500,7 +542,7 @@ __device__ __forceinline__ Row row_of(const AttArgs& a, int head, const Span& sp
   return w;
 }
 
-// Raw scores of NB key blocks from key k0 on to scores: scaled, capped, biased
+// Raw scores of NB key blocks from key k0 on: scaled, capped and biased (a.scores)
 // and masked (`masked`: some row of the wave may not see some of the keys).
 template <int NB>
 __device__ __forceinline__ void modify(const AttArgs& a, const Row& w, const int32_t* docs, int k0, int n, float ks, bool masked,
@@ -510,14 +552,16 @@ __device__ __forceinline__ void modify(const AttArgs& a, const Row& w, const int
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     const int j0 = k0 + 16 * b + 4 * g4;
-    S[b] *= f;
-    if (a.cap > 0.0f) {
+    if (a.scores) {
+      S[b] *= f;
+      if (a.cap > 0.0f) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) S[b][r] = a.cap * tanh_of(S[b][r] * inv_cap);
-    }
-    if (a.slopes) {
+        for (int r = 0; r < 4; ++r) S[b][r] = a.cap * tanh_of(S[b][r] * inv_cap);
+      }
+      if (a.slopes) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) S[b][r] -= w.slope * fabsf(static_cast<float>(w.pos - j0 - r));
+        for (int r = 0; r < 4; ++r) S[b][r] -= w.slope * fabsf(static_cast<float>(w.pos - j0 - r));
+      }
     }
     if (masked) {
       int4 dj = make_int4(0, 0, 0, 0);
@@ -530,10 +574,6 @@ __device__ __forceinline__ void modify(const AttArgs& a, const Row& w, const int
   }
 }
 
-__device__ __forceinline__ msk::bf16x8_t codes_bf16(uint32_t lo, uint32_t hi) {
-  const uint2 a = codes_to_bf16(lo, 1.0f), b = codes_to_bf16(hi, 1.0f);
-  return msk::as_bf16x8(make_uint4(a.x, a.y, b.x, b.y));
-}
 __device__ __forceinline__ uint2 codes_to_f16(uint32_t c) {
   return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(c), 1.0f, false)),
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(c), 1.0f, true)));
@@ -575,11 +615,14 @@ template <int D>
 __device__ __forceinline__ int value_slot(int u) { return (((u & 7) | ((u >> 1) & 8)) / (256 / D)) & (D / 16 - 1); }
 
 constexpr int few_waves(int D) { return D == 256 ? 4 : 8; }
-constexpr int few_stages(int D) { return D == 64 ? 4 : 2; }
+#ifndef FS
+#define FS 2
+#endif
+constexpr int few_stages(int D) { return D == 64 ? FS : 2; }
 
 template <int D, bool MODS>
 __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttArgs a) {
-  constexpr int NW = few_waves(D), NST = few_stages(D), KS = D / 32, DB = D / 16;
+  constexpr int NW = few_waves(D), NST = few_stages(D), DB = D / 16;
   constexpr int PIECES = D / 16, RPL = 64 / PIECES;  // 16-byte pieces of a row, rows per load
   constexpr int KB = kStep * D, SB = 2 * KB, NK = KB / 1024, NL = 2 * NK;
   constexpr int PP = D + 4;                          // floats of a merged row
@@ -593,8 +636,8 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
   if (sp.count == 0) return;
   const int rows = sp.count * a.G, n = sp.start + sp.count;
   const Tiles tl = tiles_of(a, sp.start, n - 1, n);
-  const int total = tl.count(), share = (total + a.splits - 1) / a.splits;
-  const int i0 = min(z * share, total), i1 = min(i0 + share, total);
+  const int total = tl.count();
+  const int i0 = min(z * a.share, total), i1 = min(i0 + a.share, total);
   if (i0 == i1) {
     if (static_cast<int>(threadIdx.x) < rows) a.ml[part_row(a, head, threadIdx.x, z)] = make_float2(-INFINITY, 0.0f);
     return;
@@ -620,12 +663,8 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
   };
   const int r = min(n16, rows - 1);
   const Row w = row_of(a, head, sp, r);
-  msk::bf16x8_t Q[KS];
-  {
-    const uint16_t* qr = a.q + q_row(a, head, r) * D + 16 * g4;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) Q[s] = msk::as_bf16x8(*reinterpret_cast<const uint4*>(qr + 64 * (s >> 1) + 8 * (s & 1)));
-  }
+  Query<D> q[1];
+  q[0].load(a.q + q_row(a, head, r) * D, g4);
 #pragma unroll
   for (int p = 0; p < NST - 1; ++p) issue(wave + NW * p, p);
   Exps exps;
@@ -635,8 +674,8 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
     va = KB + u * D + 8 * (lane & 1);
   }
   const int vswz = value_slot<D>(((lane >> 1) & 7) < 4 ? 4 * g4 + ((lane >> 1) & 7) : 12 + 4 * g4 + ((lane >> 1) & 7));
-  RowState<DB> st;
-  st.clear();
+  RowState<DB> st[1];
+  st[0].clear();
   int cur = 0, nxt = NST - 1;
   for (int s = wave; s < steps; s += NW) {
     int ek, ve_s;
@@ -648,36 +687,34 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
     cur = cur + 1 == NST ? 0 : cur + 1;
     nxt = nxt + 1 == NST ? 0 : nxt + 1;
     const int k0 = key0(s);
-    msk::f32x4_t S[2];
+    msk::f32x4_t S[1][2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      S[b] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
+      S[0][b] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
       const int u = 16 * b + n16;
+      uint4 K[key_pieces(D)];
 #pragma unroll
-      for (int x = 0; x < KS / 2; ++x) {
-        const uint4 c = *reinterpret_cast<const uint4*>(sg + u * D + 16 * ((4 * x + g4) ^ key_slot<D>(u)));
-        S[b] = msk::mfma16(codes_bf16(c.x, c.y), Q[2 * x], S[b]);
-        S[b] = msk::mfma16(codes_bf16(c.z, c.w), Q[2 * x + 1], S[b]);
+      for (int x = 0; x < key_pieces(D); ++x)
+        K[x] = *reinterpret_cast<const uint4*>(sg + u * D + 16 * (key_piece(x, g4) ^ key_slot<D>(u)));
+#pragma unroll
+      for (int x = 0; x < key_pieces(D); ++x) {
+        S[0][b] = msk::mfma16(codes_bf16(K[x].x, K[x].y), q[0].part[2 * x], S[0][b]);
+        S[0][b] = msk::mfma16(codes_bf16(K[x].z, K[x].w), q[0].part[2 * x + 1], S[0][b]);
       }
     }
     const bool last = k0 + kStep > n;
     const float ks = pow2(ek), ev = static_cast<float>(ve_s);
-    f16x8_t P[1];
-    const float c = MODS ? a.mul : a.mul * ks;
     if constexpr (MODS) {
-      modify(a, w, docs, k0, n, ks, true, S);
+      modify(a, w, docs, k0, n, ks, true, S[0]);
     } else if (k0 + kStep > sp.start + 1) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-          if (k0 + 16 * b + 4 * g4 + x > w.pos) S[b][x] = -INFINITY;
+          if (k0 + 16 * b + 4 * g4 + x > w.pos) S[0][b][x] = -INFINITY;
     }
-    softmax_max(st, S, c, ev);
-    const float off = ev - st.A;
-    P[0] = __builtin_bit_cast(f16x8_t, make_uint4(softmax_pair(S[0][0], S[0][1], c, off), softmax_pair(S[0][2], S[0][3], c, off),
-                                                  softmax_pair(S[1][0], S[1][1], c, off), softmax_pair(S[1][2], S[1][3], c, off)));
-    softmax_sum(st, P, ev);
+    f16x8_t P[1][1];
+    softmax_step<1, DB, 1>(st, S, MODS && a.scores ? a.mul : a.mul * ks, ev, P);
 #pragma unroll
     for (int c = 0; c < DB; ++c) {
       uint2 t = msk::lds_read_tr8(sg + va + 16 * (c ^ vswz));
@@ -690,7 +727,7 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
         t.y = keep(t.y, k0 + 16 + 4 * g4);
       }
       const uint2 lo = codes_to_f16(t.x), hi = codes_to_f16(t.y);
-      st.O[c] = mfma_f16(__builtin_bit_cast(f16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y)), P[0], st.O[c]);
+      st[0].O[c] = mfma_f16(__builtin_bit_cast(f16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y)), P[0][0], st[0].O[c]);
     }
   }
   msk::wait_vm<0>();  // the reloads past the last step have landed
@@ -699,17 +736,17 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
   float* mx = part + NW * 16 * PP;                 // [NW][16] L, then l and A
   float *sm = mx + NW * 16, *rx = sm + NW * 16;
   int* flags = reinterpret_cast<int*>(rx + NW * 16);
-  bool bad = n16 < rows && st.lost();
+  bool bad = n16 < rows && st[0].lost();
   if (n16 < rows) {
     if (g4 == 0) {
-      mx[wave * 16 + n16] = st.L;
-      sm[wave * 16 + n16] = st.l;
-      rx[wave * 16 + n16] = st.A;
+      mx[wave * 16 + n16] = st[0].L;
+      sm[wave * 16 + n16] = st[0].l;
+      rx[wave * 16 + n16] = st[0].A;
     }
 #pragma unroll
     for (int c = 0; c < DB; ++c)
       *reinterpret_cast<float4*>(part + (wave * 16 + n16) * PP + 16 * c + 4 * g4) =
-          make_float4(st.O[c][0], st.O[c][1], st.O[c][2], st.O[c][3]);
+          make_float4(st[0].O[c][0], st[0].O[c][1], st[0].O[c][2], st[0].O[c][3]);
   }
   __syncthreads();
   const int used = min(NW, steps);  // waves with a step
@@ -752,24 +789,24 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
 // its share of the tiles of 64 keys.  Codes come to LDS by direct loads, a tile
 // ahead, and become operands when a wave reads them, as above: the conversions
 // run beside the matrix instructions, and LDS holds and moves a byte per value.
-template <int D, int QB, int NW, bool MODS>
-__global__ __launch_bounds__(64 * NW, NW / 2) void attention_q_tile_kernel(AttArgs a, int blocks) {
-  constexpr int kTileThreads = 64 * NW;
-  constexpr int ROWS = 16 * NW * QB, KS = D / 32, DB = D / 16;
+constexpr int kTileWaves = 4;
+constexpr size_t tile_lds(int D) { return size_t{4} * kKvBlock * D; }  // two stages of keys and values
+
+template <int D, int QB, bool MODS>
+__global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void attention_q_tile_kernel(AttArgs a, int blocks) {
+  constexpr int NW = kTileWaves, ROWS = 16 * NW * QB, DB = D / 16;
   constexpr int PIECES = D / 16, RPL = 64 / PIECES;  // 16-byte pieces of a row, rows per load
   constexpr int TILE = kKvBlock * D, NL = TILE / 1024 / NW;  // bytes of a tile's keys (or values), their loads per wave
   static_assert(NL >= 1 && NL * NW * 1024 == TILE, "loads");
-  extern __shared__ __align__(16) unsigned char kv_lds[];  // two stages of a tile's keys and values
-  __shared__ int doc_s[2 * kTileThreads / 64];
-  __shared__ uint32_t near_s[4];
+  extern __shared__ __align__(16) unsigned char kv_lds[];
+  __shared__ int doc_s[2 * NW];
+  __shared__ uint32_t near_s[NW];
   const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = blockIdx.x % a.heads, zj = blockIdx.x / a.heads, j = zj % blocks, z = zj / blocks, seq = head / a.Hkv;
   const Span sp = span_of(a.span, seq, a.pos0, a.T);
   const int rows = sp.count * a.G, n = sp.start + sp.count;
-  // the longest row blocks first, the second half shortest first: two work-groups
-  // that share a CU add up to about the same work
-  const int first = (blocks + 1) / 2, r0 = (j < first ? blocks - 1 - j : j - first) * ROWS;
+  const int r0 = (blocks - 1 - j) * ROWS;  // the longest row blocks first
   if (r0 >= rows) return;
   const int r1 = min(r0 + ROWS, rows);  // the work-group's rows
   const Tiles tl = tiles_of(a, sp.start + r0 / a.G, sp.start + (r1 - 1) / a.G, n);
@@ -784,14 +821,12 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void attention_q_tile_kernel(AttAr
   const int32_t* docs = MODS && a.docs ? a.docs + static_cast<size_t>(seq) * a.max_ctx : nullptr;
 
   Row w[QB];
-  msk::bf16x8_t Q[QB][KS];
+  Query<D> q[QB];
 #pragma unroll
   for (int b = 0; b < QB; ++b) {
     const int r = min(r0 + (wave * QB + b) * 16 + n16, r1 - 1);  // rows past the last repeat it (never stored)
     w[b] = row_of(a, head, sp, r);
-    const uint16_t* qr = a.q + q_row(a, head, r) * D + 16 * g4;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) Q[b][s] = msk::as_bf16x8(*reinterpret_cast<const uint4*>(qr + 64 * (s >> 1) + 8 * (s & 1)));
+    q[b].load(a.q + q_row(a, head, r) * D, g4);
   }
 
   // documents: only tiles with a key of a document between the rows' least and
@@ -813,13 +848,13 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void attention_q_tile_kernel(AttAr
       }
       if (lane == 0) {
         doc_s[wave] = d_min;
-        doc_s[kTileThreads / 64 + wave] = d_max;
+        doc_s[NW + wave] = d_max;
       }
       __syncthreads();
 #pragma unroll
-      for (int x = 0; x < kTileThreads / 64; ++x) {
+      for (int x = 0; x < NW; ++x) {
         d_min = min(d_min, doc_s[x]);
-        d_max = max(d_max, doc_s[kTileThreads / 64 + x]);
+        d_max = max(d_max, doc_s[NW + x]);
       }
     }
   }
@@ -832,7 +867,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void attention_q_tile_kernel(AttAr
             chunk = (i - i0) / 64;
             const int t = i0 + 64 * chunk + 16 * wave + (lane >> 2);
             bool hit = false;
-            if (wave < 4 && t < i1) {
+            if (t < i1) {
               const int4* d = reinterpret_cast<const int4*>(docs + tl.at(t) * kKvBlock + 16 * (lane & 3));
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
@@ -848,11 +883,11 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void attention_q_tile_kernel(AttAr
 #pragma unroll
             for (int x = 0; x < 16; ++x) bits |= static_cast<uint32_t>((h >> (4 * x)) & 1) << x;
             __syncthreads();  // the chunk before is read
-            if (lane == 0 && wave < 4) near_s[wave] = bits;
+            if (lane == 0) near_s[wave] = bits;
             __syncthreads();
             near = 0;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) near |= static_cast<uint64_t>(near_s[x]) << (16 * x);
+            for (int x = 0; x < NW; ++x) near |= static_cast<uint64_t>(near_s[x]) << (16 * x);
           }
           const uint64_t rest = near >> ((i - i0) & 63);
           if (rest) return i + static_cast<int>(__builtin_ctzll(rest));
@@ -884,9 +919,10 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void attention_q_tile_kernel(AttAr
   // positions of the wave's first and last rows
   const int p_min = sp.start + min(r0 + wave * QB * 16, r1 - 1) / a.G;
   const int p_max = sp.start + min(r0 + (wave + 1) * QB * 16 - 1, r1 - 1) / a.G;
-  const unsigned char* ka[KS / 2];  // this lane's 16 bytes of keys 0 .. 15
+  constexpr int KP = key_pieces(D);
+  const unsigned char* ka[KP];  // this lane's pieces of keys 0 .. 15
 #pragma unroll
-  for (int x = 0; x < KS / 2; ++x) ka[x] = kv_lds + n16 * D + 16 * ((4 * x + g4) ^ key_slot<D>(n16));
+  for (int x = 0; x < KP; ++x) ka[x] = kv_lds + n16 * D + 16 * (key_piece(x, g4) ^ key_slot<D>(n16));
   const int vx = (lane >> 1) & 7, vrow = (vx < 4 ? 0 : 12) + 4 * g4 + vx;  // vx >= 4: key 16 + 4 g + vx - 4
   const unsigned char* const va = kv_lds + TILE + vrow * D + 8 * (lane & 1);
   const int vswz = value_slot<D>(vrow);
@@ -896,15 +932,11 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void attention_q_tile_kernel(AttAr
 
   int it = advance(i0), nx = advance(it + 1);  // this tile and the next
   Exps exps;
-  // A tile in pieces whose order is kept (sched_barrier), so that matrix
-  // instructions run beside vector work: conversions, and the second half's
-  // exponentials beside the first half's values.  Codes are read three pieces ahead.
   auto step = [&](int p) {
     const int k0 = tl.at(it) * kKvBlock;
     int ek, ve_it;
     exps.at(tl, i0, i1, it, ke, ve, ek, ve_it);
     const float ks = pow2(ek), ev = static_cast<float>(ve_it);
-    const float c = MODS ? a.mul : a.mul * ks;
     bool skip, masked;  // whether no row of the wave sees the tile, and whether some do not see all of it
     if constexpr (MODS) {
       skip = !((k0 <= p_max && (a.window <= 0 || k0 + kKvBlock - 1 > p_min - a.window)) || k0 < a.prefix);
@@ -919,81 +951,59 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void attention_q_tile_kernel(AttAr
     msk::bare_barrier();  // the tile is staged, the other stage is read
     issue(nx, p ^ 1);
     if (n - k0 < kKvBlock) {  // values past the end may be anything: code 0
-      for (int x = (n - k0) * D + 16 * threadIdx.x; x < TILE; x += 16 * kTileThreads)
+      for (int x = (n - k0) * D + 16 * threadIdx.x; x < TILE; x += 16 * 64 * NW)
         *reinterpret_cast<uint4*>(kv_lds + p * 2 * TILE + TILE + x) = make_uint4(0, 0, 0, 0);
       msk::bare_barrier();
     }
     if (!skip) {
       msk::f32x4_t S[QB][4];
-      {
-        uint4 A[3];
-        auto key = [&](int f) { return *reinterpret_cast<const uint4*>(ka[f / 4] + p * 2 * TILE + f % 4 * 16 * D); };
+      uint4 K4[4];
+      auto key = [&](int f) { return *reinterpret_cast<const uint4*>(ka[f % KP] + p * 2 * TILE + f / KP * 16 * D); };
 #pragma unroll
-        for (int f = 0; f < 2; ++f) A[f] = key(f);
+      for (int f = 0; f < 4; ++f) K4[f] = key(f);
 #pragma unroll
-        for (int f = 0; f < 2 * KS; ++f) {
-          if (f + 2 < 2 * KS) A[(f + 2) % 3] = key(f + 2);
-          const uint4 c = A[f % 3];
-          const msk::bf16x8_t lo = codes_bf16(c.x, c.y), hi = codes_bf16(c.z, c.w);
+      for (int f = 0; f < 4 * KP; ++f) {
+        const uint4 k = K4[f % 4];
+        const msk::bf16x8_t lo = codes_bf16(k.x, k.y), hi = codes_bf16(k.z, k.w);
+        if (f + 4 < 4 * KP) K4[f % 4] = key(f + 4);
 #pragma unroll
-          for (int b = 0; b < QB; ++b)
-            S[b][f % 4] = msk::mfma16(lo, Q[b][f / 4 * 2], f < 4 ? msk::f32x4_t{0.f, 0.f, 0.f, 0.f} : S[b][f % 4]);
+        for (int b = 0; b < QB; ++b)
+          S[b][f / KP] = msk::mfma16(lo, q[b].part[f % KP * 2], f % KP == 0 ? msk::f32x4_t{0.f, 0.f, 0.f, 0.f} : S[b][f / KP]);
 #pragma unroll
-          for (int b = 0; b < QB; ++b) S[b][f % 4] = msk::mfma16(hi, Q[b][f / 4 * 2 + 1], S[b][f % 4]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        for (int b = 0; b < QB; ++b) S[b][f / KP] = msk::mfma16(hi, q[b].part[f % KP * 2 + 1], S[b][f / KP]);
+        __builtin_amdgcn_sched_barrier(0);  // no more operands at a time
       }
+      auto value = [&](int f) {  // 16 columns of 32 keys
+        return msk::lds_read_tr8(va + p * 2 * TILE + 32 * (f / DB) * D + 16 * ((f % DB) ^ vswz));
+      };
+      if constexpr (MODS) {
+        if (masked || a.scores) {
 #pragma unroll
-      for (int b = 0; b < QB; ++b) {
-        if constexpr (MODS) {
-          modify(a, w[b], docs, k0, n, ks, masked, S[b]);
-        } else if (masked) {
+          for (int b = 0; b < QB; ++b) modify(a, w[b], docs, k0, n, ks, masked, S[b]);
+        }
+      } else if (masked) {
+#pragma unroll
+        for (int b = 0; b < QB; ++b)
 #pragma unroll
           for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
             for (int x = 0; x < 4; ++x)
               if (k0 + 16 * kb + 4 * g4 + x > w[b].pos) S[b][kb][x] = -INFINITY;
-        }
-        softmax_max(st[b], S[b], c, ev);
       }
-      uint32_t P[QB][2][4];
-      float off[QB];
+      f16x8_t P[QB][2];
+      softmax_step<QB, DB, 2>(st, S, MODS && a.scores ? a.mul : a.mul * ks, ev, P);
+      uint2 V[4];
 #pragma unroll
-      for (int b = 0; b < QB; ++b) off[b] = ev - st[b].A;
-      auto pair = [&](int b, int h, int i) {
-        const msk::f32x4_t& v = S[b][2 * h + i / 2];
-        P[b][h][i] = softmax_pair(v[2 * (i % 2)], v[2 * (i % 2) + 1], c, off[b]);
-      };
-      auto operand = [&](int b, int h) {
-        return __builtin_bit_cast(f16x8_t, make_uint4(P[b][h][0], P[b][h][1], P[b][h][2], P[b][h][3]));
-      };
-      auto value = [&](int f) {  // 16 columns of 32 keys
-        return msk::lds_read_tr8(va + p * 2 * TILE + 32 * (f / DB) * D + 16 * ((f % DB) ^ vswz));
-      };
-      uint2 A[4];
-#pragma unroll
-      for (int f = 0; f < 3; ++f) A[f] = value(f);
-#pragma unroll
-      for (int b = 0; b < QB; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) pair(b, 0, i);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int f = 0; f < 4; ++f) V[f] = value(f);
+      uint4 v = codes_f16(V[0].x, V[0].y);
 #pragma unroll
       for (int f = 0; f < 2 * DB; ++f) {
-        if (f + 3 < 2 * DB) A[(f + 3) % 4] = value(f + 3);
-        const f16x8_t v = __builtin_bit_cast(f16x8_t, codes_f16(A[f % 4].x, A[f % 4].y));
+        if (f + 4 < 2 * DB) V[f % 4] = value(f + 4);
+        const uint2 next = V[(f + 1) % 4];
 #pragma unroll
-        for (int b = 0; b < QB; ++b) st[b].O[f % DB] = mfma_f16(v, operand(b, f / DB), st[b].O[f % DB]);
-        if (f < DB) {
-#pragma unroll
-          for (int i = f * 4 * QB / DB; i < (f + 1) * 4 * QB / DB; ++i) pair(i / 4, 1, i % 4);
-        }
+        for (int b = 0; b < QB; ++b) st[b].O[f % DB] = mfma_f16(__builtin_bit_cast(f16x8_t, v), P[b][f / DB], st[b].O[f % DB]);
+        if (f + 1 < 2 * DB) v = codes_f16(next.x, next.y);
         __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int b = 0; b < QB; ++b) {
-        const f16x8_t both[2] = {operand(b, 0), operand(b, 1)};
-        softmax_sum(st[b], both, ev);
       }
     }
     it = nx;
@@ -1023,9 +1033,9 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void attention_q_tile_kernel(AttAr
       }
   }
   __syncthreads();  // LDS is free
-  if (any_thread<kTileThreads / 64>(bad, reinterpret_cast<int*>(kv_lds))) {  // nothing of out is written yet: it may be q
+  if (any_thread<NW>(bad, reinterpret_cast<int*>(kv_lds))) {  // nothing of out is written yet: it may be q
     __syncthreads();  // the flags are read
-    for (int r = r0 + wave; r < r1; r += kTileThreads / 64)
+    for (int r = r0 + wave; r < r1; r += NW)
       attend_row<D>(a, head, sp, r, tl, i0, i1, z, reinterpret_cast<float*>(kv_lds) + wave * D);
     return;
   }
@@ -1053,22 +1063,21 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void attention_q_tile_kernel(AttAr
 
 // ---- the splits of a row, joined
 //
-// Work-group: one row.  Every wave weighs the splits (lane = split), groups of D / 4
-// threads add up every NG-th of them.
+// WPR waves per row.  Every wave weighs the splits (lane = split); groups of D / 4
+// lanes add up every NG-th of them.
 constexpr int kMostSplits = 64;
 constexpr int kJoinThreads = 256;
+constexpr int kJoinManyRows = 2048;
 
-template <int D>
-__global__ __launch_bounds__(kJoinThreads) void attention_q_join_kernel(AttArgs a) {
-  constexpr int COLS = D / 4, NG = kJoinThreads / COLS;
-  __shared__ float ws[kMostSplits];
-  __shared__ __align__(16) float sums[NG][D];
-  const int per = a.T * a.G, head = blockIdx.x / per, r = blockIdx.x % per;
-  const Span sp = span_of(a.span, head / a.Hkv, a.pos0, a.T);
-  if (r >= sp.count * a.G) return;
+template <int D, int WPR>
+__global__ __launch_bounds__(kJoinThreads) void attention_q_join_kernel(AttArgs a, int rows) {
+  constexpr int COLS = D / 4, NG = 64 * WPR / COLS, RPW = kJoinThreads / 64 / WPR;  // rows of a work-group
+  __shared__ __align__(16) float sums[RPW][NG][D];
+  const int lane = threadIdx.x & 63, t = threadIdx.x % (64 * WPR), slot = threadIdx.x / (64 * WPR);
+  const int row = blockIdx.x * RPW + slot, per = a.T * a.G, head = row / per, r = row % per;
+  const bool in = row < rows && r < span_of(a.span, min(head, a.heads - 1) / a.Hkv, a.pos0, a.T).count * a.G;
   const size_t pr = part_row(a, head, r, 0);
-  const int lane = threadIdx.x & 63;
-  const float2 ml = lane < a.splits ? a.ml[pr + lane] : make_float2(-INFINITY, 0.0f);
+  const float2 ml = in && lane < a.splits ? a.ml[pr + lane] : make_float2(-INFINITY, 0.0f);
   float top = ml.x;
 #pragma unroll
   for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
@@ -1076,25 +1085,28 @@ __global__ __launch_bounds__(kJoinThreads) void attention_q_join_kernel(AttArgs 
   float total = w;
 #pragma unroll
   for (int x = 32; x >= 1; x >>= 1) total += __shfl_xor(total, x, 64);
-  if (threadIdx.x < 64) ws[lane] = w;
-  __syncthreads();
-  const int c = threadIdx.x % COLS, g = threadIdx.x / COLS;
+  const int c = t % COLS, g = t / COLS;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int z = g; z < a.splits; z += NG) {
-    const float f = ws[z];
-    if (f == 0.0f && a.ml[pr + z].y == 0.0f) continue;  // a share without keys: nothing was written
+  for (int z0 = 0; z0 < a.splits; z0 += NG) {
+    const int z = z0 + g;
+    const float f = __shfl(w, z & 63, 64), y = __shfl(ml.y, z & 63, 64);
+    if (!in || z >= a.splits || y == 0.0f) continue;  // a share without keys: nothing was written
     const float4 x = *reinterpret_cast<const float4*>(a.part + (pr + z) * D + 4 * c);
     v.x = fmaf(f, x.x, v.x), v.y = fmaf(f, x.y, v.y), v.z = fmaf(f, x.z, v.z), v.w = fmaf(f, x.w, v.w);
   }
-  *reinterpret_cast<float4*>(&sums[g][4 * c]) = v;
-  __syncthreads();
-  if (threadIdx.x < COLS) {
+  if constexpr (NG > 1) {
+    *reinterpret_cast<float4*>(&sums[slot][g][4 * c]) = v;
+    __syncthreads();
+    if (g == 0) {
 #pragma unroll
-    for (int x = 1; x < NG; ++x) {
-      const float4 y = *reinterpret_cast<const float4*>(&sums[x][4 * c]);
-      v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
+      for (int x = 1; x < NG; ++x) {
+        const float4 y = *reinterpret_cast<const float4*>(&sums[slot][x][4 * c]);
+        v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
+      }
     }
+  }
+  if (in && g == 0) {
     const float f = total == 0.0f ? 0.0f : 1.0f / total;
     *reinterpret_cast<uint2*>(a.out + q_row(a, head, r) * D + 4 * c) =
         make_uint2(f32_to_bf16_bits(v.x * f) | f32_to_bf16_bits(v.y * f) << 16,
@@ -1104,48 +1116,48 @@ __global__ __launch_bounds__(kJoinThreads) void attention_q_join_kernel(AttArgs 
 
 // How a call is run.
 struct Plan {
-  int variant;      // 0: attention_q_few_kernel, 1 ..: attention_q_tile_kernel
-  int rows, blocks; // of a work-group, work-groups per head and split
-  int splits;       // shares of a row's tiles
+  int variant;  // 0: attention_q_few_kernel, 1, 2: attention_q_tile_kernel of 64 or 128 rows
+  int blocks;   // work-groups per head and split
+  int splits;   // shares of a row's tiles
+  int share;    // tiles of a share
 };
 
-Plan plan_of(int64_t heads, int T, int G, int D, int pos0, int window, int prefix) {
+Plan plan_of(int64_t heads, int T, int G, int D, int pos0, bool spans, int window, int prefix) {
   Plan p;
   const int64_t rows = static_cast<int64_t>(T) * G;
-  int64_t tiles = (static_cast<int64_t>(pos0) + T + kKvBlock - 1) / kKvBlock;
-  p.variant = rows <= 16 ? 0 : heads * ((rows + 127) / 128) >= 512 && D < 256 ? 2 : 1;
-  p.rows = p.variant == 0 ? 16 : p.variant == 1 ? 64 : 128;
+  // tiles of a row block: all up to the call's end, or a window's (and the prefix's)
+  auto tiles_of_rows = [&](int64_t block) {
+    const int64_t all = (static_cast<int64_t>(pos0) + T + kKvBlock - 1) / kKvBlock;
+    if (window <= 0) return all;
+    const int64_t tokens = std::min<int64_t>(T, block / G + 2);
+    return std::min<int64_t>(all, (static_cast<int64_t>(window) + tokens) / kKvBlock + 2 + prefix / kKvBlock + 1);
+  };
+  auto with = [&](int variant, int64_t block, int64_t target, int64_t least) {
+    p.variant = variant;
+    p.blocks = static_cast<int>((rows + block - 1) / block);
+    const int64_t tiles = tiles_of_rows(block);
+    p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({target / (heads * p.blocks), tiles / least, kMostSplits})));
+    p.share = static_cast<int>((tiles + p.splits - 1) / p.splits);
+    return heads * p.blocks * p.splits;
+  };
 #ifdef SWEEP
-  static const int V = getenv("V") ? atoi(getenv("V")) : 0;
-  if (p.variant && V) { p.variant = V; p.rows = V == 1 || V == 3 ? 64 : V == 6 ? 256 : 128; }
+  static const int FT = getenv("FT") ? atoi(getenv("FT")) : 0, FL = getenv("FL") ? atoi(getenv("FL")) : 4, V = getenv("V") ? atoi(getenv("V")) : 0;
+  if (rows <= 16 && FT) { with(0, 16, FT, FL); return p; }
+  if (V) { with(V, V == 1 ? 64 : 128, getenv("TG") ? atoi(getenv("TG")) : 512, 4); return p; }
 #endif
-  p.blocks = static_cast<int>((rows + p.rows - 1) / p.rows);
-  if (window > 0) {
-    const int64_t tokens = std::min<int64_t>(T, p.rows / G + 2);
-    tiles = std::min<int64_t>(tiles, (static_cast<int64_t>(window) + tokens) / kKvBlock + 2 + prefix / kKvBlock + 1);
+  if (rows <= 16) {
+    with(0, 16, spans ? 512 : 256, 4);
+    return p;
   }
-  const int64_t wgs = heads * p.blocks;
-  int64_t target = 512, least = 4;
-#ifdef SWEEP
-  static const int TG = getenv("TG") ? atoi(getenv("TG")) : 512, LE = getenv("LE") ? atoi(getenv("LE")) : 4;
-  target = TG, least = LE;
-#endif
-  p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({target / wgs, tiles / least, kMostSplits})));
+  const int64_t least = 4 + heads * rows / 2048;
+  if (D < 256 && with(2, 128, 512, std::max<int64_t>(least, 32)) >= 512) return p;
+  with(1, 64, 512, least);
   return p;
-}
-
-template <int D, int QB, int NW>
-void launch_tile(const AttArgs& a, int blocks, bool mods, dim3 grid, hipStream_t s) {
-  constexpr size_t lds = size_t{4} * kKvBlock * D;
-  if (mods)
-    hipLaunchKernelGGL((attention_q_tile_kernel<D, QB, NW, true>), grid, dim3(64 * NW), lds, s, a, blocks);
-  else
-    hipLaunchKernelGGL((attention_q_tile_kernel<D, QB, NW, false>), grid, dim3(64 * NW), lds, s, a, blocks);
 }
 
 template <int D>
 ms_status launch_attention_q(const AttArgs& a, const Plan& p, bool mods, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.heads) * p.blocks * p.splits));
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.heads) * p.blocks * p.splits)), block(64 * kTileWaves);
   if (p.variant == 0) {
     constexpr size_t lds = static_cast<size_t>(few_waves(D)) * few_stages(D) * 2 * kStep * D;
     if (mods)
@@ -1153,22 +1165,30 @@ ms_status launch_attention_q(const AttArgs& a, const Plan& p, bool mods, hipStre
     else
       hipLaunchKernelGGL((attention_q_few_kernel<D, false>), grid, dim3(64 * few_waves(D)), lds, s, a);
   } else if (p.variant == 1) {
-    launch_tile<D, 1, 4>(a, p.blocks, mods, grid, s);
-  } else if (p.variant == 2) {
-    launch_tile<D, 2, 4>(a, p.blocks, mods, grid, s);
+    if (mods)
+      hipLaunchKernelGGL((attention_q_tile_kernel<D, 1, true>), grid, block, tile_lds(D), s, a, p.blocks);
+    else
+      hipLaunchKernelGGL((attention_q_tile_kernel<D, 1, false>), grid, block, tile_lds(D), s, a, p.blocks);
+  } else if constexpr (D < 256) {
+    if (mods)
+      hipLaunchKernelGGL((attention_q_tile_kernel<D, 2, true>), grid, block, tile_lds(D), s, a, p.blocks);
+    else
+      hipLaunchKernelGGL((attention_q_tile_kernel<D, 2, false>), grid, block, tile_lds(D), s, a, p.blocks);
   }
-#ifdef SWEEP
-  else if (p.variant == 4) launch_tile<(D > 64 ? D : 128), 1, 8>(a, p.blocks, mods, grid, s);
-#endif
-  if (p.splits > 1)
-    hipLaunchKernelGGL(attention_q_join_kernel<D>, dim3(static_cast<unsigned>(a.heads) * a.T * a.G), dim3(kJoinThreads), 0, s, a);
+  if (p.splits > 1) {
+    const int rows = a.heads * a.T * a.G;
+    if (rows >= kJoinManyRows)
+      hipLaunchKernelGGL((attention_q_join_kernel<D, 1>), dim3((rows + 3) / 4), dim3(kJoinThreads), 0, s, a, rows);
+    else
+      hipLaunchKernelGGL((attention_q_join_kernel<D, 4>), dim3(rows), dim3(kJoinThreads), 0, s, a, rows);
+  }
   return hipGetLastError() == hipSuccess ? MS_OK : MS_E_HIP;
 }
 
 // rows of all sequences that a call may have: grids and row numbers stay in 31 bits
 constexpr int64_t kMostRows = int64_t{1} << 22;
 
-// [rows][splits] results of D floats, maxima and sums
+// [rows][splits] results of D floats, exponents and sums
 uint64_t workspace_of(int64_t rows, int splits, int D) {
   return static_cast<uint64_t>(rows) * splits * (D + 2) * sizeof(float);
 }
@@ -1270,9 +1290,9 @@ ms_status ms_attention_q_workspace(const ms_kv_cache_q* cache, int32_t T, int32_
   if (T == 0) return MS_OK;
   const int64_t rows = static_cast<int64_t>(T) * Hq;
   if (rows > kMostRows || rows * cache->n_seqs > kMostRows) return MS_E_UNSUPPORTED;
-  // without a window, which only makes the splits fewer
+  // without a window, which only makes the splits fewer, and with spans, which may make them more
   const Plan p = plan_of(static_cast<int64_t>(cache->n_seqs) * cache->n_kv_heads, T, Hq / cache->n_kv_heads, cache->head_dim,
-                         pos0, 0, 0);
+                         pos0, true, 0, 0);
   if (p.splits > 1) *bytes_out = workspace_of(rows * cache->n_seqs, p.splits, cache->head_dim);
   return MS_OK;
 }
@@ -1315,10 +1335,12 @@ ms_status ms_attention_q(const ms_kv_cache_q* cache, const void* q, int32_t T, i
   a.cap = opts ? opts->softcap : 0.0f;
   const float scale = opts && opts->scale > 0.0f ? opts->scale : 1.0f / std::sqrt(static_cast<float>(D));
   const bool scores = a.cap > 0.0f || a.slopes;  // more than the product's scale
+  a.scores = scores;
   a.pre = scores ? scale : 1.0f;
   a.mul = scores ? kLog2e : scale * kLog2e;
-  const Plan p = plan_of(a.heads, T, a.G, D, pos0, a.window, a.prefix);
+  const Plan p = plan_of(a.heads, T, a.G, D, pos0, span_dev != nullptr, a.window, a.prefix);
   a.splits = p.splits;
+  a.share = p.share;
   a.part = static_cast<float*>(workspace_dev);
   a.ml = reinterpret_cast<float2*>(a.part + rows * p.splits * D);
   const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -158,14 +158,15 @@ def _ptr(x):
     """Device/host address of a tensor, numpy array or integer (None -> NULL)."""
     if x is None:
         return None
+    address = getattr(x, "data_ptr", None)  # a tensor
+    if address is not None:
+        assert x.is_contiguous()
+        return address()
     if isinstance(x, int):
         return x
     if isinstance(x, np.ndarray):
         assert x.flags.c_contiguous
         return x.ctypes.data
-    if hasattr(x, "data_ptr"):
-        assert x.is_contiguous()
-        return x.data_ptr()
     raise TypeError("cannot take the address of %r" % type(x))
 
 
@@ -460,24 +461,26 @@ def _ref(x):
 
 
 def ms_rope_kv_q(cache, rope, qkv, T, Hq, pos0, q_out, span=None, stream=None):
-    _check(lib.ms_rope_kv_q(_ref(cache), _ref(rope), _ptr(qkv), int(T), int(Hq), int(pos0), _ptr(span), _ptr(q_out),
-                            _stream(stream)), what="ms_rope_kv_q")
+    st = lib.ms_rope_kv_q(_ref(cache), _ref(rope), _ptr(qkv), T, Hq, pos0, _ptr(span), _ptr(q_out), _stream(stream))
+    if st:
+        _check(st, what="ms_rope_kv_q")
 
 
 def ms_kv_read_q(cache, pos0, n, k_out, v_out, stream=None):
-    _check(lib.ms_kv_read_q(_ref(cache), int(pos0), int(n), _ptr(k_out), _ptr(v_out), _stream(stream)),
-           what="ms_kv_read_q")
+    st = lib.ms_kv_read_q(_ref(cache), pos0, n, _ptr(k_out), _ptr(v_out), _stream(stream))
+    if st:
+        _check(st, what="ms_kv_read_q")
 
 
 def ms_attention_q_workspace(cache, T, Hq, pos0):
     n = ctypes.c_uint64()
-    _check(lib.ms_attention_q_workspace(_ref(cache), int(T), int(Hq), int(pos0), ctypes.byref(n)),
-           what="ms_attention_q_workspace")
+    _check(lib.ms_attention_q_workspace(_ref(cache), T, Hq, pos0, ctypes.byref(n)), what="ms_attention_q_workspace")
     return n.value
 
 
 def ms_attention_q(cache, q, T, Hq, pos0, out, workspace=None, opts=None, span=None, stream=None):
     """workspace: a device tensor of at least ms_attention_q_workspace bytes."""
-    n = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.ms_attention_q(_ref(cache), _ptr(q), int(T), int(Hq), int(pos0), _ptr(span), _ref(opts), _ptr(out),
-                              _ptr(workspace), n, _stream(stream)), what="ms_attention_q")
+    st = lib.ms_attention_q(_ref(cache), _ptr(q), T, Hq, pos0, _ptr(span), _ref(opts), _ptr(out), _ptr(workspace),
+                            0 if workspace is None else workspace.nbytes, _stream(stream))
+    if st:
+        _check(st, what="ms_attention_q")
