@@ -74,19 +74,23 @@ __device__ __forceinline__ Span span_of(const int32_t* span, int s, int pos0, in
 // ------------------------------------------------------ rotary and append
 //
 // Work-group: the tokens of one sequence that fall into one block of 64 cache
-// positions, for one head (query heads alike, so that the grid is the same).
-// Thread c of a row takes four consecutive values; keys and values stay in
-// registers between the block's largest magnitude and their codes.  The angle
-// p f is reduced to a fraction of a turn in double precision (a position of
-// 2^20 and 24 bits after it fit); sine and cosine of the fraction are fp32.
-constexpr int kAppendThreads = 256;
+// positions, for `group` heads one after another (queries, keys and values alike).
+// The tokens' angles are computed once (LDS): the angle p f is reduced to a fraction
+// of a turn in double precision (a position of 2^20 and 24 bits after it fit), its
+// sine and cosine are fp32.  Thread c of a row takes four consecutive values; a key's
+// or value's stay in registers between the block's largest magnitude and their codes.
+// Bound by the bytes: 2048 tokens of 48 heads of 128, 71 MB, take 20 us (3.5 TB/s); a
+// token of 40 heads 4.6 us.  With every head's angles computed by themselves and a
+// pair's partner read again instead of taken from its lane, the prompt took 25.
+constexpr int append_threads(int D) { return D == 256 ? 512 : 256; }  // at most 8 passes of a row's threads over 64
+constexpr int kAppendGroups = 512;  // the work-groups that a call is cut into by heads
 
 struct AppendArgs {
   const float* qkv;
   uint16_t* q_out;
   uint8_t *k, *v, *k_exp, *v_exp;
   const int32_t* span;
-  int T, Hq, Hkv, max_ctx, pos0, blocks;
+  int T, Hq, Hkv, max_ctx, pos0, blocks, group;
   int rot, interleaved;
   double log2_base, inv_factor, turns, low, inv_ramp;  // turns: orig_ctx / 2 pi, 0 for f / factor
   float mscale;
@@ -101,101 +105,136 @@ __device__ __forceinline__ double pair_turns(const AppendArgs& a, int i) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kAppendThreads) void rope_kv_q_kernel(AppendArgs a) {
-  constexpr int COLS = D / 4, ROWS = kAppendThreads / COLS, PASSES = kKvBlock / ROWS;
-  __shared__ uint32_t top_s[kAppendThreads / 64];
-  const int heads = a.Hq + 2 * a.Hkv;
-  const int b = blockIdx.x % a.blocks, head = blockIdx.x / a.blocks % heads, seq = blockIdx.x / a.blocks / heads;
+__global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs a) {
+  constexpr int THREADS = append_threads(D), COLS = D / 4, ROWS = THREADS / COLS, PASSES = kKvBlock / ROWS;
+  extern __shared__ __align__(16) float2 turn_s[];  // [tokens][rot / 2] cosine and sine
+  __shared__ uint32_t top_s[2][THREADS / 64];
+  const int heads = a.Hq + 2 * a.Hkv, groups = (heads + a.group - 1) / a.group;
+  const int b = blockIdx.x % a.blocks, hg = blockIdx.x / a.blocks % groups, seq = blockIdx.x / a.blocks / groups;
   const Span sp = span_of(a.span, seq, a.pos0, a.T);
   const int base = (sp.start / kKvBlock + b) * kKvBlock;
   const int lo = max(sp.start, base), hi = min(sp.start + sp.count, base + kKvBlock);
   if (lo >= hi) return;  // uniform
+  const int h0 = hg * a.group, h1 = min(h0 + a.group, heads);
   const int c4 = threadIdx.x % COLS, r0 = threadIdx.x / COLS, j0 = 4 * c4, half = a.rot / 2;
-  const float* src = a.qkv + (static_cast<size_t>(seq) * a.T * heads + head) * D + j0;
   const size_t pitch = static_cast<size_t>(heads) * D;
-  const bool turn = head < a.Hq + a.Hkv && j0 < a.rot;
-  double f[4];
-  if (turn) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = min(j0 + e, a.rot - 1);
-      f[e] = pair_turns(a, a.interleaved ? j / 2 : j < half ? j : j - half);
-    }
-  }
-  float val[PASSES][4];
-#pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    const int p = base + i * ROWS + r0;
-    const bool in = p >= lo && p < hi;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) val[i][e] = 0.0f;
-    if (!in) continue;
-    const float* x = src + (p - sp.start) * pitch;
-    const float4 own = *reinterpret_cast<const float4*>(x);
-    val[i][0] = own.x, val[i][1] = own.y, val[i][2] = own.z, val[i][3] = own.w;
-    if (turn) {
-      float y[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = j0 + e;
-        y[e] = val[i][e];
-        if (j >= a.rot) continue;
-        double t = p * f[e];
+  const float* src = a.qkv + (static_cast<size_t>(seq) * a.T + (lo - sp.start)) * pitch + j0;  // of token lo
+  // a pair's partners of this thread's values: the next value, or `half` away
+  const bool turns = j0 < a.rot, vec = half % 4 == 0, first4 = j0 < half;
+  const int partner = (threadIdx.x & 63) + (first4 ? half / 4 : -(half / 4));  // of the same row
+
+  if (half > 0 && h0 < a.Hq + a.Hkv) {
+    int lanes = 1;  // pairs side by side: a power of two
+    while (lanes < half) lanes *= 2;
+    const int i = threadIdx.x % lanes;
+    if (i < half) {
+      const double f = pair_turns(a, i);
+      for (int p = lo + static_cast<int>(threadIdx.x) / lanes; p < hi; p += THREADS / lanes) {
+        double t = p * f;
         t -= rint(t);
         float s, c;
         sincospif(2.0f * static_cast<float>(t), &s, &c);
-        c *= a.mscale;
-        s *= a.mscale;
-        const bool first = a.interleaved ? !(j & 1) : j < half;
-        const float other = a.interleaved ? val[i][e ^ 1] : x[first ? e + half : e - half];
-        y[e] = val[i][e] * c + (first ? -other * s : other * s);
+        turn_s[(p - lo) * half + i] = make_float2(c * a.mscale, s * a.mscale);
       }
+    }
+  }
+  __syncthreads();
+
+  for (int head = h0; head < h1; ++head) {
+    const bool turn = turns && head < a.Hq + a.Hkv, value = head >= a.Hq + a.Hkv;
+    const size_t row = static_cast<size_t>(seq) * a.Hkv + (value ? head - a.Hq - a.Hkv : head - a.Hq);  // keys and values
+    uint8_t* exps = (value ? a.v_exp : a.k_exp) + row * (a.max_ctx / kKvBlock) + base / kKvBlock;
+    const int was = head >= a.Hq && lo > base ? exponent(*exps) : kExpMin;
+    const float* x = src + static_cast<size_t>(head) * D;
+    float val[PASSES][4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) val[i][e] = y[e];
+    for (int i = 0; i < PASSES; ++i) {
+      const int p = lo + i * ROWS + r0;
+      float4 own = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (p < hi) own = *reinterpret_cast<const float4*>(x + static_cast<size_t>(p - lo) * pitch);
+      val[i][0] = own.x, val[i][1] = own.y, val[i][2] = own.z, val[i][3] = own.w;
+    }
+    if (turn) {
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) {
+        const int p = lo + i * ROWS + r0;
+        if (p >= hi) continue;  // a row's threads alike
+        const float2* cs = turn_s + (p - lo) * half;
+        const float* xr = x + static_cast<size_t>(p - lo) * pitch;
+        if (a.interleaved) {
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            if (j0 + e >= a.rot) continue;
+            const float2 t = cs[(j0 + e) / 2];
+            const float u = val[i][e], w = val[i][e + 1];
+            val[i][e] = u * t.x - w * t.y;
+            val[i][e + 1] = w * t.x + u * t.y;
+          }
+        } else if (vec) {  // the four values are on one side
+          float other[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) other[e] = __shfl(val[i][e], partner, 64);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 t = cs[first4 ? j0 + e : j0 + e - half];
+            val[i][e] = val[i][e] * t.x + (first4 ? -other[e] : other[e]) * t.y;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = j0 + e;
+            if (j >= a.rot) continue;
+            const float2 t = cs[j < half ? j : j - half];
+            val[i][e] = val[i][e] * t.x + (j < half ? -xr[e + half] : xr[e - half]) * t.y;
+          }
+        }
+      }
     }
     if (head < a.Hq) {
-      *reinterpret_cast<uint2*>(a.q_out + ((static_cast<size_t>(seq) * a.T + (p - sp.start)) * a.Hq + head) * D + j0) =
-          make_uint2(f32_to_bf16_bits(val[i][0]) | f32_to_bf16_bits(val[i][1]) << 16,
-                     f32_to_bf16_bits(val[i][2]) | f32_to_bf16_bits(val[i][3]) << 16);
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) {
+        const int p = lo + i * ROWS + r0;
+        if (p < hi)
+          *reinterpret_cast<uint2*>(a.q_out + ((static_cast<size_t>(seq) * a.T + (p - sp.start)) * a.Hq + head) * D + j0) =
+              make_uint2(f32_to_bf16_bits(val[i][0]) | f32_to_bf16_bits(val[i][1]) << 16,
+                         f32_to_bf16_bits(val[i][2]) | f32_to_bf16_bits(val[i][3]) << 16);
+      }
+      continue;
     }
-  }
-  if (head < a.Hq) return;  // uniform
-  uint32_t top = 0;  // bits of the largest finite magnitude
+    uint32_t top = 0;  // bits of the largest finite magnitude
 #pragma unroll
-  for (int i = 0; i < PASSES; ++i)
+    for (int i = 0; i < PASSES; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t u = __float_as_uint(val[i][e]) & 0x7fffffffu;
-      if (u < 0x7f800000u) top = max(top, u);
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t u = __float_as_uint(val[i][e]) & 0x7fffffffu;
+        if (u < 0x7f800000u) top = max(top, u);
+      }
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), s, 64)));
+    uint32_t* tops = top_s[head & 1];  // two in turn: the last head's are read before the barrier of this one's
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();  // every thread has read the old exponent too
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) top = max(top, tops[w]);
+    // top = m 2^x, 1 <= m < 2, and 448 = 1.75 * 2^8; zero and subnormal magnitudes end at kExpMin
+    int ex = static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u);
+    ex = max(min(max(ex, kExpMin), kExpMax), was);
+    if (threadIdx.x == 0) *exps = static_cast<uint8_t>(ex + kExpBias);
+    uint8_t* out = (value ? a.v : a.k) + (row * a.max_ctx + base) * D;
+    const float scale = pow2(-ex);
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int p = lo + i * ROWS + r0;
+      if (p < hi) *reinterpret_cast<uint32_t*>(out + static_cast<size_t>(p - base) * D + j0) = encode4(val[i], scale);
     }
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), s, 64)));
-  const bool value = head >= a.Hq + a.Hkv;
-  const size_t row = static_cast<size_t>(seq) * a.Hkv + (value ? head - a.Hq - a.Hkv : head - a.Hq);
-  uint8_t* exps = (value ? a.v_exp : a.k_exp) + row * (a.max_ctx / kKvBlock) + base / kKvBlock;
-  uint8_t* out = (value ? a.v : a.k) + (row * a.max_ctx + base) * D;
-  const int was = lo > base ? exponent(*exps) : kExpMin;
-  if ((threadIdx.x & 63) == 0) top_s[threadIdx.x >> 6] = top;
-  __syncthreads();  // every thread has read the old exponent too
-#pragma unroll
-  for (int w = 0; w < kAppendThreads / 64; ++w) top = max(top, top_s[w]);
-  // top = m 2^x, 1 <= m < 2, and 448 = 1.75 * 2^8; zero and subnormal magnitudes end at kExpMin
-  int ex = static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u);
-  ex = max(min(max(ex, kExpMin), kExpMax), was);
-  if (threadIdx.x == 0) *exps = static_cast<uint8_t>(ex + kExpBias);
-  const float scale = pow2(-ex);
-#pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    const int p = base + i * ROWS + r0;
-    if (p >= lo && p < hi) *reinterpret_cast<uint32_t*>(out + static_cast<size_t>(p - base) * D + j0) = encode4(val[i], scale);
-  }
-  if (lo > base && ex > was) {  // the positions before the append, at the new exponent
-    const float down = pow2(was - ex);
-    for (int i = threadIdx.x; i < (lo - base) * COLS; i += kAppendThreads) {
-      uint32_t* w = reinterpret_cast<uint32_t*>(out) + i;
-      float v[4];
-      decode4(*w, v);
-      *w = encode4(v, down);
+    if (lo > base && ex > was) {  // the positions before the append, at the new exponent
+      const float down = pow2(was - ex);
+      for (int i = threadIdx.x; i < (lo - base) * COLS; i += THREADS) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(out) + i;
+        float v[4];
+        decode4(*w, v);
+        *w = encode4(v, down);
+      }
     }
   }
 }
@@ -531,28 +570,36 @@ __device__ __forceinline__ void softmax_step(RowState<DB> (&st)[QB], const msk::
 
 // A lane's row: what its scores and masks depend on.
 struct Row {
-  int pos, doc;
+  int pos, low, doc;  // position, the first that its window has
   float slope;
 };
 __device__ __forceinline__ Row row_of(const AttArgs& a, int head, const Span& sp, int r) {
   Row w;
   w.pos = sp.start + r / a.G;
+  w.low = a.window > 0 ? max(w.pos - a.window + 1, 0) : 0;
   w.doc = a.docs ? a.docs[static_cast<size_t>(head / a.Hkv) * a.max_ctx + w.pos] : 0;
   w.slope = a.slopes ? a.slopes[head % a.Hkv * a.G + r % a.G] : 0.0f;
   return w;
 }
 
-// Raw scores of NB key blocks from key k0 on: scaled, capped and biased (a.scores)
-// and masked (`masked`: some row of the wave may not see some of the keys).
+// The documents of a lane's keys of NB key blocks.
 template <int NB>
-__device__ __forceinline__ void modify(const AttArgs& a, const Row& w, const int32_t* docs, int k0, int n, float ks, bool masked,
-                                       msk::f32x4_t (&S)[NB]) {
+__device__ __forceinline__ void load_docs(const int32_t* docs, int k0, int4 (&d)[NB]) {
+#pragma unroll
+  for (int b = 0; b < NB; ++b) d[b] = *reinterpret_cast<const int4*>(docs + k0 + 16 * b + 4 * ((threadIdx.x & 63) >> 4));
+}
+
+// Raw scores of NB key blocks from key k0 on: scaled, capped and biased (a.scores)
+// and masked (`masked`: some row of the wave may not see some of the keys; by_doc:
+// by its document).
+template <int NB>
+__device__ __forceinline__ void modify(const AttArgs& a, const Row& w, int k0, int n, float ks, bool masked, bool by_doc,
+                                       const int4 (&docs)[NB], msk::f32x4_t (&S)[NB]) {
   const int g4 = (threadIdx.x & 63) >> 4;
   const float f = ks * a.pre, inv_cap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+  if (a.scores) {
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int j0 = k0 + 16 * b + 4 * g4;
-    if (a.scores) {
+    for (int b = 0; b < NB; ++b) {
       S[b] *= f;
       if (a.cap > 0.0f) {
 #pragma unroll
@@ -560,16 +607,28 @@ __device__ __forceinline__ void modify(const AttArgs& a, const Row& w, const int
       }
       if (a.slopes) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[b][r] -= w.slope * fabsf(static_cast<float>(w.pos - j0 - r));
+        for (int r = 0; r < 4; ++r) S[b][r] -= w.slope * fabsf(static_cast<float>(w.pos - (k0 + 16 * b + 4 * g4) - r));
       }
     }
-    if (masked) {
-      int4 dj = make_int4(0, 0, 0, 0);
-      if (docs) dj = *reinterpret_cast<const int4*>(docs + j0);
-      const int d[4] = {dj.x, dj.y, dj.z, dj.w};
+  }
+  if (masked) {
+    const int pre = min(a.prefix, n);
+    const uint32_t span = static_cast<uint32_t>(w.pos - w.low);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int j = k0 + 16 * b + 4 * g4 + r;
+        if (!(static_cast<uint32_t>(j - w.low) <= span || j < pre)) S[b][r] = -INFINITY;
+      }
+  }
+  if (by_doc) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int d[4] = {docs[b].x, docs[b].y, docs[b].z, docs[b].w};
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (!sees(a, w.pos, j0 + r, n, w.doc, d[r])) S[b][r] = -INFINITY;
+        if (d[r] != w.doc || w.doc < 0) S[b][r] = -INFINITY;
     }
   }
 }
@@ -615,14 +674,11 @@ template <int D>
 __device__ __forceinline__ int value_slot(int u) { return (((u & 7) | ((u >> 1) & 8)) / (256 / D)) & (D / 16 - 1); }
 
 constexpr int few_waves(int D) { return D == 256 ? 4 : 8; }
-#ifndef FS
-#define FS 2
-#endif
-constexpr int few_stages(int D) { return D == 64 ? FS : 2; }
+constexpr int kFewStages = 2;
 
 template <int D, bool MODS>
 __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttArgs a) {
-  constexpr int NW = few_waves(D), NST = few_stages(D), DB = D / 16;
+  constexpr int NW = few_waves(D), NST = kFewStages, DB = D / 16;
   constexpr int PIECES = D / 16, RPL = 64 / PIECES;  // 16-byte pieces of a row, rows per load
   constexpr int KB = kStep * D, SB = 2 * KB, NK = KB / 1024, NL = 2 * NK;
   constexpr int PP = D + 4;                          // floats of a merged row
@@ -680,13 +736,15 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
   for (int s = wave; s < steps; s += NW) {
     int ek, ve_s;
     exps.at(tl, i0, i1, i0 + (s >> 1), ke, ve, ek, ve_s);
+    const int k0 = key0(s);
+    int4 dj[2] = {};
+    if (MODS && docs) load_docs(docs, k0, dj);
     msk::wait_vm<(NST - 2) * NL>();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     issue(s + NW * (NST - 1), nxt);
     const unsigned char* sg = ring + cur * SB;
     cur = cur + 1 == NST ? 0 : cur + 1;
     nxt = nxt + 1 == NST ? 0 : nxt + 1;
-    const int k0 = key0(s);
     msk::f32x4_t S[1][2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -705,7 +763,7 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
     const bool last = k0 + kStep > n;
     const float ks = pow2(ek), ev = static_cast<float>(ve_s);
     if constexpr (MODS) {
-      modify(a, w, docs, k0, n, ks, true, S[0]);
+      modify(a, w, k0, n, ks, true, docs != nullptr, dj, S[0]);
     } else if (k0 + kStep > sp.start + 1) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -799,8 +857,8 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
   constexpr int TILE = kKvBlock * D, NL = TILE / 1024 / NW;  // bytes of a tile's keys (or values), their loads per wave
   static_assert(NL >= 1 && NL * NW * 1024 == TILE, "loads");
   extern __shared__ __align__(16) unsigned char kv_lds[];
-  __shared__ int doc_s[2 * NW];
-  __shared__ uint32_t near_s[NW];
+  __shared__ int doc_s[2 * NW], one_s[NW];
+  __shared__ uint32_t near_s[NW], whole_s[NW];
   const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = blockIdx.x % a.heads, zj = blockIdx.x / a.heads, j = zj % blocks, z = zj / blocks, seq = head / a.Hkv;
@@ -830,17 +888,21 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
   }
 
   // documents: only tiles with a key of a document between the rows' least and
-  // largest are visited; 64 tiles are looked at at a time
+  // largest are visited, and those whose keys are all of the rows' one document need
+  // no look at it; 64 tiles are looked at at a time
   int d_min = INT32_MAX, d_max = -1, chunk = -1;
-  uint64_t near = ~uint64_t{0};
+  uint64_t near = ~uint64_t{0}, whole = 0, was_whole = 0;  // was_whole: of the 64 before
+  bool one = true;  // all rows are of one document
   if constexpr (MODS) {
     if (docs) {
 #pragma unroll
       for (int b = 0; b < QB; ++b)
-        if (w[b].doc >= 0) {
-          d_min = min(d_min, w[b].doc);
-          d_max = max(d_max, w[b].doc);
-        }
+      {
+        one = one && w[b].doc >= 0;
+        d_min = w[b].doc >= 0 ? min(d_min, w[b].doc) : d_min;
+        d_max = max(d_max, w[b].doc);
+      }
+      one = __all(one);
 #pragma unroll
       for (int x = 8; x >= 1; x >>= 1) {
         d_min = min(d_min, __shfl_xor(d_min, x, 64));
@@ -849,13 +911,16 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
       if (lane == 0) {
         doc_s[wave] = d_min;
         doc_s[NW + wave] = d_max;
+        one_s[wave] = one;
       }
       __syncthreads();
 #pragma unroll
       for (int x = 0; x < NW; ++x) {
         d_min = min(d_min, doc_s[x]);
         d_max = max(d_max, doc_s[NW + x]);
+        one = one && one_s[x];
       }
+      one = one && d_min == d_max;
     }
   }
   // the first tile to visit from i on (the same in every thread)
@@ -866,7 +931,7 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
           if ((i - i0) / 64 != chunk) {  // wave: 16 tiles, lane: a quarter of one
             chunk = (i - i0) / 64;
             const int t = i0 + 64 * chunk + 16 * wave + (lane >> 2);
-            bool hit = false;
+            bool hit = false, all = true;
             if (t < i1) {
               const int4* d = reinterpret_cast<const int4*>(docs + tl.at(t) * kKvBlock + 16 * (lane & 3));
 #pragma unroll
@@ -874,20 +939,33 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
                 const int4 v = d[x];
                 hit |= (v.x >= d_min && v.x <= d_max) || (v.y >= d_min && v.y <= d_max) || (v.z >= d_min && v.z <= d_max) ||
                        (v.w >= d_min && v.w <= d_max);
+                all = all && v.x == d_min && v.y == d_min && v.z == d_min && v.w == d_min;
               }
             }
-            uint64_t h = __ballot(hit);
+            uint64_t h = __ballot(hit), f = __ballot(all);
             h |= h >> 1;
             h |= h >> 2;  // bit 4 k: tile k
-            uint32_t bits = 0;
+            f &= f >> 1;
+            f &= f >> 2;
+            uint32_t bits = 0, full = 0;
 #pragma unroll
-            for (int x = 0; x < 16; ++x) bits |= static_cast<uint32_t>((h >> (4 * x)) & 1) << x;
+            for (int x = 0; x < 16; ++x) {
+              bits |= static_cast<uint32_t>((h >> (4 * x)) & 1) << x;
+              full |= static_cast<uint32_t>((f >> (4 * x)) & 1) << x;
+            }
             __syncthreads();  // the chunk before is read
-            if (lane == 0) near_s[wave] = bits;
+            if (lane == 0) {
+              near_s[wave] = bits;
+              whole_s[wave] = full;
+            }
             __syncthreads();
-            near = 0;
+            was_whole = whole;
+            near = whole = 0;
 #pragma unroll
-            for (int x = 0; x < NW; ++x) near |= static_cast<uint64_t>(near_s[x]) << (16 * x);
+            for (int x = 0; x < NW; ++x) {
+              near |= static_cast<uint64_t>(near_s[x]) << (16 * x);
+              whole |= static_cast<uint64_t>(whole_s[x]) << (16 * x);
+            }
           }
           const uint64_t rest = near >> ((i - i0) & 63);
           if (rest) return i + static_cast<int>(__builtin_ctzll(rest));
@@ -940,11 +1018,20 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
     bool skip, masked;  // whether no row of the wave sees the tile, and whether some do not see all of it
     if constexpr (MODS) {
       skip = !((k0 <= p_max && (a.window <= 0 || k0 + kKvBlock - 1 > p_min - a.window)) || k0 < a.prefix);
-      masked = docs || !((k0 + kKvBlock - 1 <= p_min && (a.window <= 0 || p_max - k0 < a.window)) ||
-                         (k0 + kKvBlock <= a.prefix && k0 + kKvBlock <= n));
+      masked = !((k0 + kKvBlock - 1 <= p_min && (a.window <= 0 || p_max - k0 < a.window)) ||
+                 (k0 + kKvBlock <= a.prefix && k0 + kKvBlock <= n));
     } else {
       skip = k0 > p_max;
       masked = k0 + kKvBlock - 1 > p_min;
+    }
+    int4 dj[4] = {};
+    bool by_doc = false;
+    if constexpr (MODS) {
+      if (docs) {  // before the next tile's loads, which nothing waits for then
+        const int d = it - i0;
+        by_doc = !(one && (((d / 64 == chunk ? whole : was_whole) >> (d & 63)) & 1));
+        if (by_doc && !skip) load_docs(docs, k0, dj);
+      }
     }
     const int after = advance(nx + 1);
     msk::wait_vm<0>();
@@ -977,9 +1064,9 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
         return msk::lds_read_tr8(va + p * 2 * TILE + 32 * (f / DB) * D + 16 * ((f % DB) ^ vswz));
       };
       if constexpr (MODS) {
-        if (masked || a.scores) {
+        if (masked || by_doc || a.scores) {
 #pragma unroll
-          for (int b = 0; b < QB; ++b) modify(a, w[b], docs, k0, n, ks, masked, S[b]);
+          for (int b = 0; b < QB; ++b) modify(a, w[b], k0, n, ks, masked, by_doc, dj, S[b]);
         }
       } else if (masked) {
 #pragma unroll
@@ -1087,13 +1174,23 @@ __global__ __launch_bounds__(kJoinThreads) void attention_q_join_kernel(AttArgs 
   for (int x = 32; x >= 1; x >>= 1) total += __shfl_xor(total, x, 64);
   const int c = t % COLS, g = t / COLS;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int z0 = 0; z0 < a.splits; z0 += NG) {
-    const int z = z0 + g;
-    const float f = __shfl(w, z & 63, 64), y = __shfl(ml.y, z & 63, 64);
-    if (!in || z >= a.splits || y == 0.0f) continue;  // a share without keys: nothing was written
-    const float4 x = *reinterpret_cast<const float4*>(a.part + (pr + z) * D + 4 * c);
-    v.x = fmaf(f, x.x, v.x), v.y = fmaf(f, x.y, v.y), v.z = fmaf(f, x.z, v.z), v.w = fmaf(f, x.w, v.w);
+  for (int z0 = 0; z0 < a.splits; z0 += 4 * NG) {  // four loads in flight
+    float f[4];
+    float4 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int z = z0 + i * NG + g;
+      f[i] = __shfl(w, z & 63, 64);
+      const float y = __shfl(ml.y, z & 63, 64);
+      x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (in && z < a.splits && y != 0.0f)  // a share without keys: nothing was written
+        x[i] = *reinterpret_cast<const float4*>(a.part + (pr + z) * D + 4 * c);
+      else
+        f[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      v.x = fmaf(f[i], x[i].x, v.x), v.y = fmaf(f[i], x[i].y, v.y), v.z = fmaf(f[i], x[i].z, v.z), v.w = fmaf(f[i], x[i].w, v.w);
   }
   if constexpr (NG > 1) {
     *reinterpret_cast<float4*>(&sums[slot][g][4 * c]) = v;
@@ -1140,11 +1237,6 @@ Plan plan_of(int64_t heads, int T, int G, int D, int pos0, bool spans, int windo
     p.share = static_cast<int>((tiles + p.splits - 1) / p.splits);
     return heads * p.blocks * p.splits;
   };
-#ifdef SWEEP
-  static const int FT = getenv("FT") ? atoi(getenv("FT")) : 0, FL = getenv("FL") ? atoi(getenv("FL")) : 4, V = getenv("V") ? atoi(getenv("V")) : 0;
-  if (rows <= 16 && FT) { with(0, 16, FT, FL); return p; }
-  if (V) { with(V, V == 1 ? 64 : 128, getenv("TG") ? atoi(getenv("TG")) : 512, 4); return p; }
-#endif
   if (rows <= 16) {
     with(0, 16, spans ? 512 : 256, 4);
     return p;
@@ -1159,7 +1251,7 @@ template <int D>
 ms_status launch_attention_q(const AttArgs& a, const Plan& p, bool mods, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.heads) * p.blocks * p.splits)), block(64 * kTileWaves);
   if (p.variant == 0) {
-    constexpr size_t lds = static_cast<size_t>(few_waves(D)) * few_stages(D) * 2 * kStep * D;
+    constexpr size_t lds = static_cast<size_t>(few_waves(D)) * kFewStages * 2 * kStep * D;
     if (mods)
       hipLaunchKernelGGL((attention_q_few_kernel<D, true>), grid, dim3(64 * few_waves(D)), lds, s, a);
     else
@@ -1249,18 +1341,24 @@ ms_status ms_rope_kv_q(const ms_kv_cache_q* cache, const ms_rope_desc* rope, con
   a.inv_ramp = rope->orig_ctx > 0.0 ? 1.0 / (rope->high - rope->low) : 0.0;
   a.mscale = static_cast<float>(rope->mscale);
   const int64_t heads = static_cast<int64_t>(Hq) + 2 * Hkv;
-  // in steps, so that no product passes 64 bits
-  const int64_t wgs = heads * a.blocks;
-  if (heads > INT32_MAX || wgs > UINT32_MAX / kAppendThreads || wgs * cache->n_seqs > UINT32_MAX / kAppendThreads)
-    return MS_E_UNSUPPORTED;
-  const dim3 grid(static_cast<unsigned>(wgs * cache->n_seqs)), block(kAppendThreads);
+  if (heads > INT32_MAX) return MS_E_UNSUPPORTED;
+  // heads that share a work-group's angles: as many as leave kAppendGroups work-groups, two
+  // per compute unit.  2048 tokens of 48 heads: 26.3 us with 256, 20.1 with 512, 23.0 with
+  // 1024; 16 pieces of 41 tokens 11.9, 8.7, 8.6
+  const int64_t all = heads * a.blocks;  // at most 2^31 * 2^26; in steps, so that no product passes 64 bits
+  const int threads = append_threads(D);
+  if (all > UINT32_MAX / threads || all * cache->n_seqs > UINT32_MAX / threads) return MS_E_UNSUPPORTED;
+  a.group = static_cast<int>(std::min<int64_t>(std::max<int64_t>(all * cache->n_seqs / kAppendGroups, 1), heads));
+  const int64_t wgs = (heads + a.group - 1) / a.group * a.blocks * cache->n_seqs;
+  const dim3 grid(static_cast<unsigned>(wgs)), block(threads);
+  const size_t lds = sizeof(float2) * std::min(T, kKvBlock) * (a.rot / 2);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (D == 64)
-    hipLaunchKernelGGL(rope_kv_q_kernel<64>, grid, block, 0, s, a);
+    hipLaunchKernelGGL(rope_kv_q_kernel<64>, grid, block, lds, s, a);
   else if (D == 128)
-    hipLaunchKernelGGL(rope_kv_q_kernel<128>, grid, block, 0, s, a);
+    hipLaunchKernelGGL(rope_kv_q_kernel<128>, grid, block, lds, s, a);
   else
-    hipLaunchKernelGGL(rope_kv_q_kernel<256>, grid, block, 0, s, a);
+    hipLaunchKernelGGL(rope_kv_q_kernel<256>, grid, block, lds, s, a);
   return launched();
 }
 
@@ -1339,6 +1437,7 @@ ms_status ms_attention_q(const ms_kv_cache_q* cache, const void* q, int32_t T, i
   a.pre = scores ? scale : 1.0f;
   a.mul = scores ? kLog2e : scale * kLog2e;
   const Plan p = plan_of(a.heads, T, a.G, D, pos0, span_dev != nullptr, a.window, a.prefix);
+  if (p.splits > 1 && workspace_of(rows, p.splits, D) > need) return MS_E_INVALID;  // plan_of: never more
   a.splits = p.splits;
   a.share = p.share;
   a.part = static_cast<float*>(workspace_dev);
