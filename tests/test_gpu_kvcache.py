@@ -473,3 +473,116 @@ def test_prompt_then_decode_eager_and_captured():
         K = np.abs(final.values("k")[s]).max()
         ds = ds + 2.0 ** 24 * 2.0 ** -7 * np.abs(qf).max() * K / np.sqrt(D)
         _close(got[-1][s], o, mags, ds, n, vmax)
+
+
+# ---------------------------------------------- every way a call is cut up
+
+def _bulk_cache(rng, S, H, ctx, D):
+    """Any codes but NaN's, for caches too large to be encoded here."""
+    c = kv.Cache(S, H, ctx, D)
+    for codes, exps in ((c.k, c.ke), (c.v, c.ve)):
+        codes[...] = rng.integers(0, 256, codes.shape, np.uint8)
+        codes[(codes & 127) == 127] = 0x31
+        exps[...] = kv.BIAS - 7 + rng.integers(-1, 2, exps.shape)
+    return c
+
+
+def _check_some(ref, qf, got, pos0, spans, seqs, **kw):
+    docs = kw.pop("docs", None)
+    for s in seqs:
+        one = kv.Cache.__new__(kv.Cache)
+        one.k, one.v, one.ke, one.ve = (x[s:s + 1] for x in (ref.k, ref.v, ref.ke, ref.ve))
+        _check(one, qf[s:s + 1], got[s:s + 1], pos0, None if spans is None else spans[s:s + 1], **kw,
+               **({} if docs is None else dict(docs=docs[s:s + 1])))
+
+
+# blocks of 128 rows (512 work-groups of them: one block with empty rows, two, and in two
+# shares of the keys, joined by a wave a row); blocks of 64 rows in many shares at every
+# width, with enough rows for either join; one token with more than 64 tiles a share; one
+# token of many sequences in two shares
+@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", [
+    (64, 8, 8, 64, 40, 100), (32, 16, 8, 128, 75, 60), (64, 8, 8, 128, 17, 0), (32, 8, 8, 64, 20, 4300), (32, 8, 8, 128, 20, 4300),
+    (1, 16, 16, 256, 140, 3000), (1, 8, 2, 256, 60, 2500), (1, 16, 16, 64, 140, 1500), (1, 16, 16, 128, 140, 1500),
+    (1, 4, 1, 128, 20, 5000), (32, 8, 8, 128, 1, 4200), (32, 64, 8, 64, 1, 4200), (32, 8, 8, 256, 1, 4200)])
+@pytest.mark.parametrize("kw", [{}, dict(window=1100, prefix=70, softcap=15.0), dict(span=True)])
+def test_attention_routes(S, Hq, Hkv, D, T, pos0, kw):
+    ms = _ms()
+    rng = np.random.default_rng(S + T)
+    kw = dict(kw)
+    spans = [(max(0, pos0 - 97 * s), max(1, T - s)) for s in range(S)] if kw.pop("span", False) else None
+    ref = _bulk_cache(rng, S, Hkv, -(-(pos0 + T) // 64) * 64, D)
+    q, qf = _bf16(0.5 * rng.standard_normal((S, T, Hq, D)))
+    got = _run(_cache(ref), q, T, Hq, pos0, ms.attn_opts(**kw) if kw else None,
+               None if spans is None else _span(spans)).float().cpu().numpy()
+    _check_some(ref, qf, got, pos0, spans, sorted({0, 1 % S, S // 2, S - 1}), **kw)
+
+
+@pytest.mark.parametrize("S,Hq,Hkv,T", [(512, 1, 1, 17), (32, 8, 8, 1), (300, 2, 2, 40)])
+def test_attention_documents_over_many_tiles(S, Hq, Hkv, T):
+    """More than 64 tiles a share: one document over all of them, documents that leave whole chunks of tiles out, and a
+    document at both ends of the context."""
+    ms = _ms()
+    rng = np.random.default_rng(S)
+    pos0, D = 8500, 64
+    ctx = -(-(pos0 + T) // 64) * 64
+    ref = _bulk_cache(rng, S, Hkv, ctx, D)
+    q, qf = _bf16(0.5 * rng.standard_normal((S, T, Hq, D)))
+    docs = np.zeros((S, ctx), np.int32)
+    docs[1] = np.arange(ctx) // 100
+    docs[2, 200:8300] = 7
+    docs[3, 30:8510] = np.arange(8480) // 4200 + 1
+    docs[4, pos0:] = -1
+    opts = ms.attn_opts(doc=torch.from_numpy(docs).cuda())
+    got = _run(_cache(ref), q, T, Hq, pos0, opts).float().cpu().numpy()
+    _check_some(ref, qf, got, pos0, None, [0, 1, 2, 3, 4, S - 1], docs=docs)
+    assert not np.any(got[4])
+
+
+def test_two_streams_and_replayed_graphs_do_not_meet():
+    """Two caches, each its own stream, workspace and captured decode step, replayed in turn and at once with eager work
+    between: every step equals the eager calls alone."""
+    ms = _ms()
+    rng = np.random.default_rng(5)
+    S, Hq, Hkv, D, ctx, start, steps = 2, 8, 2, 128, 4096, 3000, 5
+    desc = ms.rope_desc(D, 1e4)
+    first = torch.from_numpy(rng.standard_normal((2, S, start, Hq + 2 * Hkv, D)).astype(np.float32)).cuda()
+    toks = torch.from_numpy(rng.standard_normal((2, steps, S, 1, Hq + 2 * Hkv, D)).astype(np.float32)).cuda()
+
+    class Run:
+        def __init__(self, i):
+            self.cache, self.span = ms.new_kv_cache_q(S, Hkv, D, ctx), _span([(start, 1)] * S)
+            self.x, self.stream, self.graph = torch.zeros_like(toks[0, 0]), torch.cuda.Stream(), None
+            self.q, self.out = (torch.zeros(S, 1, Hq, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            self.ws = torch.empty(max(ms.ms_attention_q_workspace(self.cache, 1, Hq, ctx - 1), 16), dtype=torch.uint8, device="cuda")
+            q = torch.empty(S, start, Hq, D, dtype=torch.bfloat16, device="cuda")
+            ms.ms_rope_kv_q(self.cache, desc, first[i], start, Hq, 0, q)
+            torch.cuda.synchronize()
+
+        def calls(self):
+            _steps(ms, self.cache, self.x, self.q, self.out, self.ws, desc, None, self.span, 1, Hq, ctx - 1, self.stream)
+
+        def step(self, x):
+            with torch.cuda.stream(self.stream):
+                self.x.copy_(x)
+                self.graph.replay() if self.graph else self.calls()
+                got = self.out.clone()
+                self.span[:, 0] += 1
+            return got
+
+    want = []
+    for i in range(2):
+        run = Run(i)
+        want.append([run.step(toks[i, t]) for t in range(steps)])
+        torch.cuda.synchronize()
+    for captured in (False, True):
+        runs = [Run(0), Run(1)]
+        if captured:
+            for r in runs:
+                r.graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(r.graph, stream=r.stream):
+                    r.calls()
+        got = [[r.step(toks[i, t]) for i, r in enumerate(runs)] for t in range(steps)]
+        torch.cuda.synchronize()
+        for t in range(steps):
+            for i in range(2):
+                assert torch.equal(got[t][i], want[i][t]), (captured, t, i)
