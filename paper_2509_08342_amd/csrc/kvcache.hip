@@ -454,14 +454,19 @@ __device__ __forceinline__ void attend_row(const AttArgs& a, int head, const Spa
 // 2^(y + ev - A) code; L and A are whole numbers, so that c S + ev - A is one fma
 // that rounds once whatever their size, and rescaling by their changes is exact.  A
 // makes the largest probability 2^6 to 2^7 when it is set: half an fp16 step is 2^-11
-// of a probability, and the smallest step 2^-30 of the largest weight or less.  One
-// fp16 part is enough here: the 3-bit mantissa of the codes that it meets is 2^-4
-// off already.  The sum is taken of the same fp16 probabilities by the matrix cores
-// (a row of ones), in 32 bits.  Only if it overflows (a probability past fp16: 2^9
-// above the last maximum; the first keys of a row) is the maximum looked for, and L
-// and A moved.  Exponents past 2^24 (kHuge), where whole numbers are no longer exact,
-// leave the row to attend_row.
+// of a probability, and the smallest step 2^-30 of the largest weighted value or
+// less.  One fp16 part is enough here: the 3-bit mantissa of the codes that it meets
+// is 2^-4 off already.  The sum is taken of the same fp16 probabilities by the matrix
+// cores (a row of ones), in 32 bits.  Only if it overflows (a probability past fp16:
+// 2^9 above the last maximum; the first keys of a row) is the maximum looked for, and L
+// and A moved.  The sum knows no values: a block whose scale is so far below an earlier
+// one's (zeros have the least) that n keys could lose it more than n 2^-28 of the
+// largest weight is summed by itself, without 2^ev.  (L is at least the maximum that A
+// was set by, so the weight 1 is 2^(kAim + ev - that block's ev) or more in the sum, and
+// half the smallest fp16 step is 2^-25.)  Exponents past 2^24 (kHuge), where whole
+// numbers are no longer exact, leave the row to attend_row.
 constexpr float kAim = 7.0f;
+constexpr int kFarBelow = 4;
 constexpr float kNone = -3e38f;  // L and A of a row without keys
 constexpr float kHuge = 16777216.0f;
 
@@ -540,22 +545,45 @@ __device__ __forceinline__ msk::f32x4_t probabilities(const msk::f32x4_t (&S)[2 
   return sum;
 }
 
+// The scale of the value blocks so far: whether one is far below an earlier one.
+struct Far {
+  int most = kExpMin;
+  __device__ __forceinline__ bool below(int ev) {
+    const bool far = ev < most - kFarBelow;
+    most = max(most, ev);
+    return far;
+  }
+};
+
+// a row's largest exponent c S, -inf where it sees nothing
+template <int NB>
+__device__ __forceinline__ float top_of(const msk::f32x4_t (&S)[NB], float c) {
+  float top = S[0][0];
+#pragma unroll
+  for (int k = 0; k < NB; ++k)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) top = max_of(top, S[k][r]);
+  return ceilf(group_max(top) * c);
+}
+
 // Softmax of QB rows' scores S of 2 H key blocks: their operands P, and what l, L, A
-// and O become.
+// and O become; far: their values are far below earlier ones (the same in every lane).
 template <int QB, int DB, int H>
 __device__ __forceinline__ void softmax_step(RowState<DB> (&st)[QB], const msk::f32x4_t (&S)[QB][2 * H], float c, float ev,
-                                             f16x8_t (&P)[QB][H]) {
+                                             bool far, f16x8_t (&P)[QB][H]) {
+  if (far) {
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+      const float L = fmaxf(st[b].L, top_of(S[b], c));
+      st[b].l = fmaf(probabilities<H>(S[b], c, kAim - L, P[b])[0], 0x1p-7f, st[b].l * __builtin_amdgcn_exp2f(st[b].L - L));
+      st[b].L = L;
+    }
+  }
 #pragma unroll
   for (int b = 0; b < QB; ++b) {
     msk::f32x4_t sum = probabilities<H>(S[b], c, ev - st[b].A, P[b]);
     if (__any(!(sum[0] < INFINITY))) {
-      float top = S[b][0][0];
-#pragma unroll
-      for (int k = 0; k < 2 * H; ++k)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) top = max_of(top, S[b][k][r]);
-      const float up = ceilf(group_max(top) * c);  // -inf where the row sees nothing
-      const float L = fmaxf(st[b].L, up), A = fmaxf(st[b].A, up + ev - kAim);
+      const float top = top_of(S[b], c), L = fmaxf(st[b].L, top), A = fmaxf(st[b].A, top + ev - kAim);
       st[b].l *= __builtin_amdgcn_exp2f(st[b].L - L);
       const float f = __builtin_amdgcn_exp2f(st[b].A - A);
 #pragma unroll
@@ -564,7 +592,7 @@ __device__ __forceinline__ void softmax_step(RowState<DB> (&st)[QB], const msk::
       st[b].A = A;
       sum = probabilities<H>(S[b], c, ev - A, P[b]);
     }
-    st[b].l = fmaf(sum[0], __builtin_amdgcn_exp2f(st[b].A - ev - st[b].L), st[b].l);
+    if (!far) st[b].l = fmaf(sum[0], __builtin_amdgcn_exp2f(st[b].A - ev - st[b].L), st[b].l);
   }
 }
 
@@ -724,6 +752,7 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
 #pragma unroll
   for (int p = 0; p < NST - 1; ++p) issue(wave + NW * p, p);
   Exps exps;
+  Far far;
   int va;  // this lane's 8 bytes of column block 0
   {
     const int x = (lane >> 1) & 7, u = (x < 4 ? 0 : 12) + 4 * g4 + x;  // x >= 4: key 16 + 4 g + x - 4
@@ -772,7 +801,7 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
           if (k0 + 16 * b + 4 * g4 + x > w.pos) S[0][b][x] = -INFINITY;
     }
     f16x8_t P[1][1];
-    softmax_step<1, DB, 1>(st, S, MODS && a.scores ? a.mul : a.mul * ks, ev, P);
+    softmax_step<1, DB, 1>(st, S, MODS && a.scores ? a.mul : a.mul * ks, ev, far.below(ve_s), P);
 #pragma unroll
     for (int c = 0; c < DB; ++c) {
       uint2 t = msk::lds_read_tr8(sg + va + 16 * (c ^ vswz));
@@ -896,8 +925,7 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
   if constexpr (MODS) {
     if (docs) {
 #pragma unroll
-      for (int b = 0; b < QB; ++b)
-      {
+      for (int b = 0; b < QB; ++b) {
         one = one && w[b].doc >= 0;
         d_min = w[b].doc >= 0 ? min(d_min, w[b].doc) : d_min;
         d_max = max(d_max, w[b].doc);
@@ -1010,6 +1038,7 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
 
   int it = advance(i0), nx = advance(it + 1);  // this tile and the next
   Exps exps;
+  Far far;
   auto step = [&](int p) {
     const int k0 = tl.at(it) * kKvBlock;
     int ek, ve_it;
@@ -1078,7 +1107,7 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
               if (k0 + 16 * kb + 4 * g4 + x > w[b].pos) S[b][kb][x] = -INFINITY;
       }
       f16x8_t P[QB][2];
-      softmax_step<QB, DB, 2>(st, S, MODS && a.scores ? a.mul : a.mul * ks, ev, P);
+      softmax_step<QB, DB, 2>(st, S, MODS && a.scores ? a.mul : a.mul * ks, ev, far.below(ve_it), P);
       uint2 V[4];
 #pragma unroll
       for (int f = 0; f < 4; ++f) V[f] = value(f);

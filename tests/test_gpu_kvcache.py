@@ -347,6 +347,29 @@ def test_attention_of_blocks_far_apart_in_scale(T, pos0, far):
         _check(ref, qf, _run(_cache(ref), q, T, Hq, pos0).float().cpu().numpy(), pos0, None)
 
 
+@pytest.mark.parametrize("T,pos0", [(1, 3000), (4, 500), (150, 200)])
+@pytest.mark.parametrize("apart", [5, 8, 20, 33, 80])
+def test_small_and_zero_values_keep_their_weight(T, pos0, apart):
+    """Scores that favour no block, values of every third block 2^apart below the others', the least scale of all with
+    zeros in it at 80: what they weigh counts in every row's sum, whichever block comes first."""
+    rng = np.random.default_rng(apart)
+    S, Hq, Hkv, D = 1, 8, 2, 64
+    ctx = -(-(pos0 + T) // 64) * 64
+    for first in (0, 1):
+        ref = _random_cache(rng, S, Hkv, ctx, D, spread=0)
+        ref.ve[:, :, first::3] = max(kv.BIAS - 7 - apart, kv.BIAS + kv.EMIN)
+        if apart == 80:
+            zero = np.arange(ctx) // 64 % 3 == first
+            ref.v[:, :, zero] = 0
+        q, qf = _bf16(0.5 * rng.standard_normal((S, T, Hq, D)))
+        got = _run(_cache(ref), q, T, Hq, pos0).float().cpu().numpy()
+        o, mags, ds = kv.attention(qf[0], ref.values("k")[0], ref.values("v")[0], pos0)
+        # the sum's probabilities may be other fp16 numbers than the values' then: half a step of each, 2^13 more of ds / 2;
+        # and the 2^-28 of the largest weight for a key that the sum may leave out
+        n = pos0 + T
+        _close(got[0], o, mags * (1 + n * 2.0 ** -17), ds + 2.0 ** 12, n, np.abs(ref.values("v")).max())
+
+
 @pytest.mark.parametrize("T,pos0", [(1, 700), (5, 100), (150, 64)])
 @pytest.mark.parametrize("exponent", [20, 36, 60])
 @pytest.mark.parametrize("sign", [1, -1])
