@@ -11,7 +11,12 @@ Layer i's forward predicts layer i + 1 from h^i and prefetches it
 attention; layer 0 of the next token is predicted from the last layer's
 intermediate activation h^L of the current token (Sec. 3.2, following
 AdapMoE), and its copies run under the head and layer 0's attention (the
-first layer's window, T_head + T_att)."""
+first layer's window, T_head + T_att).
+
+kv_bits=8 keeps the key/value caches in 8 bits (ms_rope_kv_q,
+ms_attention_q): half the bytes, which the VRAM budget can give to experts,
+any context length, stretched positions (rope) and attention options
+(opts)."""
 from __future__ import annotations
 
 import time
@@ -27,7 +32,9 @@ from workload import to_device
 
 class Decoder:
     def __init__(self, shape: synth.ModelShape, attn: synth.AttnShape, *, seed=0, n_sets=2, max_tokens=1,
-                 max_ctx=256, budget_total=0, keep_f32=True, threads=16):
+                 max_ctx=256, budget_total=0, keep_f32=True, threads=16, kv_bits=16, rope=None, opts=None):
+        if kv_bits not in (8, 16) or (kv_bits == 16 and (rope is not None or opts is not None)):
+            raise ValueError("kv_bits is 16, or 8 with or without rope and opts")
         self.shape, self.attn = shape, attn
         self.stack = Stack(shape, seed=seed, n_sets=n_sets, max_tokens=max_tokens, budget_total=budget_total,
                            keep_f32=keep_f32, threads=threads)
@@ -53,8 +60,15 @@ class Decoder:
         self.head = to_device(hr, shape.dtype)
         self.embed = to_device(er, shape.dtype)
         self.head_f32, self.embed_f32 = (hf, ef) if keep_f32 else (None, None)
-        self.kc = torch.zeros(self.L, Hkv, max_ctx, D, dtype=bf, device=dev)
-        self.vc = torch.zeros(self.L, Hkv, max_ctx, D, dtype=bf, device=dev)
+        self.kv_bits = kv_bits
+        if kv_bits == 8:
+            self.rope, self.opts = rope or ms.rope_desc(D, attn.rope_base), opts
+            room = -(-max_ctx // ms.KV_BLOCK) * ms.KV_BLOCK
+            self.kvq = [ms.new_kv_cache_q(1, Hkv, D, room) for _ in range(self.L)]
+            self.work = torch.empty(0, dtype=torch.uint8, device=dev)
+        else:
+            self.kc = torch.zeros(self.L, Hkv, max_ctx, D, dtype=bf, device=dev)
+            self.vc = torch.zeros(self.L, Hkv, max_ctx, D, dtype=bf, device=dev)
         T = max_tokens
         self.qkv = torch.empty(T, self.n_qkv, dtype=torch.float32, device=dev)
         self.q = torch.empty(T, Hq, D, dtype=bf, device=dev)
@@ -74,6 +88,18 @@ class Decoder:
         """Forget the context (the caches are overwritten as positions fill)."""
         self.pos = 0
 
+    def attend(self, l, T, pos0, stream):
+        """Rotary, append to layer l's cache and attention: self.qkv -> self.o."""
+        a = self.attn
+        if self.kv_bits == 16:
+            ms.ms_rope_kv(self.qkv, T, a.n_heads, a.n_kv_heads, a.head_dim, pos0, a.rope_base, self.q,
+                          self.kc[l], self.vc[l], self.max_ctx, stream)
+            ms.ms_attention(self.q, self.kc[l], self.vc[l], T, a.n_heads, a.n_kv_heads, a.head_dim, pos0,
+                            self.max_ctx, self.o, stream)
+            return
+        ms.ms_rope_kv_q(self.kvq[l], self.rope, self.qkv, T, a.n_heads, pos0, self.q, None, stream)
+        ms.ms_attention_q(self.kvq[l], self.q, T, a.n_heads, pos0, self.o, self.work, self.opts, None, stream)
+
     # ------------------------------------------------------------- a step
     def step(self, x0, T, flags=ms.MS_FWD_PREDICT_NEXT, stream=None, capture=(), marks=None):
         """Run T tokens (x0 [T][d] bf16 device rows, at positions pos ..
@@ -87,6 +113,11 @@ class Decoder:
         d, V = self.shape.d_model, a.vocab
         pos0 = self.pos
         assert pos0 + T <= self.max_ctx and T <= self.max_tokens
+        if self.kv_bits == 8:
+            need = ms.ms_attention_q_workspace(self.kvq[0], T, a.n_heads, pos0)
+            if need > self.work.numel():  # one for all layers: their calls follow each other on the stream
+                stream.synchronize()
+                self.work = torch.empty(need, dtype=torch.uint8, device="cuda")
         cap = {}
         src = x0
 
@@ -100,10 +131,7 @@ class Decoder:
             wq, wo = self.layer_weights(l)
             mark("att")
             ms.ms_dense(src, wq, T, d, self.n_qkv, self.qkv, None, stream)
-            ms.ms_rope_kv(self.qkv, T, a.n_heads, a.n_kv_heads, a.head_dim, pos0, a.rope_base, self.q,
-                          self.kc[l], self.vc[l], self.max_ctx, stream)
-            ms.ms_attention(self.q, self.kc[l], self.vc[l], T, a.n_heads, a.n_kv_heads, a.head_dim, pos0,
-                            self.max_ctx, self.o, stream)
+            self.attend(l, T, pos0, stream)
             ms.ms_dense(self.o, wo, T, a.n_heads * a.head_dim, d, self.att, None, stream)
             ms.ms_residual_norm(self.ctx, src, self.att, T, self.h, stream)
             mark("moe")

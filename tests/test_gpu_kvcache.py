@@ -609,3 +609,53 @@ def test_two_streams_and_replayed_graphs_do_not_meet():
         for t in range(steps):
             for i in range(2):
                 assert torch.equal(got[t][i], want[i][t]), (captured, t, i)
+
+
+def test_decoder_over_the_8_bit_cache():
+    """A two-layer decoder around the experts with kv_bits=8, a prompt and greedy tokens past two scales' blocks, stretched
+    positions, a window and capped scores: every layer's codes and its attention against the oracle."""
+    from decoder import Decoder
+    from gpu_helpers import check_close
+    from oracle import decoder as od
+    from workload import top_bytes
+    ms = _ms()
+    shape, attn = synth.ModelShape("dec-tiny", 2, 256, 512, 8, 2, "bf16"), synth.TINY_ATTN
+    Hq, Hkv, D, P, n_dec = attn.n_heads, attn.n_kv_heads, attn.head_dim, 126, 4
+    kw = dict(softcap=20.0, window=90, prefix=2)
+    f = kv.frequencies(D, attn.rope_base, 4.0, 64, 1.0, 8.0)
+    with Decoder(shape, attn, seed=4, n_sets=2, max_tokens=P, max_ctx=140, budget_total=2 * 8 * shape.expert_bytes, kv_bits=8,
+                 rope=ms.rope_desc(D, attn.rope_base, False, 4.0, 64, 1.0, 8.0), opts=ms.attn_opts(**kw)) as dec:
+        dec.stack.configure(0.5, 2 * 4 * top_bytes(dec.stack.rig, 0.5))
+        for l in range(2):
+            dec.stack.rig.load_tops(l, [0, 1, 2, 3])
+        ms.ms_sync(dec.ctx)
+        x = torch.empty(P, shape.d_model, dtype=torch.bfloat16, device="cuda")
+        x1 = torch.empty(1, shape.d_model, dtype=torch.bfloat16, device="cuda")
+        dec.embed_ids(torch.from_numpy(synth.prompt_tokens(attn, 4, P)).cuda(), P, x)
+        refs = [kv.Cache(1, Hkv, 192, D) for _ in range(2)]
+        for step in range(1 + n_dec):
+            T, pos0 = (P if step == 0 else 1), dec.pos
+            cap = dec.step(x if step == 0 else x1, T, capture=(0, 1))
+            torch.cuda.synchronize()
+            for l in range(2):
+                xin = cap[l]["x"].astype(np.float64)
+                qf, of = dec.f32[l % dec.n_sets]
+                qkv = (xin @ qf.astype(np.float64).T).reshape(T, Hq + 2 * Hkv, D)
+                turned = np.stack([kv.rope(qkv[t, :Hq + Hkv], pos0 + t, D, f) for t in range(T)])
+                refs[l].append(0, pos0, turned[:, Hq:], qkv[:, Hq + Hkv:])
+                k, v, ke, ve = _host(dec.kvq[l])
+                n = pos0 + T
+                blocks = -(-n // 64)
+                assert np.array_equal(ke[..., :blocks], refs[l].ke[..., :blocks])
+                assert np.array_equal(ve[..., :blocks], refs[l].ve[..., :blocks])
+                for got, want in ((k, refs[l].k), (v, refs[l].v)):
+                    # a projection's fp32 error moves a value over the middle of two codes: by one code, and rarely
+                    a, b = got[:, :, :n].astype(int), want[:, :, :n].astype(int)
+                    assert np.abs(a - b)[(a & 127 > 0) & (b & 127 > 0)].max(initial=0) <= 1 and np.mean(a != b) < 1e-3
+                ref = kv.Cache(1, Hkv, k.shape[2], D)
+                ref.k, ref.v, ref.ke, ref.ve = k, v, ke, ve
+                o = kv.attention(od.bf16_round(turned[:, :Hq]), ref.values("k")[0], ref.values("v")[0], pos0, **kw)[0]
+                att = od.bf16_round(o.reshape(T, -1)) @ of.astype(np.float64).T
+                check_close(cap[l]["h"], od.bf16_round(od.rmsnorm(xin + att)), "bf16", "step %d layer %d h" % (step, l))
+            dec.embed_ids(dec.ids, 1, x1)
+        assert dec.pos == P + n_dec
