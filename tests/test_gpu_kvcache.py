@@ -260,6 +260,22 @@ def test_attention_masks(S, Hq, Hkv, D, T, pos0, kw):
     _check(ref, qf, _run(_cache(ref), q, T, Hq, pos0, opts).float().cpu().numpy(), pos0, None, **kw)
 
 
+@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", [(2, 4, 2, 64, 1, 700), (1, 8, 2, 128, 150, 260), (1, 8, 1, 256, 100, 90)])
+@pytest.mark.parametrize("cap", [0.01, 1.0, 128.0, 129.0, 5000.0])
+@pytest.mark.parametrize("size", [0.1, 2.0, 200.0])
+def test_attention_caps(S, Hq, Hkv, D, T, pos0, cap, size):
+    """Caps on both sides of where tanh is taken another way, scores far below, around and far above them."""
+    rng = np.random.default_rng(int(cap))
+    ref = _random_cache(rng, S, Hkv, -(-(pos0 + T) // 64) * 64, D)
+    q, qf = _bf16(size * rng.standard_normal((S, T, Hq, D)))
+    got = _run(_cache(ref), q, T, Hq, pos0, _ms().attn_opts(softcap=cap)).float().cpu().numpy()
+    for s in range(S):
+        o, mags, ds = kv.attention(qf[s], ref.values("k")[s], ref.values("v")[s], pos0, softcap=cap)
+        # tanh = 1 - 2 / (1 + e): e off by 2^-23 and 2 |x| 2^-23 of itself, of which the slope (1 - tanh^2) / 2 leaves
+        # 2^-23, the reciprocal 2^-23 of at most 2, the last rounding 2^-24: 7 steps of 2^-24 of the cap
+        _close(got[s], o, mags, ds + 7 * min(cap, 128.0), pos0 + T, np.abs(ref.values("v")).max())
+
+
 @pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", [(1, 4, 2, 64, 300, 0), (2, 4, 1, 128, 150, 100), (1, 8, 1, 256, 70, 3),
                                                (3, 4, 2, 64, 1, 500), (1, 8, 2, 128, 5, 2000)])
 @pytest.mark.parametrize("length", [1, 50, 64, 130])
