@@ -1267,30 +1267,42 @@ struct Plan {
   int share;    // tiles of a share
 };
 
+// All that a call's splits depend on is rounded down, so that a window makes them no
+// more than they are without it, and `spans` no fewer.
+//   Few rows: a work-group per compute unit, two with spans (their sequences may be of
+// any length), of at least two tiles: 32 sequences of 4000 keys, 32 heads over 8 of 128,
+// take 42.9 us with 256 work-groups and 48.4 with 512; 8 sequences of up to 3001, drafts
+// of five, 24 heads over 8 of 64, 17.1 and 14.6; one token behind 1500 10.0 us with
+// shares of four tiles and 9.4 with two.  Below 2048 / D tiles they are not split, which
+// saves the join: 32 heads over 8 of 128 at 700 keys 8.4 and 10.1 us, at 1000 9.6 and 9.8, at
+// 1500 11.4 and 9.5; 16 over 4 of 256 at 400 14.0 and 13.8, at 700 17.3 and 14.2.
+//   More: row blocks of 128 (more matrix instructions to a converted code) if their
+// work-groups, with shares of sixteen tiles or more on average, fill the chip twice
+// over, else of 64: 2048 tokens behind 8192, 32 heads over 8 of 128, 315 and 384 us; 512
+// behind 4096 58.7 and 67.7; but 1024 behind none 29 and 21.4, and 100 6.7 against 9.6.
 Plan plan_of(int64_t heads, int T, int G, int D, int pos0, bool spans, int window, int prefix) {
   Plan p;
   const int64_t rows = static_cast<int64_t>(T) * G;
-  // tiles of a row block: all up to the call's end, or a window's (and the prefix's)
-  auto tiles_of_rows = [&](int64_t block) {
-    const int64_t all = (static_cast<int64_t>(pos0) + T + kKvBlock - 1) / kKvBlock;
-    if (window <= 0) return all;
-    const int64_t tokens = std::min<int64_t>(T, block / G + 2);
-    return std::min<int64_t>(all, (static_cast<int64_t>(window) + tokens) / kKvBlock + 2 + prefix / kKvBlock + 1);
-  };
+  const int64_t all = (static_cast<int64_t>(pos0) + T + kKvBlock - 1) / kKvBlock;
+  const int64_t mean = std::max<int64_t>(all - T / (2 * kKvBlock), 1);  // over the rows
   auto with = [&](int variant, int64_t block, int64_t target, int64_t least) {
     p.variant = variant;
     p.blocks = static_cast<int>((rows + block - 1) / block);
-    const int64_t tiles = tiles_of_rows(block);
-    p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({target / (heads * p.blocks), tiles / least, kMostSplits})));
-    p.share = static_cast<int>((tiles + p.splits - 1) / p.splits);
+    int64_t most = all;  // tiles of a row block
+    if (window > 0)
+      most = std::min<int64_t>(all, (static_cast<int64_t>(window) + std::min<int64_t>(T, block / G + 2)) / kKvBlock + 3 +
+                                        prefix / kKvBlock);
+    p.splits = static_cast<int>(
+        std::max<int64_t>(1, std::min<int64_t>({target / (heads * p.blocks), std::min(most, mean) / least, kMostSplits})));
+    p.share = static_cast<int>((most + p.splits - 1) / p.splits);
     return heads * p.blocks * p.splits;
   };
   if (rows <= 16) {
-    with(0, 16, spans ? 512 : 256, 4);
+    with(0, 16, spans ? 512 : 256, all * D < 2048 ? all : 2);
     return p;
   }
-  const int64_t least = 4 + heads * rows / 2048;
-  if (D < 256 && with(2, 128, 512, std::max<int64_t>(least, 32)) >= 512) return p;
+  const int64_t least = 4 + heads * rows / 2048;  // what a share costs to write and join
+  if (D < 256 && with(2, 128, 512, std::max<int64_t>(least, 16)) >= 512) return p;
   with(1, 64, 512, least);
   return p;
 }
