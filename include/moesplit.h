@@ -553,7 +553,7 @@ typedef struct {
  * the largest finite magnitude at most 448 * 2^e; larger finite values become
  * the largest code, infinities and NaN the code of NaN.  An append that
  * continues 64 positions keeps e at least what it was, and rounds the
- * positions before pos0 again where e rises (exact but for codes below the
+ * positions before the append again where e rises (exact but for codes below the
  * least normal one); positions past the append are undefined then until they
  * are written.  Two calls that write the same 64 positions must not overlap in
  * time. */
@@ -592,7 +592,11 @@ ms_status ms_attention_q_workspace(const ms_kv_cache_q* cache, int32_t T, int32_
 /* Grouped-query attention over the cache (which holds the call's own tokens:
  * ms_rope_kv_q first): softmax in fp32 with the maximum subtracted.  q, out
  * [n_seqs][T][Hq][D] bf16, 16-byte aligned (out may be q; other overlaps are
- * MS_E_INVALID); Hq any multiple of n_kv_heads; opts NULL: causal.
+ * MS_E_INVALID); Hq any multiple of n_kv_heads; n_seqs T Hq at most 2^22
+ * (MS_E_UNSUPPORTED); opts NULL: causal.  Probabilities are rounded to fp16:
+ * a result is within 2^-10 of the sum of its weighted values' magnitudes, and
+ * n 2^-28 of the largest value for n keys, beside its rounding to bf16 and its
+ * scores' in fp32.
  * workspace_dev: 16-byte aligned, at least ms_attention_q_workspace bytes,
  * used until the call has finished on `stream`; calls that may overlap in
  * time need one each.  What masked keys and values hold (NaN included) does

@@ -241,7 +241,8 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
 
 // ------------------------------------------------------------- read back
 //
-// 16 codes per thread.
+// 16 codes per thread.  Bound by the bytes written; 2048 positions of 8 heads of 128
+// (13 MB) take 4.8 us, one position 2.6.
 constexpr int kReadThreads = 256;
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -713,6 +714,11 @@ __device__ __forceinline__ bool any_thread(bool v, int* flags) {
 // values by transposing reads of eight keys of a column each.  16-byte piece p of
 // row u sits in slot p ^ key_slot(u) or p ^ value_slot(u), so that the lanes
 // which LDS serves together meet 16 different slots of 256 bytes.
+//   Bound by the cache's bytes: 131000 keys of 8 heads of 128, 268 MB, take 42 us (6.4
+// TB/s), 32 sequences of up to 8191 of 4 heads, 95 MB, 20.7; one token behind 1500 is
+// bound by latency, 7 us.  Two stages a wave: at D = 64 they leave room for a second
+// work-group per compute unit, 11.6 us for eight sequences' drafts of five against 16.4
+// with three or four stages.
 constexpr int kStep = 32;
 
 template <int D>
@@ -895,6 +901,12 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
 // its share of the tiles of 64 keys.  Codes come to LDS by direct loads, a tile
 // ahead, and become operands when a wave reads them, as above: the conversions
 // run beside the matrix instructions, and LDS holds and moves a byte per value.
+//   Bound by the issue of vector and matrix instructions (some 300 and 68 a wave and
+// tile of 32 rows): 512 tokens behind 32256, 32 heads over 8 of 128, take 275 us, 1.0
+// PFLOP/s of products; 2048 behind none 52, the 32 tiles of the longest block one after
+// another.  Tiles converted once by all waves and kept in LDS as 16-bit values were
+// slower, as were two groups of four waves with a share of the keys each (357 us for
+// 338 of 2048 tokens behind 8192).
 constexpr int kTileWaves = 4;
 constexpr size_t tile_lds(int D) { return size_t{4} * kKvBlock * D; }  // two stages of keys and values
 
@@ -1199,7 +1211,10 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
 // ---- the splits of a row, joined
 //
 // WPR waves per row.  Every wave weighs the splits (lane = split); groups of D / 4
-// lanes add up every NG-th of them.
+// lanes add up every NG-th of them.  Bound by latency for few rows (4.6 us for 32 rows of 64
+// splits), by the results' bytes for many (10 us for 16384 rows of 4).  One wave a row and
+// four, with the attention before them: 13.4 and 12.9 us with 128 rows, 282 and 295 with
+// 16384.  Joined by the last work-group of a head instead, 131000 keys took 49.6 us for 46.2.
 constexpr int kMostSplits = 64;
 constexpr int kJoinThreads = 256;
 constexpr int kJoinManyRows = 2048;
