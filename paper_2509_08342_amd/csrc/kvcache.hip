@@ -726,7 +726,7 @@ __device__ __forceinline__ int key_slot(int u) { return (u / (256 / D)) & (D / 1
 template <int D>
 __device__ __forceinline__ int value_slot(int u) { return (((u & 7) | ((u >> 1) & 8)) / (256 / D)) & (D / 16 - 1); }
 
-constexpr int few_waves(int D) { return D == 256 ? 4 : 8; }
+constexpr int few_waves(int D) { return D == 256 ? 4 : 8; }  // rings of eight at 256 are more than the LDS
 constexpr int kFewStages = 2;
 
 template <int D, bool MODS>
@@ -910,6 +910,7 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
 constexpr int kTileWaves = 4;
 constexpr size_t tile_lds(int D) { return size_t{4} * kKvBlock * D; }  // two stages of keys and values
 
+// Work-groups a compute unit: two by the registers of 128 rows, or of a width of 256.
 template <int D, int QB, bool MODS>
 __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void attention_q_tile_kernel(AttArgs a, int blocks) {
   constexpr int NW = kTileWaves, ROWS = 16 * NW * QB, DB = D / 16;

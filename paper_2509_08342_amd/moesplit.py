@@ -460,8 +460,14 @@ def _ref(x):
     return None if x is None else ctypes.byref(x)
 
 
+def _span(x):
+    if x is not None and str(getattr(x, "dtype", "torch.int32")) != "torch.int32":
+        raise ValueError("span: torch.int32 expected")
+    return _ptr(x)
+
+
 def ms_rope_kv_q(cache, rope, qkv, T, Hq, pos0, q_out, span=None, stream=None):
-    st = lib.ms_rope_kv_q(_ref(cache), _ref(rope), _ptr(qkv), T, Hq, pos0, _ptr(span), _ptr(q_out), _stream(stream))
+    st = lib.ms_rope_kv_q(_ref(cache), _ref(rope), _ptr(qkv), T, Hq, pos0, _span(span), _ptr(q_out), _stream(stream))
     if st:
         _check(st, what="ms_rope_kv_q")
 
@@ -480,7 +486,7 @@ def ms_attention_q_workspace(cache, T, Hq, pos0):
 
 def ms_attention_q(cache, q, T, Hq, pos0, out, workspace=None, opts=None, span=None, stream=None):
     """workspace: a device tensor of at least ms_attention_q_workspace bytes."""
-    st = lib.ms_attention_q(_ref(cache), _ptr(q), T, Hq, pos0, _ptr(span), _ref(opts), _ptr(out), _ptr(workspace),
+    st = lib.ms_attention_q(_ref(cache), _ptr(q), T, Hq, pos0, _span(span), _ref(opts), _ptr(out), _ptr(workspace),
                             0 if workspace is None else workspace.nbytes, _stream(stream))
     if st:
         _check(st, what="ms_attention_q")

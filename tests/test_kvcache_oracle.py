@@ -182,3 +182,6 @@ def test_cache_shapes_are_checked_by_the_binding():
         ms.kv_cache_q(k, v, ke, ve[:, :, :1])
     with pytest.raises(ValueError):
         ms.attn_opts(slopes=torch.zeros(4, dtype=torch.bfloat16))
+    for fn, args in ((ms.ms_rope_kv_q, (c, _rope(), 4096, 1, 3, 0, 4096)), (ms.ms_attention_q, (c, 4096, 1, 3, 0, 4096, None))):
+        with pytest.raises(ValueError):
+            fn(*args, span=torch.tensor([[0, 1], [0, 1]]))
