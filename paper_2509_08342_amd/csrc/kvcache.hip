@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "device.h"
 #include "kernels.h"
@@ -75,9 +76,8 @@ __device__ __forceinline__ Span span_of(const int32_t* span, int s, int pos0, in
 //
 // Work-group: the tokens of one sequence that fall into one block of 64 cache
 // positions, for `group` heads one after another (queries, keys and values alike).
-// The tokens' angles are computed once (LDS): the angle p f is reduced to a fraction
-// of a turn in double precision (a position of 2^20 and 24 bits after it fit), its
-// sine and cosine are fp32.  Thread c of a row takes four consecutive values; a key's
+// The tokens' angles are computed once (LDS), reduced to a fraction of a turn in
+// double precision.  Thread c of a row takes four consecutive values; a key's
 // or value's stay in registers between the block's largest magnitude and their codes.
 // Bound by the bytes: 2048 tokens of 48 heads of 128, 71 MB, take 20 us (3.5 TB/s); a
 // token of 40 heads 4.6 us.  With every head's angles computed by themselves and a
@@ -92,8 +92,7 @@ struct AppendArgs {
   const int32_t* span;
   int T, Hq, Hkv, max_ctx, pos0, blocks, group;
   int rot, interleaved;
-  double log2_base, inv_factor, turns, low, inv_ramp;  // turns: orig_ctx / 2 pi, 0 for f / factor
-  float mscale;
+  double log2_base, inv_factor, turns, low, inv_ramp, mscale;  // turns: orig_ctx / 2 pi, 0 for f / factor
 };
 
 // turns per position of pair i
@@ -104,10 +103,51 @@ __device__ __forceinline__ double pair_turns(const AppendArgs& a, int i) {
   return f * ((1.0 - keep) * a.inv_factor + keep) * 0.15915494309189535;
 }
 
+// Cosine and sine of t turns times scale: the rest x to a quarter, in half turns, |x| <=
+// 1/4, and the series of both there, to 2^-33.  (Where a work-group has no keys: in fp32.)
+__device__ __forceinline__ double2 turn_of(double t, double scale) {
+  const double q = rint(4.0 * t), x = fma(-0.5, q, 2.0 * t), y = x * x;
+  double s = -0.007370430945714348, c = -0.02580689139001405;
+  s = fma(s, y, 0.08214588661112819);
+  s = fma(s, y, -0.5992645293207919);
+  s = fma(s, y, 2.550164039877345);
+  s = fma(s, y, -5.167712780049969);
+  s = fma(s, y, 3.141592653589793) * x * scale;
+  c = fma(c, y, 0.23533063035889312);
+  c = fma(c, y, -1.3352627688545893);
+  c = fma(c, y, 4.058712126416768);
+  c = fma(c, y, -4.934802200544679);
+  c = fma(c, y, 1.0) * scale;
+  const int n = static_cast<int>(q - 4.0 * floor(0.25 * q));
+  const double a = n & 1 ? s : c, b = n & 1 ? c : s;
+  return make_double2(n == 1 || n == 2 ? -a : a, n >= 2 ? -b : b);
+}
+
+// d as fp32 that a second rounding, to a code, cannot tell from d: of the two neighbours
+// the one with an odd last bit where d is neither.
+__device__ __forceinline__ float to_odd(double d) {
+  const float f = static_cast<float>(d);
+  const double e = d - f;
+  const uint32_t u = __float_as_uint(f);
+  if (!(e > 0.0 || e < 0.0) || (u & 1)) return f;  // exact, or not finite, or odd
+  return __uint_as_float((e > 0.0) == (u >> 31 == 0) ? u + 1 : u - 1);
+}
+
+// One value of a turned pair: u c + w s, *t = (c, s), *rest what their rounding to fp32
+// left.  Keys in double precision (exact: a key's code is the nearest to the turned value,
+// not to its rounding to fp32), queries in fp32, as they go on as bf16.
+template <bool KEY>
+__device__ __forceinline__ float turned(float u, float w, const float2* t, const float2* rest) {
+  const float2 c = *t;
+  if constexpr (!KEY) return u * c.x + w * c.y;
+  const float2 r = *rest;
+  return to_odd(u * (static_cast<double>(c.x) + r.x) + w * (static_cast<double>(c.y) + r.y));
+}
+
 template <int D>
 __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs a) {
   constexpr int THREADS = append_threads(D), COLS = D / 4, ROWS = THREADS / COLS, PASSES = kKvBlock / ROWS;
-  extern __shared__ __align__(16) float2 turn_s[];  // [tokens][rot / 2] cosine and sine
+  extern __shared__ __align__(16) float2 turn_s[];  // [tokens][rot / 2] cosine and sine, then what their rounding left
   __shared__ uint32_t top_s[2][THREADS / 64];
   const int heads = a.Hq + 2 * a.Hkv, groups = (heads + a.group - 1) / a.group;
   const int b = blockIdx.x % a.blocks, hg = blockIdx.x / a.blocks % groups, seq = blockIdx.x / a.blocks / groups;
@@ -123,6 +163,9 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
   const bool turns = j0 < a.rot, vec = half % 4 == 0, first4 = j0 < half;
   const int partner = (threadIdx.x & 63) + (first4 ? half / 4 : -(half / 4));  // of the same row
 
+  float2* const rest_s = turn_s + min(a.T, kKvBlock) * half;
+  const bool keys = h1 > a.Hq;  // else the angles need no more than queries take
+  const float scale = static_cast<float>(a.mscale);
   if (half > 0 && h0 < a.Hq + a.Hkv) {
     int lanes = 1;  // pairs side by side: a power of two
     while (lanes < half) lanes *= 2;
@@ -130,18 +173,26 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
     if (i < half) {
       const double f = pair_turns(a, i);
       for (int p = lo + static_cast<int>(threadIdx.x) / lanes; p < hi; p += THREADS / lanes) {
-        double t = p * f;
-        t -= rint(t);
-        float s, c;
-        sincospif(2.0f * static_cast<float>(t), &s, &c);
-        turn_s[(p - lo) * half + i] = make_float2(c * a.mscale, s * a.mscale);
+        const int at = (p - lo) * half + i;
+        if (keys) {
+          const double2 t = turn_of(p * f, a.mscale);
+          const float2 near = make_float2(static_cast<float>(t.x), static_cast<float>(t.y));
+          turn_s[at] = near;
+          rest_s[at] = make_float2(static_cast<float>(t.x - near.x), static_cast<float>(t.y - near.y));
+        } else {
+          double t = p * f;
+          t -= rint(t);
+          float s, c;
+          sincospif(2.0f * static_cast<float>(t), &s, &c);
+          turn_s[at] = make_float2(c * scale, s * scale);
+        }
       }
     }
   }
   __syncthreads();
 
   for (int head = h0; head < h1; ++head) {
-    const bool turn = turns && head < a.Hq + a.Hkv, value = head >= a.Hq + a.Hkv;
+    const bool turn = turns && head < a.Hq + a.Hkv, value = head >= a.Hq + a.Hkv, key = head >= a.Hq;
     const size_t row = static_cast<size_t>(seq) * a.Hkv + (value ? head - a.Hq - a.Hkv : head - a.Hq);  // keys and values
     uint8_t* exps = (value ? a.v_exp : a.k_exp) + row * (a.max_ctx / kKvBlock) + base / kKvBlock;
     const int was = head >= a.Hq && lo > base ? exponent(*exps) : kExpMin;
@@ -154,21 +205,22 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
       if (p < hi) own = *reinterpret_cast<const float4*>(x + static_cast<size_t>(p - lo) * pitch);
       val[i][0] = own.x, val[i][1] = own.y, val[i][2] = own.z, val[i][3] = own.w;
     }
-    if (turn) {
+    auto rotate = [&](auto is_key) {
+      constexpr bool KEY = decltype(is_key)::value;
 #pragma unroll
       for (int i = 0; i < PASSES; ++i) {
         const int p = lo + i * ROWS + r0;
         if (p >= hi) continue;  // a row's threads alike
-        const float2* cs = turn_s + (p - lo) * half;
+        const float2 *cs = turn_s + (p - lo) * half, *rest = rest_s + (p - lo) * half;
         const float* xr = x + static_cast<size_t>(p - lo) * pitch;
         if (a.interleaved) {
 #pragma unroll
           for (int e = 0; e < 4; e += 2) {
+            const int m = (j0 + e) / 2;
             if (j0 + e >= a.rot) continue;
-            const float2 t = cs[(j0 + e) / 2];
             const float u = val[i][e], w = val[i][e + 1];
-            val[i][e] = u * t.x - w * t.y;
-            val[i][e + 1] = w * t.x + u * t.y;
+            val[i][e] = turned<KEY>(u, -w, cs + m, rest + m);
+            val[i][e + 1] = turned<KEY>(w, u, cs + m, rest + m);
           }
         } else if (vec) {  // the four values are on one side
           float other[4];
@@ -176,20 +228,23 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
           for (int e = 0; e < 4; ++e) other[e] = __shfl(val[i][e], partner, 64);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float2 t = cs[first4 ? j0 + e : j0 + e - half];
-            val[i][e] = val[i][e] * t.x + (first4 ? -other[e] : other[e]) * t.y;
+            const int m = first4 ? j0 + e : j0 + e - half;
+            val[i][e] = turned<KEY>(val[i][e], first4 ? -other[e] : other[e], cs + m, rest + m);
           }
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int j = j0 + e;
+            const int j = j0 + e, m = j < half ? j : j - half;
             if (j >= a.rot) continue;
-            const float2 t = cs[j < half ? j : j - half];
-            val[i][e] = val[i][e] * t.x + (j < half ? -xr[e + half] : xr[e - half]) * t.y;
+            val[i][e] = turned<KEY>(val[i][e], j < half ? -xr[e + half] : xr[e - half], cs + m, rest + m);
           }
         }
       }
-    }
+    };
+    if (turn && key)
+      rotate(std::true_type{});
+    else if (turn)
+      rotate(std::false_type{});
     if (head < a.Hq) {
 #pragma unroll
       for (int i = 0; i < PASSES; ++i) {
@@ -1415,7 +1470,7 @@ ms_status ms_rope_kv_q(const ms_kv_cache_q* cache, const ms_rope_desc* rope, con
   a.turns = rope->orig_ctx / (2.0 * M_PI);
   a.low = rope->low;
   a.inv_ramp = rope->orig_ctx > 0.0 ? 1.0 / (rope->high - rope->low) : 0.0;
-  a.mscale = static_cast<float>(rope->mscale);
+  a.mscale = rope->mscale;
   const int64_t heads = static_cast<int64_t>(Hq) + 2 * Hkv;
   if (heads > INT32_MAX) return MS_E_UNSUPPORTED;
   // heads that share a work-group's angles: as many as leave kAppendGroups work-groups, two
@@ -1427,7 +1482,7 @@ ms_status ms_rope_kv_q(const ms_kv_cache_q* cache, const ms_rope_desc* rope, con
   a.group = static_cast<int>(std::min<int64_t>(std::max<int64_t>(all * cache->n_seqs / kAppendGroups, 1), heads));
   const int64_t wgs = (heads + a.group - 1) / a.group * a.blocks * cache->n_seqs;
   const dim3 grid(static_cast<unsigned>(wgs)), block(threads);
-  const size_t lds = sizeof(float2) * std::min(T, kKvBlock) * (a.rot / 2);
+  const size_t lds = 2 * sizeof(float2) * std::min(T, kKvBlock) * (a.rot / 2);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (D == 64)
     hipLaunchKernelGGL(rope_kv_q_kernel<64>, grid, block, lds, s, a);
