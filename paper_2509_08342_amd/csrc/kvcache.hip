@@ -155,7 +155,6 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
   const int base = (sp.start / kKvBlock + b) * kKvBlock;
   const int lo = max(sp.start, base), hi = min(sp.start + sp.count, base + kKvBlock);
   if (lo >= hi) return;  // uniform
-  const int h0 = hg * a.group, h1 = min(h0 + a.group, heads);
   const int c4 = threadIdx.x % COLS, r0 = threadIdx.x / COLS, j0 = 4 * c4, half = a.rot / 2;
   const size_t pitch = static_cast<size_t>(heads) * D;
   const float* src = a.qkv + (static_cast<size_t>(seq) * a.T + (lo - sp.start)) * pitch + j0;  // of token lo
@@ -164,9 +163,11 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
   const int partner = (threadIdx.x & 63) + (first4 ? half / 4 : -(half / 4));  // of the same row
 
   float2* const rest_s = turn_s + min(a.T, kKvBlock) * half;
-  const bool keys = h1 > a.Hq;  // else the angles need no more than queries take
+  // heads hg, hg + groups, ...: keys, which take longest, are spread; without one the angles need no more than queries take
+  const int past = (a.Hq - hg) % groups, first_key = a.Hq + (past > 0 ? groups - past : -past);
+  const bool keys = first_key < a.Hq + a.Hkv;
   const float scale = static_cast<float>(a.mscale);
-  if (half > 0 && h0 < a.Hq + a.Hkv) {
+  if (half > 0 && (hg < a.Hq || keys)) {
     int lanes = 1;  // pairs side by side: a power of two
     while (lanes < half) lanes *= 2;
     const int i = threadIdx.x % lanes;
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
   }
   __syncthreads();
 
-  for (int head = h0; head < h1; ++head) {
+  for (int head = hg, nth = 0; head < heads; head += groups, ++nth) {
     const bool turn = turns && head < a.Hq + a.Hkv, value = head >= a.Hq + a.Hkv, key = head >= a.Hq;
     const size_t row = static_cast<size_t>(seq) * a.Hkv + (value ? head - a.Hq - a.Hkv : head - a.Hq);  // keys and values
     uint8_t* exps = (value ? a.v_exp : a.k_exp) + row * (a.max_ctx / kKvBlock) + base / kKvBlock;
@@ -266,7 +267,7 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
       }
 #pragma unroll
     for (int s = 32; s >= 1; s >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), s, 64)));
-    uint32_t* tops = top_s[head & 1];  // two in turn: the last head's are read before the barrier of this one's
+    uint32_t* tops = top_s[nth & 1];  // two in turn: the last head's are read before the barrier of this one's
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();  // every thread has read the old exponent too
 #pragma unroll
