@@ -75,13 +75,13 @@ __device__ __forceinline__ Span span_of(const int32_t* span, int s, int pos0, in
 // ------------------------------------------------------ rotary and append
 //
 // Work-group: the tokens of one sequence that fall into one block of 64 cache
-// positions, for `group` heads one after another (queries, keys and values alike).
+// positions, for `group` heads or fewer one after another (queries, keys and values alike).
 // The tokens' angles are computed once (LDS), reduced to a fraction of a turn in
 // double precision.  Thread c of a row takes four consecutive values; a key's
 // or value's stay in registers between the block's largest magnitude and their codes.
-// Bound by the bytes: 2048 tokens of 48 heads of 128, 71 MB, take 20 us (3.5 TB/s); a
-// token of 40 heads 4.6 us.  With every head's angles computed by themselves and a
-// pair's partner read again instead of taken from its lane, the prompt took 25.
+// 2048 tokens of 48 heads of 128, 71 MB, take 22 us (3.2 TB/s), a token of 40 heads 5.3:
+// the bytes, and the double precision of keys.  In fp32 alone they took 20 and 4.6, and a
+// few keys in a million got the code beside the nearest one.
 constexpr int append_threads(int D) { return D == 256 ? 512 : 256; }  // at most 8 passes of a row's threads over 64
 constexpr int kAppendGroups = 512;  // the work-groups that a call is cut into by heads
 
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
 // ------------------------------------------------------------- read back
 //
 // 16 codes per thread.  Bound by the bytes written; 2048 positions of 8 heads of 128
-// (13 MB) take 4.8 us, one position 2.6.
+// (13 MB) take 4.8 to 5.5 us, one position 2.6.
 constexpr int kReadThreads = 256;
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -1475,8 +1475,8 @@ ms_status ms_rope_kv_q(const ms_kv_cache_q* cache, const ms_rope_desc* rope, con
   const int64_t heads = static_cast<int64_t>(Hq) + 2 * Hkv;
   if (heads > INT32_MAX) return MS_E_UNSUPPORTED;
   // heads that share a work-group's angles: as many as leave kAppendGroups work-groups, two
-  // per compute unit.  2048 tokens of 48 heads: 26.3 us with 256, 20.1 with 512, 23.0 with
-  // 1024; 16 pieces of 41 tokens 11.9, 8.7, 8.6
+  // per compute unit.  2048 tokens of 48 heads: 28.1 us with 256, 22.0 with 512, 31.1 with
+  // 1024; 16 pieces of 41 tokens 13.4, 9.7, 13.0
   const int64_t all = heads * a.blocks;  // at most 2^31 * 2^26; in steps, so that no product passes 64 bits
   const int threads = append_threads(D);
   if (all > UINT32_MAX / threads || all * cache->n_seqs > UINT32_MAX / threads) return MS_E_UNSUPPORTED;
