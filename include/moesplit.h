@@ -594,10 +594,10 @@ ms_status ms_attention_q_workspace(const ms_kv_cache_q* cache, int32_t T, int32_
  * ms_rope_kv_q first): softmax in fp32 with the maximum subtracted.  q, out
  * [n_seqs][T][Hq][D] bf16, 16-byte aligned (out may be q; other overlaps are
  * MS_E_INVALID); Hq any multiple of n_kv_heads; n_seqs T Hq at most 2^22
- * (MS_E_UNSUPPORTED); opts NULL: causal.  Probabilities are rounded to fp16:
- * a result is within 2^-10 of the sum of its weighted values' magnitudes, and
- * n 2^-28 of the largest value for n keys, beside its rounding to bf16 and its
- * scores' in fp32.
+ * (MS_E_UNSUPPORTED); opts NULL: causal.  Probabilities keep 22 bits: a result
+ * is within 2^-20 of the sum of its weighted values' magnitudes, and n 2^-28 of
+ * the largest value for n keys, beside its rounding to bf16 and its scores'
+ * and sums' in fp32.
  * workspace_dev: 16-byte aligned, at least ms_attention_q_workspace bytes,
  * used until the call has finished on `stream`; calls that may overlap in
  * time need one each.  What masked keys and values hold (NaN included) does

@@ -509,21 +509,22 @@ __device__ __forceinline__ void attend_row(const AttArgs& a, int head, const Spa
 // block b.  Codes are converted to bf16 (exact); the keys' scale 2^ek multiplies the
 // sums.  (The 8-bit matrix instructions would take the codes as they are, but align
 // the products of a sum to 2^-14 or so of the largest.)
-//   O^T += V^T P^T takes the probabilities where they are, as fp16 pairs,
-// contraction slot 4 h + r of lane group g being key 16 h + 4 g + r of 32, and codes
-// converted to fp16 (exact).  A value block's 2^ev goes into the probability's
-// exponent.
+//   O^T += V^T P^T takes the probabilities where they are, contraction slot 4 h + r of
+// lane group g being key 16 h + 4 g + r of 32, and codes converted to fp16 (exact).  A
+// value block's 2^ev goes into the probability's exponent.  A probability enters as two
+// fp16 parts, rounded and the rest rounded, 22 bits or more together: one would be off by
+// up to 2^-11, more than all the fp32 steps before it.  The second part's products and
+// sums cost nothing where the bytes bound the kernel and a fifth to a third of a prompt
+// (2048 tokens 52.7 -> 63.6 us, 512 behind 32256 271 -> 351).
 //
 // A score's exponent is y = c S, c = mul 2^ek.  A row keeps its sum l = sum 2^(y - L) and O = sum
 // 2^(y + ev - A) code; L and A are whole numbers, so that c S + ev - A is one fma
 // that rounds once whatever their size, and rescaling by their changes is exact.  A
-// makes the largest probability 2^6 to 2^7 when it is set: half an fp16 step is 2^-11
-// of a probability, and the smallest step 2^-30 of the largest weighted value or
-// less.  One fp16 part is enough here: the 3-bit mantissa of the codes that it meets
-// is 2^-4 off already.  The sum is taken of the same fp16 probabilities by the matrix
-// cores (a row of ones), in 32 bits.  Only if it overflows (a probability past fp16:
-// 2^9 above the last maximum; the first keys of a row) is the maximum looked for, and L
-// and A moved.  The sum knows no values: a block whose scale is so far below an earlier
+// makes the largest probability 2^6 to 2^7 when it is set: the smallest fp16 step, which
+// ends the second part, is 2^-30 of the largest weighted value or less.  The sum is
+// taken of the same parts by the matrix cores (a row of ones), in 32 bits.  Only if it
+// overflows (a probability past fp16: 2^9 above the last maximum; the first keys of a
+// row) is the maximum looked for, and L and A moved.  The sum knows no values: a block whose scale is so far below an earlier
 // one's (zeros have the least) that n keys could lose it more than n 2^-28 of the
 // largest weight is summed by itself, without 2^ev.  (L is at least the maximum that A
 // was set by, so the weight 1 is 2^(kAim + ev - that block's ev) or more in the sum, and
@@ -586,25 +587,36 @@ struct RowState {
   __device__ __forceinline__ bool lost() const { return !isfinite(l) || (A != kNone && fabsf(A) > kHuge); }
 };
 
-// Two probabilities: those of the scores s0 and s1.
-__device__ __forceinline__ uint32_t softmax_pair(float s0, float s1, float c, float off) {
-  const f32x2_t p = {__builtin_amdgcn_exp2f(fmaf(s0, c, off)), __builtin_amdgcn_exp2f(fmaf(s1, c, off))};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(p, f16x2_t));
+// Probabilities of eight keys as matrix operands: rounded, and the rest rounded.
+struct Prob {
+  f16x8_t hi, lo;
+};
+
+// Two probabilities, those of the scores s0 and s1, in places 2 i and 2 i + 1.
+__device__ __forceinline__ void softmax_pair(float s0, float s1, float c, float off, int i, Prob& p) {
+  const f32x2_t e = {__builtin_amdgcn_exp2f(fmaf(s0, c, off)), __builtin_amdgcn_exp2f(fmaf(s1, c, off))};
+  const f16x2_t hi = __builtin_convertvector(e, f16x2_t);
+  p.hi[2 * i] = hi[0];
+  p.hi[2 * i + 1] = hi[1];
+  float minus = -1.0f;
+  asm("" : "+s"(minus));  // unknown to the compiler, which makes one mixed fma of it and both conversions then
+  p.lo[2 * i] = static_cast<_Float16>(fmaf(static_cast<float>(hi[0]), minus, e[0]));
+  p.lo[2 * i + 1] = static_cast<_Float16>(fmaf(static_cast<float>(hi[1]), minus, e[1]));
 }
 
 // The probabilities of 2 H key blocks, H operands, and their sum for every row
 // (all four values alike).
 template <int H>
-__device__ __forceinline__ msk::f32x4_t probabilities(const msk::f32x4_t (&S)[2 * H], float c, float off, f16x8_t (&P)[H]) {
+__device__ __forceinline__ msk::f32x4_t probabilities(const msk::f32x4_t (&S)[2 * H], float c, float off, Prob (&P)[H]) {
   const f16x8_t ones = {1, 1, 1, 1, 1, 1, 1, 1};
   msk::f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int h = 0; h < H; ++h) {
-    P[h] = __builtin_bit_cast(
-        f16x8_t, make_uint4(softmax_pair(S[2 * h][0], S[2 * h][1], c, off), softmax_pair(S[2 * h][2], S[2 * h][3], c, off),
-                            softmax_pair(S[2 * h + 1][0], S[2 * h + 1][1], c, off),
-                            softmax_pair(S[2 * h + 1][2], S[2 * h + 1][3], c, off)));
-    sum = mfma_f16(ones, P[h], sum);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      softmax_pair(S[2 * h + i / 2][2 * (i % 2)], S[2 * h + i / 2][2 * (i % 2) + 1], c, off, i, P[h]);
+    sum = mfma_f16(ones, P[h].hi, sum);
+    sum = mfma_f16(ones, P[h].lo, sum);
   }
   return sum;
 }
@@ -634,7 +646,7 @@ __device__ __forceinline__ float top_of(const msk::f32x4_t (&S)[NB], float c) {
 // and O become; far: their values are far below earlier ones (the same in every lane).
 template <int QB, int DB, int H>
 __device__ __forceinline__ void softmax_step(RowState<DB> (&st)[QB], const msk::f32x4_t (&S)[QB][2 * H], float c, float ev,
-                                             bool far, f16x8_t (&P)[QB][H]) {
+                                             bool far, Prob (&P)[QB][H]) {
   if (far) {
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
@@ -881,7 +893,7 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
         for (int x = 0; x < 4; ++x)
           if (k0 + 16 * b + 4 * g4 + x > w.pos) S[0][b][x] = -INFINITY;
     }
-    f16x8_t P[1][1];
+    Prob P[1][1];
     softmax_step<1, DB, 1>(st, S, MODS && a.scores ? a.mul : a.mul * ks, ev, far.below(ve_s), P);
 #pragma unroll
     for (int c = 0; c < DB; ++c) {
@@ -895,7 +907,9 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
         t.y = keep(t.y, k0 + 16 + 4 * g4);
       }
       const uint2 lo = codes_to_f16(t.x), hi = codes_to_f16(t.y);
-      st[0].O[c] = mfma_f16(__builtin_bit_cast(f16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y)), P[0][0], st[0].O[c]);
+      const f16x8_t v = __builtin_bit_cast(f16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y));
+      st[0].O[c] = mfma_f16(v, P[0][0].hi, st[0].O[c]);
+      st[0].O[c] = mfma_f16(v, P[0][0].lo, st[0].O[c]);
     }
   }
   msk::wait_vm<0>();  // the reloads past the last step have landed
@@ -1194,7 +1208,7 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
             for (int x = 0; x < 4; ++x)
               if (k0 + 16 * kb + 4 * g4 + x > w[b].pos) S[b][kb][x] = -INFINITY;
       }
-      f16x8_t P[QB][2];
+      Prob P[QB][2];
       softmax_step<QB, DB, 2>(st, S, MODS && a.scores ? a.mul : a.mul * ks, ev, far.below(ve_it), P);
       uint2 V[4];
 #pragma unroll
@@ -1205,7 +1219,9 @@ __global__ __launch_bounds__(64 * kTileWaves, QB == 1 && D < 256 ? 3 : 2) void a
         if (f + 4 < 2 * DB) V[f % 4] = value(f + 4);
         const uint2 next = V[(f + 1) % 4];
 #pragma unroll
-        for (int b = 0; b < QB; ++b) st[b].O[f % DB] = mfma_f16(__builtin_bit_cast(f16x8_t, v), P[b][f / DB], st[b].O[f % DB]);
+        for (int b = 0; b < QB; ++b) st[b].O[f % DB] = mfma_f16(__builtin_bit_cast(f16x8_t, v), P[b][f / DB].hi, st[b].O[f % DB]);
+#pragma unroll
+        for (int b = 0; b < QB; ++b) st[b].O[f % DB] = mfma_f16(__builtin_bit_cast(f16x8_t, v), P[b][f / DB].lo, st[b].O[f % DB]);
         if (f + 1 < 2 * DB) v = codes_f16(next.x, next.y);
         __builtin_amdgcn_sched_barrier(0);
       }

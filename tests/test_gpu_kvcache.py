@@ -675,3 +675,37 @@ def test_decoder_over_the_8_bit_cache():
                 check_close(cap[l]["h"], od.bf16_round(od.rmsnorm(xin + att)), "bf16", "step %d layer %d h" % (step, l))
             dec.embed_ids(dec.ids, 1, x1)
         assert dec.pos == P + n_dec
+
+
+# ------------------------------------------------------------- probabilities
+
+# one token, a few tokens, row blocks of 64 and of 128, whole and in shares of the keys
+@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", [(1, 8, 2, 128, 1, 200), (2, 4, 2, 64, 5, 1500), (1, 4, 1, 256, 3, 300),
+                                               (1, 16, 8, 64, 90, 200), (1, 4, 2, 128, 40, 3000), (1, 4, 2, 256, 60, 200),
+                                               (64, 8, 8, 64, 40, 100), (32, 16, 8, 128, 75, 130)])
+def test_probabilities_keep_22_bits(S, Hq, Hkv, D, T, pos0):
+    """Five values a column that cancel to about 2^-18 of their terms, one query and exact scores between 0 and -1 for all
+    tokens.  A weight is off by 2^-22 as two fp16 parts, 2^-22 by the scale's three roundings, 2^-22 by the exponent's (below
+    8 in size) and 2^-23 by its exponential: less than 2^-20 with the sums'; parts below fp16's steps by 2^-25 of at least
+    2^6.  One fp16 number would leave up to 2^-11."""
+    rng = np.random.default_rng(T + D)
+    ctx = -(-(pos0 + T) // 64) * 64
+    one = kv.Cache(1, Hkv, ctx, D)
+    one.k[0, :, 1:, 0] = kv.encode(-rng.random((Hkv, ctx - 1)) * np.sqrt(D))
+    p = np.exp(one.values("k")[0, :, :, 0] / np.sqrt(D))
+    for h in range(Hkv):
+        for c in range(D):
+            left = 0.0
+            for i, at in enumerate(rng.choice(np.arange(1, pos0), 5, replace=False)):
+                one.v[0, h, at, c] = kv.encode(256.0 if i == 0 else -left / p[h, at])
+                left += p[h, at] * kv.TABLE[one.v[0, h, at, c]]
+    ref = kv.Cache(S, Hkv, ctx, D)
+    for name in ("k", "v", "ke", "ve"):
+        getattr(ref, name)[...] = getattr(one, name)
+    q, qf = _bf16(np.ones((S, T, Hq, D)))
+    got = _run(_cache(ref), q, T, Hq, pos0).float().cpu().numpy()
+    o, mags, _ = kv.attention(qf[0], one.values("k")[0], one.values("v")[0], pos0)
+    bound = 2.0 ** -8 * np.abs(o) + 2.0 ** -20 * mags + 5 * 2.0 ** -31 * 448
+    assert np.median(np.abs(o) / mags) < 2.0 ** -15
+    for s in (0, S // 2, S - 1):
+        assert np.all(np.abs(got[s] - o) <= bound)
