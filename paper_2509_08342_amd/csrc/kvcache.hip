@@ -366,22 +366,19 @@ __device__ __forceinline__ Tiles tiles_of(const AttArgs& a, int p0, int p1, int 
   return t;
 }
 
-// tanh, relative error below 2^-20: its series near zero, where the
-// difference of exponentials would cancel
-__device__ __forceinline__ float tanh_of(float x) {
+// tanh.  Up to kSeries in size its series, off by less than 2^-22 of itself.
+constexpr float kSeries = 0.25f;
+__device__ __forceinline__ float tanh_series(float x) {
   const float y = x * x;
-  const float series = x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-  const float e = __builtin_amdgcn_exp2f(fabsf(x) * (-2.0f * kLog2e));
-  const float far = (1.0f - e) / (1.0f + e);
-  return fabsf(x) < 0.25f ? series : copysignf(far, x);
+  return x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
 }
-
-// Caps up to here take tanh(x) = 1 - 2 / (1 + e^(2 x)) of every score, off by less than
-// 2^-21 of the cap: 2^-14 at most, an eighth of what fp16 rounds a probability by.
-// Larger ones take tanh_of, whose error follows the score (2048 tokens behind 8192, 16
-// heads of 128 over 2: 306 and 372 us; 206 without a cap).  Either is bound by the
-// exponentials and reciprocals: 16 cycles a wave each.
-constexpr float kSmallCap = 128.0f;
+// Off by less than 2^-20 of itself from kSeries on, and by 2^-25 near zero, where the
+// exponential is nearly 1.
+__device__ __forceinline__ float tanh_exp(float x) {
+  const float e = __builtin_amdgcn_exp2f(fabsf(x) * (-2.0f * kLog2e));
+  return copysignf((1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e), x);
+}
+__device__ __forceinline__ float tanh_of(float x) { return fabsf(x) < kSeries ? tanh_series(x) : tanh_exp(x); }
 
 // Whether the query at position i sees key j of n (document di, dj).
 __device__ __forceinline__ bool sees(const AttArgs& a, int i, int j, int n, int di, int dj) {
@@ -703,19 +700,28 @@ __device__ __forceinline__ void modify(const AttArgs& a, const Row& w, int k0, i
   if (a.scores) {
     float f = ks * a.pre;
     if (a.cap > 0.0f) {
+      // Where all of a wave's scores are far below the cap, none is rounded to steps of the
+      // cap's; else 2^-25 of the cap is as small as the largest one's own rounding.  (2048
+      // tokens behind 8192, 16 heads of 128 over 2: 354 and 402 us; 259 without a cap.)
       f *= 1.0f / a.cap;
-      if (a.cap <= kSmallCap) {
-        f *= 2.0f * kLog2e;
+      float top = 0.0f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          S[b][r] *= f;
+          top = max_of(top, fabsf(S[b][r]));
+        }
+      if (__any(!(top < kSeries))) {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            S[b][r] = fmaf(-2.0f * a.cap, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(S[b][r] * f)), a.cap);
+          for (int r = 0; r < 4; ++r) S[b][r] = a.cap * tanh_exp(S[b][r]);
       } else {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) S[b][r] = a.cap * tanh_of(S[b][r] * f);
+          for (int r = 0; r < 4; ++r) S[b][r] = a.cap * tanh_series(S[b][r]);
       }
       f = 1.0f;
     }

@@ -679,20 +679,13 @@ def test_decoder_over_the_8_bit_cache():
 
 # ------------------------------------------------------------- probabilities
 
-# one token, a few tokens, row blocks of 64 and of 128, whole and in shares of the keys
-@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", [(1, 8, 2, 128, 1, 200), (2, 4, 2, 64, 5, 1500), (1, 4, 1, 256, 3, 300),
-                                               (1, 16, 8, 64, 90, 200), (1, 4, 2, 128, 40, 3000), (1, 4, 2, 256, 60, 200),
-                                               (64, 8, 8, 64, 40, 100), (32, 16, 8, 128, 75, 130)])
-def test_probabilities_keep_22_bits(S, Hq, Hkv, D, T, pos0):
-    """Five values a column that cancel to about 2^-18 of their terms, one query and exact scores between 0 and -1 for all
-    tokens.  A weight is off by 2^-22 as two fp16 parts, 2^-22 by the scale's three roundings, 2^-22 by the exponent's (below
-    8 in size) and 2^-23 by its exponential: less than 2^-20 with the sums'; parts below fp16's steps by 2^-25 of at least
-    2^6.  One fp16 number would leave up to 2^-11."""
-    rng = np.random.default_rng(T + D)
-    ctx = -(-(pos0 + T) // 64) * 64
+def _cancelling(rng, S, Hkv, ctx, D, pos0, cap=0.0):
+    """Caches of one query's (all ones) exact products between 0 and -1 and, in every column, five values that cancel to
+    about 2^-18 of their terms, at positions that every token sees."""
     one = kv.Cache(1, Hkv, ctx, D)
     one.k[0, :, 1:, 0] = kv.encode(-rng.random((Hkv, ctx - 1)) * np.sqrt(D))
-    p = np.exp(one.values("k")[0, :, :, 0] / np.sqrt(D))
+    s = one.values("k")[0, :, :, 0] / np.sqrt(D)
+    p = np.exp(cap * np.tanh(s / cap) if cap else s)
     for h in range(Hkv):
         for c in range(D):
             left = 0.0
@@ -702,10 +695,35 @@ def test_probabilities_keep_22_bits(S, Hq, Hkv, D, T, pos0):
     ref = kv.Cache(S, Hkv, ctx, D)
     for name in ("k", "v", "ke", "ve"):
         getattr(ref, name)[...] = getattr(one, name)
+    return ref
+
+
+def _check_cancelling(S, Hq, Hkv, D, T, pos0, off, **kw):
+    """off: a weight's error.  Beside it, the weights' parts below fp16's steps: 2^-25 of at least 2^6 for each of the five."""
+    ref = _cancelling(np.random.default_rng(T + D), S, Hkv, -(-(pos0 + T) // 64) * 64, D, pos0, kw.get("softcap", 0.0))
     q, qf = _bf16(np.ones((S, T, Hq, D)))
-    got = _run(_cache(ref), q, T, Hq, pos0).float().cpu().numpy()
-    o, mags, _ = kv.attention(qf[0], one.values("k")[0], one.values("v")[0], pos0)
-    bound = 2.0 ** -8 * np.abs(o) + 2.0 ** -20 * mags + 5 * 2.0 ** -31 * 448
+    got = _run(_cache(ref), q, T, Hq, pos0, _ms().attn_opts(**kw) if kw else None).float().cpu().numpy()
+    o, mags, _ = kv.attention(qf[0], ref.values("k")[0], ref.values("v")[0], pos0, **kw)
     assert np.median(np.abs(o) / mags) < 2.0 ** -15
     for s in (0, S // 2, S - 1):
-        assert np.all(np.abs(got[s] - o) <= bound)
+        assert np.all(np.abs(got[s] - o) <= 2.0 ** -8 * np.abs(o) + off * mags + 5 * 2.0 ** -31 * 448)
+
+
+# one token, a few tokens, row blocks of 64 and of 128, whole and in shares of the keys
+CANCELLING = [(1, 8, 2, 128, 1, 200), (2, 4, 2, 64, 5, 1500), (1, 4, 1, 256, 3, 300), (1, 16, 8, 64, 90, 200),
+              (1, 4, 2, 128, 40, 3000), (1, 4, 2, 256, 60, 200), (64, 8, 8, 64, 40, 100), (32, 16, 8, 128, 75, 130)]
+
+
+@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", CANCELLING)
+def test_probabilities_keep_22_bits(S, Hq, Hkv, D, T, pos0):
+    """A weight is off by 2^-22 as two fp16 parts, 2^-22 by the scale's three roundings, 2^-22 by the exponent's (below 8 in
+    size) and 2^-23 by its exponential: less than 2^-20 with the sums'.  One fp16 number would leave up to 2^-11."""
+    _check_cancelling(S, Hq, Hkv, D, T, pos0, 2.0 ** -20)
+
+
+@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", CANCELLING)
+@pytest.mark.parametrize("cap", [2.0, 30.0, 128.0, 1000.0])
+def test_capped_scores_are_as_exact_as_their_size(S, Hq, Hkv, D, T, pos0, cap):
+    """Capped scores of up to 1 whatever the cap: five roundings of the score and its cap, 2^-21, and tanh to 2^-20 of
+    itself, beside the 2^-20 of uncapped ones.  Steps of 2^-22 of a cap of 128 would be 2^-15."""
+    _check_cancelling(S, Hq, Hkv, D, T, pos0, 2.0 ** -20 + 2.0 ** -20 + 2.0 ** -21, softcap=cap)
