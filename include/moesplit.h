@@ -548,8 +548,9 @@ typedef struct {
  * ms_rope_kv (Hkv = cache n_kv_heads, D = head_dim, Hq a multiple of Hkv;
  * 16-byte aligned); q_out [n_seqs][T][Hq][D] bf16 (16-byte aligned); keys
  * (turned) and values go into the cache at the tokens' positions, rounded to
- * the nearest code, ties to even.  Keys turn in double precision, queries in
- * fp32.
+ * the nearest code, ties to even.  Angles are computed in double precision;
+ * keys turn in it too, queries in fp32.  A token's query is the same however
+ * its call is cut up.
  *   The exponent e of 64 positions of a head is the least in [-40, 40] with
  * the largest finite magnitude at most 448 * 2^e; larger finite values become
  * the largest code, infinities and NaN the code of NaN.  An append that

@@ -79,8 +79,8 @@ __device__ __forceinline__ Span span_of(const int32_t* span, int s, int pos0, in
 // The tokens' angles are computed once (LDS), reduced to a fraction of a turn in
 // double precision.  Thread c of a row takes four consecutive values; a key's
 // or value's stay in registers between the block's largest magnitude and their codes.
-// 2048 tokens of 48 heads of 128, 71 MB, take 22 us (3.2 TB/s), a token of 40 heads 5.3:
-// the bytes, and the double precision of keys.  In fp32 alone they took 20 and 4.6, and a
+// 2048 tokens of 48 heads of 128, 71 MB, take 22 us (3.2 TB/s), a token of them 5.1: the
+// bytes, and the double precision of keys, whose registers leave two waves a SIMD.  In fp32 alone they took 20 and 4.6, and a
 // few keys in a million got the code beside the nearest one.
 constexpr int append_threads(int D) { return D == 256 ? 512 : 256; }  // at most 8 passes of a row's threads over 64
 constexpr int kAppendGroups = 512;  // the work-groups that a call is cut into by heads
@@ -104,7 +104,7 @@ __device__ __forceinline__ double pair_turns(const AppendArgs& a, int i) {
 }
 
 // Cosine and sine of t turns times scale: the rest x to a quarter, in half turns, |x| <=
-// 1/4, and the series of both there, to 2^-33.  (Where a work-group has no keys: in fp32.)
+// 1/4, and the series of both there, to 2^-33.
 __device__ __forceinline__ double2 turn_of(double t, double scale) {
   const double q = rint(4.0 * t), x = fma(-0.5, q, 2.0 * t), y = x * x;
   double s = -0.007370430945714348, c = -0.02580689139001405;
@@ -135,11 +135,12 @@ __device__ __forceinline__ float to_odd(double d) {
 
 // One value of a turned pair: u c + w s, *t = (c, s), *rest what their rounding to fp32
 // left.  Keys in double precision (exact: a key's code is the nearest to the turned value,
-// not to its rounding to fp32), queries in fp32, as they go on as bf16.
+// not to its rounding to fp32), queries in fp32, as they go on as bf16, from the same
+// angles: a token's query does not depend on how its call is cut up.
 template <bool KEY>
 __device__ __forceinline__ float turned(float u, float w, const float2* t, const float2* rest) {
   const float2 c = *t;
-  if constexpr (!KEY) return u * c.x + w * c.y;
+  if constexpr (!KEY) return fmaf(u, c.x, w * c.y);
   const float2 r = *rest;
   return to_odd(u * (static_cast<double>(c.x) + r.x) + w * (static_cast<double>(c.y) + r.y));
 }
@@ -163,30 +164,18 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
   const int partner = (threadIdx.x & 63) + (first4 ? half / 4 : -(half / 4));  // of the same row
 
   float2* const rest_s = turn_s + min(a.T, kKvBlock) * half;
-  // heads hg, hg + groups, ...: keys, which take longest, are spread; without one the angles need no more than queries take
-  const int past = (a.Hq - hg) % groups, first_key = a.Hq + (past > 0 ? groups - past : -past);
-  const bool keys = first_key < a.Hq + a.Hkv;
-  const float scale = static_cast<float>(a.mscale);
-  if (half > 0 && (hg < a.Hq || keys)) {
+  if (half > 0 && hg < a.Hq + a.Hkv) {  // (its heads are hg, hg + groups, ...: keys, which take longest, are spread)
     int lanes = 1;  // pairs side by side: a power of two
     while (lanes < half) lanes *= 2;
     const int i = threadIdx.x % lanes;
     if (i < half) {
       const double f = pair_turns(a, i);
       for (int p = lo + static_cast<int>(threadIdx.x) / lanes; p < hi; p += THREADS / lanes) {
+        const double2 t = turn_of(p * f, a.mscale);
+        const float2 near = make_float2(static_cast<float>(t.x), static_cast<float>(t.y));
         const int at = (p - lo) * half + i;
-        if (keys) {
-          const double2 t = turn_of(p * f, a.mscale);
-          const float2 near = make_float2(static_cast<float>(t.x), static_cast<float>(t.y));
-          turn_s[at] = near;
-          rest_s[at] = make_float2(static_cast<float>(t.x - near.x), static_cast<float>(t.y - near.y));
-        } else {
-          double t = p * f;
-          t -= rint(t);
-          float s, c;
-          sincospif(2.0f * static_cast<float>(t), &s, &c);
-          turn_s[at] = make_float2(c * scale, s * scale);
-        }
+        turn_s[at] = near;
+        rest_s[at] = make_float2(static_cast<float>(t.x - near.x), static_cast<float>(t.y - near.y));
       }
     }
   }

@@ -727,3 +727,22 @@ def test_capped_scores_are_as_exact_as_their_size(S, Hq, Hkv, D, T, pos0, cap):
     """Capped scores of up to 1 whatever the cap: five roundings of the score and its cap, 2^-21, and tanh to 2^-20 of
     itself, beside the 2^-20 of uncapped ones.  Steps of 2^-22 of a cap of 128 would be 2^-15."""
     _check_cancelling(S, Hq, Hkv, D, T, pos0, 2.0 ** -20 + 2.0 ** -20 + 2.0 ** -21, softcap=cap)
+
+
+# --------------------------------------------------------- turned positions
+
+@pytest.mark.parametrize("Hq,Hkv,D,rot,inter,T,pos0", [(32, 8, 128, 128, False, 2048, 0), (16, 2, 256, 256, True, 3000, 70000),
+                                                       (24, 8, 64, 36, False, 1700, 1000000)])
+def test_queries_do_not_depend_on_how_a_call_is_cut(Hq, Hkv, D, rot, inter, T, pos0):
+    """A prompt, in which work-groups take heads of all kinds, and its tokens one at a time: the same queries, bit by bit."""
+    ms = _ms()
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    ctx = -(-(pos0 + T) // 64) * 64
+    cache, desc = ms.new_kv_cache_q(1, Hkv, D, ctx), ms.rope_desc(rot, 1e4, inter, 4.0, 8192, 1.0, 8.0, 1.1)
+    x = torch.empty(1, T, Hq + 2 * Hkv, D, device="cuda").normal_(generator=gen)
+    q, q1 = (torch.zeros(1, T, Hq, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ms.ms_rope_kv_q(cache, desc, x, T, Hq, pos0, q)
+    for t in range(T):
+        ms.ms_rope_kv_q(cache, desc, x[:, t], 1, Hq, pos0 + t, q1[:, t])
+    torch.cuda.synchronize()
+    assert torch.equal(q, q1)
