@@ -746,3 +746,91 @@ def test_queries_do_not_depend_on_how_a_call_is_cut(Hq, Hkv, D, rot, inter, T, p
         ms.ms_rope_kv_q(cache, desc, x[:, t], 1, Hq, pos0 + t, q1[:, t])
     torch.cuda.synchronize()
     assert torch.equal(q, q1)
+
+
+def _code_borders(x, pair):
+    """Whether x (of a unit scale) lies so near to the middle of two codes that a turn's 2^-30 of its pair's size may decide:
+    sine and cosine to 2^-33 and, at position 2^20, angles to 2^-32, on either side."""
+    a = np.abs(x)
+    step = np.exp2(np.floor(np.log2(np.maximum(a, 2.0 ** -6))) - 3)
+    return np.abs(a / step - np.floor(a / step) - 0.5) * step <= 2.0 ** -30 * pair
+
+
+# every width, layout and part of the head; one token, inside a block, several blocks
+# (the table of angles at its largest: 256 turned values, 64 tokens); far positions
+@pytest.mark.parametrize("D,rot,inter,T,pos0", [
+    (64, 64, False, 1, 100), (64, 20, False, 70, 30), (64, 64, True, 130, 1 << 20), (128, 128, False, 200, 77),
+    (128, 128, False, 64, (1 << 20) - 64), (128, 96, True, 1, 131000), (256, 256, False, 130, 0), (256, 256, True, 64, 64),
+    (256, 128, False, 3, 1 << 20)])
+@pytest.mark.parametrize("mscale", [1.0, 1.3])
+def test_turned_keys_have_the_nearest_codes(D, rot, inter, T, pos0, mscale):
+    """Keys whose first value of every pair turns to within an fp32 step of the middle of two codes."""
+    ms = _ms()
+    rng = np.random.default_rng(D + T)
+    H, half = 2, rot // 2
+    f = kv.frequencies(rot, 1e4, 4.0, 8192, 1.0, 8.0)
+    i = np.arange(half)
+    first, second = (2 * i, 2 * i + 1) if inter else (i, i + half)
+    y = np.zeros((T, H, D))
+    middle = (rng.integers(8, 16, (T, H, half)) + 0.5) * np.exp2(rng.integers(-6, 4, (T, H, half)))
+    y[..., first] = middle * rng.choice([-1, 1], middle.shape)
+    y[..., second] = rng.uniform(-440, 440, middle.shape)
+    y[..., second[0]] = 400.0  # every block's scale is 1
+    x = np.stack([kv.rope(y[t], -(pos0 + t), rot, f, inter, 1.0) for t in range(T)]) / mscale
+    qkv = np.zeros((1, T, 3 * H, D), np.float32)
+    qkv[0, :, H:2 * H] = x
+    x = qkv[0, :, H:2 * H].astype(np.float64)
+    turned = np.stack([kv.rope(x[t], pos0 + t, rot, f, inter, mscale) for t in range(T)])
+    ctx = -(-(pos0 + T) // 64) * 64
+    cache = ms.new_kv_cache_q(1, H, D, ctx)
+    cache.tensors[2].fill_(kv.BIAS - 20)
+    q = torch.empty(1, T, H, D, dtype=torch.bfloat16, device="cuda")
+    ms.ms_rope_kv_q(cache, ms.rope_desc(rot, 1e4, inter, 4.0, 8192, 1.0, 8.0, mscale), torch.from_numpy(qkv).cuda(), T, H, pos0, q)
+    torch.cuda.synchronize()
+    assert bool((cache.tensors[2][:, :, pos0 // 64:] == kv.BIAS).all())
+    got = cache.tensors[0][0, :, pos0:pos0 + T].cpu().numpy().transpose(1, 0, 2)
+    pair = np.zeros((T, H, D))
+    pair[..., first] = pair[..., second] = np.hypot(turned[..., first], turned[..., second])
+    near = _code_borders(turned, pair)
+    assert np.mean(near[..., first]) < 0.3
+    assert np.array_equal(kv.TABLE[got][~near], kv.TABLE[kv.encode(turned)][~near])
+
+
+# work-groups of two and three heads, head counts that their number does not divide, groups
+# of queries alone, with keys and with both of keys and values; appends from inside a
+# block on, and sequences of their own spans
+@pytest.mark.parametrize("S,Hq,Hkv,D,rot,inter,T,pos0,spans", [
+    (1, 24, 8, 64, 64, False, 1700, 37, None), (1, 16, 16, 64, 32, True, 2100, 0, None), (4, 15, 3, 128, 128, False, 1000, 60, None),
+    (8, 4, 2, 256, 256, False, 1020, 90, None), (3, 6, 2, 128, 44, False, 2500, 100, [(100, 2500), (63, 1111), (0, 2499)])])
+def test_append_of_many_heads_a_work_group(S, Hq, Hkv, D, rot, inter, T, pos0, spans):
+    ms = _ms()
+    rng = np.random.default_rng(T)
+    ctx = -(-(pos0 + T) // 64) * 64 + 64
+    ref = _random_cache(rng, S, Hkv, ctx, D)
+    cache = _cache(ref)
+    qkv = rng.standard_normal((S, T, Hq + 2 * Hkv, D)).astype(np.float32)
+    qkv *= np.exp2(rng.integers(-3, 4, (S, T, Hq + 2 * Hkv, 1))).astype(np.float32)
+    q = torch.full((S, T, Hq, D), -7.0, dtype=torch.bfloat16, device="cuda")
+    ms.ms_rope_kv_q(cache, ms.rope_desc(rot, 1e4, inter, 4.0, 8192, 1.0, 8.0, 1.25), torch.from_numpy(qkv).cuda(), T, Hq, pos0, q,
+                    None if spans is None else _span(spans))
+    torch.cuda.synchronize()
+    f = kv.frequencies(rot, 1e4, 4.0, 8192, 1.0, 8.0)
+    k, v, ke, ve = _host(cache)
+    qg = q.float().cpu().numpy()
+    for s in range(S):
+        start, n = (pos0, T) if spans is None else spans[s]
+        x = qkv[s, :n].astype(np.float64)
+        turned = np.stack([kv.rope(x[t, :Hq + Hkv], start + t, rot, f, inter, 1.25) for t in range(n)])
+        err = 2.0 ** -21 * 1.25 * np.abs(x[:, :Hq]).max(axis=-1, keepdims=True)
+        assert np.all(np.abs(qg[s, :n] - turned[:, :Hq]) <= 2.0 ** -8 * np.abs(turned[:, :Hq]) + err)
+        assert np.all(qg[s, n:] == -7.0)
+        ref.append(s, start, turned[:, Hq:], x[:, Hq + Hkv:])
+        assert np.array_equal(ke[s], ref.ke[s]) and np.array_equal(ve[s], ref.ve[s])
+        assert np.array_equal(v[s], ref.v[s])
+        differ = k[s] != ref.k[s]
+        if differ.any():  # only values next to the middle of two codes
+            h, p, c = np.nonzero(differ)
+            unit = np.exp2(ke[s, h, p // 64].astype(float) - kv.BIAS)
+            assert np.all((p >= start) & (p < start + n))
+            t = turned[p - start, Hq + h, c] / unit
+            assert np.all(_code_borders(t, 2 * np.abs(x[p - start, Hq + h]).max(axis=-1) / unit))
