@@ -80,8 +80,9 @@ __device__ __forceinline__ Span span_of(const int32_t* span, int s, int pos0, in
 // double precision.  Thread c of a row takes four consecutive values; a key's
 // or value's stay in registers between the block's largest magnitude and their codes.
 // 2048 tokens of 48 heads of 128, 71 MB, take 22 us (3.2 TB/s), a token of them 5.1: the
-// bytes, and the double precision of keys, whose registers leave two waves a SIMD.  In fp32 alone they took 20 and 4.6, and a
-// few keys in a million got the code beside the nearest one.
+// bytes, and the double precision of keys, whose registers leave two waves a SIMD.  In
+// fp32 alone they took 20 and 4.6, and a few keys in a million got the code beside the
+// nearest one.
 constexpr int append_threads(int D) { return D == 256 ? 512 : 256; }  // at most 8 passes of a row's threads over 64
 constexpr int kAppendGroups = 512;  // the work-groups that a call is cut into by heads
 
@@ -523,7 +524,6 @@ constexpr float kHuge = 16777216.0f;
 
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ msk::f32x4_t mfma_f16(f16x8_t a, f16x8_t b, msk::f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
