@@ -65,7 +65,11 @@ class Decoder:
             self.rope, self.opts = rope or ms.rope_desc(D, attn.rope_base), opts
             room = -(-max_ctx // ms.KV_BLOCK) * ms.KV_BLOCK
             self.kvq = [ms.new_kv_cache_q(1, Hkv, D, room) for _ in range(self.L)]
-            self.work = torch.empty(0, dtype=torch.uint8, device=dev)
+            # one workspace for all layers and steps: their calls follow each other on a stream, and no
+            # position needs more than the last one that T tokens may start at
+            need = max(ms.ms_attention_q_workspace(self.kvq[0], t, Hq, max_ctx - t)
+                       for t in range(1, min(max_tokens, max_ctx) + 1))
+            self.work = torch.empty(need, dtype=torch.uint8, device=dev)
         else:
             self.kc = torch.zeros(self.L, Hkv, max_ctx, D, dtype=bf, device=dev)
             self.vc = torch.zeros(self.L, Hkv, max_ctx, D, dtype=bf, device=dev)
@@ -113,11 +117,6 @@ class Decoder:
         d, V = self.shape.d_model, a.vocab
         pos0 = self.pos
         assert pos0 + T <= self.max_ctx and T <= self.max_tokens
-        if self.kv_bits == 8:
-            need = ms.ms_attention_q_workspace(self.kvq[0], T, a.n_heads, pos0)
-            if need > self.work.numel():  # one for all layers: their calls follow each other on the stream
-                stream.synchronize()
-                self.work = torch.empty(need, dtype=torch.uint8, device="cuda")
         cap = {}
         src = x0
 

@@ -587,7 +587,8 @@ typedef struct {
 } ms_attn_opts;
 
 /* Device bytes that ms_attention_q needs at workspace_dev for these sizes (0:
- * none), whatever the options and spans; pure host arithmetic. */
+ * none), whatever the options and spans; pure host arithmetic.  Never less for
+ * a larger pos0. */
 ms_status ms_attention_q_workspace(const ms_kv_cache_q* cache, int32_t T, int32_t Hq, int32_t pos0,
                                    uint64_t* bytes_out);
 

@@ -834,3 +834,29 @@ def test_append_of_many_heads_a_work_group(S, Hq, Hkv, D, rot, inter, T, pos0, s
             assert np.all((p >= start) & (p < start + n))
             t = turned[p - start, Hq + h, c] / unit
             assert np.all(_code_borders(t, 2 * np.abs(x[p - start, Hq + h]).max(axis=-1) / unit))
+
+
+# ------------------------------------------------------------ the decoder
+
+def test_decoder_steps_allocate_no_device_memory():
+    """Its workspace is there from the start and stays: prompts of odd sizes, then tokens past many shares of the context, on
+    a stream that is not the current one."""
+    from decoder import Decoder
+    from workload import top_bytes
+    ms = _ms()
+    shape, attn = synth.ModelShape("dec-tiny", 2, 256, 512, 8, 2, "bf16"), synth.TINY_ATTN
+    with Decoder(shape, attn, seed=4, n_sets=2, max_tokens=400, max_ctx=3000, budget_total=2 * 8 * shape.expert_bytes,
+                 keep_f32=False, kv_bits=8) as dec:
+        work = dec.work
+        assert work.numel() >= max(ms.ms_attention_q_workspace(dec.kvq[0], T, attn.n_heads, 3000 - T) for T in (1, 7, 40, 399))
+        assert work.numel() > 0
+        dec.stack.configure(0.5, 2 * 4 * top_bytes(dec.stack.rig, 0.5))
+        stream = torch.cuda.Stream()
+        x = torch.randn(400, shape.d_model, device="cuda").to(torch.bfloat16)
+        torch.cuda.synchronize()
+        dec.step(x, 400, stream=stream)
+        before = torch.cuda.memory_stats()["allocation.all.allocated"]
+        for T in [1] * 70 + [399, 40, 7] + [1] * 70 + [400] * 4 + [1] * 9:
+            dec.step(x, T, stream=stream)
+        stream.synchronize()
+        assert torch.cuda.memory_stats()["allocation.all.allocated"] == before and dec.work is work

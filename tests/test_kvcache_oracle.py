@@ -185,3 +185,16 @@ def test_cache_shapes_are_checked_by_the_binding():
     for fn, args in ((ms.ms_rope_kv_q, (c, _rope(), 4096, 1, 3, 0, 4096)), (ms.ms_attention_q, (c, 4096, 1, 3, 0, 4096, None))):
         with pytest.raises(ValueError):
             fn(*args, span=torch.tensor([[0, 1], [0, 1]]))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("S,H,G", [(1, 1, 1), (1, 8, 4), (1, 2, 8), (3, 5, 3), (32, 8, 8), (70, 4, 1)])
+def test_no_position_needs_a_smaller_workspace_than_one_before(S, H, G, D):
+    """So the last position that T tokens may start at tells what a decode ever needs."""
+    from paper_2509_08342_amd import moesplit as ms
+    c = _cache(S=S, H=H, D=D, ctx=1 << 17)
+    for T in (1, 2, 5, 16, 17, 40, 129, 500, 2048):
+        if S * T * H * G <= 1 << 22:
+            sizes = [ms.ms_attention_q_workspace(c, T, H * G, p) for p in [*range(0, 9000, 64), *range(9000, (1 << 17) - T, 1009)]]
+            assert all(a <= b for a, b in zip(sizes, sizes[1:])), T
+            assert sizes[-1] > 0 or S * H > 256 or T > 1
