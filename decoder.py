@@ -15,8 +15,8 @@ first layer's window, T_head + T_att).
 
 kv_bits=8 keeps the key/value caches in 8 bits (ms_rope_kv_q,
 ms_attention_q): half the bytes, which the VRAM budget can give to experts,
-any context length, stretched positions (rope) and attention options
-(opts)."""
+any context length, stretched positions (rope) and attention options (opts;
+documents [1][max_ctx rounded up to a multiple of 64])."""
 from __future__ import annotations
 
 import time

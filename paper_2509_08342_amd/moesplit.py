@@ -460,20 +460,37 @@ def _ref(x):
     return None if x is None else ctypes.byref(x)
 
 
-def _span(x):
-    if x is not None and str(getattr(x, "dtype", "torch.int32")) != "torch.int32":
-        raise ValueError("span: torch.int32 expected")
+def _span(x, cache):
+    if x is not None:
+        if str(getattr(x, "dtype", "torch.int32")) != "torch.int32":
+            raise ValueError("span: torch.int32 expected")
+        if cache is not None and getattr(x, "shape", None) not in (None, (cache.n_seqs, 2)):
+            raise ValueError("span: [%d][2] expected" % cache.n_seqs)
+    return _ptr(x)
+
+
+def _rows(x, name, size, cache, rows):
+    """x's address; a tensor holds at least n_seqs * rows * head_dim numbers of `size` bytes, in whatever shape."""
+    held = getattr(x, "nbytes", None)
+    if held is not None and cache is not None:
+        values = cache.n_seqs * rows * cache.head_dim
+        if held < values * size or x.itemsize != size:
+            raise ValueError("%s: %d values of %d bytes expected" % (name, values, size))
     return _ptr(x)
 
 
 def ms_rope_kv_q(cache, rope, qkv, T, Hq, pos0, q_out, span=None, stream=None):
-    st = lib.ms_rope_kv_q(_ref(cache), _ref(rope), _ptr(qkv), T, Hq, pos0, _span(span), _ptr(q_out), _stream(stream))
+    heads = Hq + 2 * cache.n_kv_heads if cache is not None else 0
+    st = lib.ms_rope_kv_q(_ref(cache), _ref(rope), _rows(qkv, "qkv", 4, cache, T * heads), T, Hq, pos0, _span(span, cache),
+                          _rows(q_out, "q_out", 2, cache, T * Hq), _stream(stream))
     if st:
         _check(st, what="ms_rope_kv_q")
 
 
 def ms_kv_read_q(cache, pos0, n, k_out, v_out, stream=None):
-    st = lib.ms_kv_read_q(_ref(cache), pos0, n, _ptr(k_out), _ptr(v_out), _stream(stream))
+    rows = n * cache.n_kv_heads if cache is not None else 0
+    st = lib.ms_kv_read_q(_ref(cache), pos0, n, _rows(k_out, "k_out", 2, cache, rows), _rows(v_out, "v_out", 2, cache, rows),
+                          _stream(stream))
     if st:
         _check(st, what="ms_kv_read_q")
 
@@ -486,7 +503,14 @@ def ms_attention_q_workspace(cache, T, Hq, pos0):
 
 def ms_attention_q(cache, q, T, Hq, pos0, out, workspace=None, opts=None, span=None, stream=None):
     """workspace: a device tensor of at least ms_attention_q_workspace bytes."""
-    st = lib.ms_attention_q(_ref(cache), _ptr(q), T, Hq, pos0, _span(span), _ref(opts), _ptr(out), _ptr(workspace),
-                            0 if workspace is None else workspace.nbytes, _stream(stream))
+    if opts is not None and cache is not None:
+        slopes, doc = getattr(opts, "tensors", (None, None))
+        if slopes is not None and getattr(slopes, "shape", None) not in (None, (Hq,)):
+            raise ValueError("attn_opts: slopes of %r expected" % ((Hq,),))
+        if doc is not None and getattr(doc, "shape", None) not in (None, (cache.n_seqs, cache.max_ctx)):
+            raise ValueError("attn_opts: doc of %r expected" % ((cache.n_seqs, cache.max_ctx),))
+    st = lib.ms_attention_q(_ref(cache), _rows(q, "q", 2, cache, T * Hq), T, Hq, pos0, _span(span, cache), _ref(opts),
+                            _rows(out, "out", 2, cache, T * Hq), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
+                            _stream(stream))
     if st:
         _check(st, what="ms_attention_q")

@@ -198,3 +198,37 @@ def test_no_position_needs_a_smaller_workspace_than_one_before(S, H, G, D):
             sizes = [ms.ms_attention_q_workspace(c, T, H * G, p) for p in [*range(0, 9000, 64), *range(9000, (1 << 17) - T, 1009)]]
             assert all(a <= b for a, b in zip(sizes, sizes[1:])), T
             assert sizes[-1] > 0 or S * H > 256 or T > 1
+
+
+def test_tensor_shapes_are_checked_by_the_binding():
+    """A kernel would read or write past a tensor that is too small, or other sequences' numbers of one laid out otherwise."""
+    torch = pytest.importorskip("torch")
+    from paper_2509_08342_amd import moesplit as ms
+    S, Hq, Hkv, D, ctx, T = 2, 6, 3, 64, 128, 3
+    c = ms.new_kv_cache_q(S, Hkv, D, ctx, device="cpu")
+
+    def t(*shape, dtype=torch.bfloat16):
+        return torch.zeros(*shape, dtype=dtype)
+
+    qkv, q = t(S, T, Hq + 2 * Hkv, D, dtype=torch.float32), t(S, T, Hq, D)
+    short = q.flatten()[:-1]
+    for args in [(qkv.flatten()[:-1], T, Hq, 0, q), (qkv, T, Hq, 0, short), (qkv.to(torch.bfloat16), T, Hq, 0, q),
+                 (qkv, T, Hq, 0, qkv)]:
+        with pytest.raises(ValueError):
+            ms.ms_rope_kv_q(c, _rope(), *args)
+    k = t(S, Hkv, 70, D)
+    for args in [(0, 71, k, k), (0, 70, k, k[:, :, :69].contiguous()), (0, 70, k.float(), k)]:
+        with pytest.raises(ValueError):
+            ms.ms_kv_read_q(c, *args)
+    for args in [(q, T + 1, Hq, 0, q), (q, T, Hq, 0, short), (q.float(), T, Hq, 0, q), (q, T, Hq, 0, q.float())]:
+        with pytest.raises(ValueError):
+            ms.ms_attention_q(c, *args)
+    for span in (t(S, 3, dtype=torch.int32), t(S - 1, 2, dtype=torch.int32), t(2 * S, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            ms.ms_attention_q(c, q, T, Hq, 0, q, span=span)
+        with pytest.raises(ValueError):
+            ms.ms_rope_kv_q(c, _rope(), qkv, T, Hq, 0, q, span=span)
+    for opts in (dict(doc=t(S, T, dtype=torch.int32)), dict(doc=t(ctx, dtype=torch.int32)), dict(doc=t(1, ctx, dtype=torch.int32)),
+                 dict(slopes=t(Hkv, dtype=torch.float32))):
+        with pytest.raises(ValueError):
+            ms.ms_attention_q(c, q, T, Hq, 0, q, opts=ms.attn_opts(**opts))
