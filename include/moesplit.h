@@ -528,11 +528,11 @@ typedef struct {
 /* Rotary positions.  The first rot_dim (even, 0 .. head_dim) values of a head
  * turn in pairs (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved; the
  * rest stays.  Pair i turns by p f'_i at position p, cosine and sine times
- * mscale (> 0; 1 where nothing is stretched).  f_i = base^(-2 i / rot_dim),
- * base > 1.  factor >= 1 stretches positions: f'_i = f_i / factor if orig_ctx
- * is 0, else f'_i = f_i ((1 - g) / factor + g) with g the position of the
- * turns that pair i makes in the original context, orig_ctx f_i / (2 pi),
- * between low and high (0 <= low < high; 0 below, 1 above). */
+ * mscale (> 0, within fp32; 1 where nothing is stretched).  f_i =
+ * base^(-2 i / rot_dim), base > 1.  factor >= 1 stretches positions: f'_i = f_i
+ * / factor if orig_ctx is 0, else f'_i = f_i ((1 - g) / factor + g) with g the
+ * position of the turns that pair i makes in the original context, orig_ctx
+ * f_i / (2 pi), between low and high (0 <= low < high; 0 below, 1 above). */
 typedef struct {
   double base;
   double factor;

@@ -1452,7 +1452,8 @@ ms_status ms_rope_kv_q(const ms_kv_cache_q* cache, const ms_rope_desc* rope, con
   const int Hkv = cache->n_kv_heads, D = cache->head_dim;
   if (!rope || T < 0 || Hq <= 0 || Hq % Hkv != 0 || pos0 < 0) return MS_E_INVALID;
   if (!(rope->base > 1.0) || !std::isfinite(rope->base) || !(rope->factor >= 1.0) || !std::isfinite(rope->factor) ||
-      !(rope->orig_ctx >= 0.0) || !std::isfinite(rope->orig_ctx) || !(rope->mscale > 0.0) || !std::isfinite(rope->mscale) ||
+      !(rope->orig_ctx >= 0.0) || !std::isfinite(rope->orig_ctx) || !(rope->mscale > 0.0) ||
+      !std::isfinite(static_cast<float>(rope->mscale)) ||
       rope->rot_dim < 0 || rope->rot_dim > D || rope->rot_dim % 2 != 0)
     return MS_E_INVALID;
   if (rope->orig_ctx > 0.0 && (!(rope->low >= 0.0) || !(rope->high > rope->low) || !std::isfinite(rope->high)))

@@ -232,3 +232,10 @@ def test_tensor_shapes_are_checked_by_the_binding():
                  dict(slopes=t(Hkv, dtype=torch.float32))):
         with pytest.raises(ValueError):
             ms.ms_attention_q(c, q, T, Hq, 0, q, opts=ms.attn_opts(**opts))
+
+
+@pytest.mark.parametrize("mscale", [3.5e38, 1e300])
+def test_scales_of_cosine_and_sine_past_fp32_are_refused(mscale):
+    """Sines that are infinite in fp32 would make NaN of finite values."""
+    from paper_2509_08342_amd import moesplit as ms
+    assert _status(ms.ms_rope_kv_q, _cache(), _rope(mscale=mscale), 4096, 1, 4, 0, 4096) == ms.MS_E_INVALID
