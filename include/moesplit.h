@@ -570,7 +570,7 @@ ms_status ms_kv_read_q(const ms_kv_cache_q* cache, int32_t pos0, int32_t n, void
 /* What a score and the set of visible keys may have beside the causal order.
  * Zero or NULL in a field: without.  For the query at position i and the key
  * at position j of one sequence:
- *   s = scale q.k (scale 0: 1 / sqrt(head_dim)); s = softcap tanh(s / softcap);
+ *   s = scale q.k (scale up to 2e38, 0: 1 / sqrt(head_dim)); s = softcap tanh(s / softcap);
  *   s = s - slopes_dev[query head] |i - j| (device fp32 [Hq]);
  *   the key is seen if j <= i and i - j < window, or if j < prefix (earlier
  *   and later queries alike), as far as the sequence has keys (its last token

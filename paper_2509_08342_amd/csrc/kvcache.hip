@@ -1544,7 +1544,7 @@ ms_status ms_attention_q(const ms_kv_cache_q* cache, const void* q, int32_t T, i
                          uint64_t workspace_bytes, void* stream) {
   uint64_t need = 0;
   if (const ms_status st = ms_attention_q_workspace(cache, T, Hq, pos0, &need); st != MS_OK) return st;
-  if (opts && (!(opts->scale >= 0.0f) || !std::isfinite(opts->scale) || !(opts->softcap >= 0.0f) ||
+  if (opts && (!(opts->scale >= 0.0f) || !std::isfinite(opts->scale * kLog2e) || !(opts->softcap >= 0.0f) ||
                !std::isfinite(opts->softcap) || opts->window < 0 || opts->prefix < 0 || !aligned16(opts->docs_dev)))
     return MS_E_INVALID;
   if (T == 0) return MS_OK;

@@ -836,6 +836,19 @@ def test_append_of_many_heads_a_work_group(S, Hq, Hkv, D, rot, inter, T, pos0, s
             assert np.all(_code_borders(t, 2 * np.abs(x[p - start, Hq + h]).max(axis=-1) / unit))
 
 
+@pytest.mark.parametrize("T,pos0", [(1, 300), (40, 100)])
+@pytest.mark.parametrize("scale", [1e-40, 2e38])
+@pytest.mark.parametrize("size", [0.0, 2.0 ** -124])
+def test_scales_at_the_ends_of_fp32(T, pos0, scale, size):
+    """The largest scale is as good as any for queries that are small enough, zeros among them; so is one below the least
+    normal number."""
+    rng = np.random.default_rng(T)
+    ref = _random_cache(rng, 1, 2, 192 if T == 40 else 320, 64)
+    q, qf = _bf16(size * rng.integers(-2, 3, (1, T, 4, 64)))
+    got = _run(_cache(ref), q, T, 4, pos0, _ms().attn_opts(scale=scale)).float().cpu().numpy()
+    _check(ref, qf, got, pos0, None, scale=scale)
+
+
 # ------------------------------------------------------------ the decoder
 
 def test_decoder_steps_allocate_no_device_memory():

@@ -239,3 +239,9 @@ def test_scales_of_cosine_and_sine_past_fp32_are_refused(mscale):
     """Sines that are infinite in fp32 would make NaN of finite values."""
     from paper_2509_08342_amd import moesplit as ms
     assert _status(ms.ms_rope_kv_q, _cache(), _rope(mscale=mscale), 4096, 1, 4, 0, 4096) == ms.MS_E_INVALID
+
+
+def test_scales_that_pass_fp32_in_powers_of_two_are_refused():
+    """exp(scale x) is taken as 2^(scale log2(e) x): an infinite factor would make NaN of a product of zero."""
+    from paper_2509_08342_amd import moesplit as ms
+    assert _status(lambda: ms.ms_attention_q(_cache(), 4096, 1, 4, 0, 1 << 20, None, ms.attn_opts(scale=3e38))) == ms.MS_E_INVALID
