@@ -456,61 +456,56 @@ def attn_opts(scale=0.0, softcap=0.0, window=0, prefix=0, slopes=None, doc=None)
     return o
 
 
-def _ref(x):
-    return None if x is None else ctypes.byref(x)
-
-
 def _span(x, cache):
-    if x is not None:
-        if str(getattr(x, "dtype", "torch.int32")) != "torch.int32":
-            raise ValueError("span: torch.int32 expected")
-        if cache is not None and getattr(x, "shape", None) not in (None, (cache.n_seqs, 2)):
-            raise ValueError("span: [%d][2] expected" % cache.n_seqs)
+    if str(getattr(x, "dtype", "torch.int32")) != "torch.int32":
+        raise ValueError("span: torch.int32 expected")
+    if cache is not None and getattr(x, "shape", None) not in (None, (cache.n_seqs, 2)):
+        raise ValueError("span: [%d][2] expected" % cache.n_seqs)
     return _ptr(x)
 
 
-def _rows(x, name, size, cache, rows):
-    """x's address; a tensor holds at least n_seqs * rows * head_dim numbers of `size` bytes, in whatever shape."""
-    held = getattr(x, "nbytes", None)
-    if held is not None and cache is not None:
-        values = cache.n_seqs * rows * cache.head_dim
-        if held < values * size or x.itemsize != size:
-            raise ValueError("%s: %d values of %d bytes expected" % (name, values, size))
-    return _ptr(x)
+def _rows(x, name, size, values):
+    """x's address; a tensor is contiguous and holds at least `values` numbers of `size` bytes, in whatever shape."""
+    try:
+        if x.nbytes >= values * size and x.itemsize == size and x.is_contiguous():
+            return x.data_ptr()
+    except AttributeError:  # an address
+        return _ptr(x)
+    raise ValueError("%s: %d contiguous values of %d bytes expected" % (name, values, size))
 
 
 def ms_rope_kv_q(cache, rope, qkv, T, Hq, pos0, q_out, span=None, stream=None):
-    heads = Hq + 2 * cache.n_kv_heads if cache is not None else 0
-    st = lib.ms_rope_kv_q(_ref(cache), _ref(rope), _rows(qkv, "qkv", 4, cache, T * heads), T, Hq, pos0, _span(span, cache),
-                          _rows(q_out, "q_out", 2, cache, T * Hq), _stream(stream))
+    n, kv = (cache.n_seqs * T * cache.head_dim, 2 * cache.n_kv_heads) if cache is not None else (0, 0)
+    st = lib.ms_rope_kv_q(cache, rope, _rows(qkv, "qkv", 4, n * (Hq + kv)), T, Hq, pos0,
+                          None if span is None else _span(span, cache), _rows(q_out, "q_out", 2, n * Hq), _stream(stream))
     if st:
         _check(st, what="ms_rope_kv_q")
 
 
 def ms_kv_read_q(cache, pos0, n, k_out, v_out, stream=None):
-    rows = n * cache.n_kv_heads if cache is not None else 0
-    st = lib.ms_kv_read_q(_ref(cache), pos0, n, _rows(k_out, "k_out", 2, cache, rows), _rows(v_out, "v_out", 2, cache, rows),
-                          _stream(stream))
+    values = cache.n_seqs * n * cache.head_dim * cache.n_kv_heads if cache is not None else 0
+    st = lib.ms_kv_read_q(cache, pos0, n, _rows(k_out, "k_out", 2, values), _rows(v_out, "v_out", 2, values), _stream(stream))
     if st:
         _check(st, what="ms_kv_read_q")
 
 
 def ms_attention_q_workspace(cache, T, Hq, pos0):
     n = ctypes.c_uint64()
-    _check(lib.ms_attention_q_workspace(_ref(cache), T, Hq, pos0, ctypes.byref(n)), what="ms_attention_q_workspace")
+    _check(lib.ms_attention_q_workspace(cache, T, Hq, pos0, ctypes.byref(n)), what="ms_attention_q_workspace")
     return n.value
 
 
 def ms_attention_q(cache, q, T, Hq, pos0, out, workspace=None, opts=None, span=None, stream=None):
     """workspace: a device tensor of at least ms_attention_q_workspace bytes."""
+    n = cache.n_seqs * T * cache.head_dim * Hq if cache is not None else 0
     if opts is not None and cache is not None:
         slopes, doc = getattr(opts, "tensors", (None, None))
         if slopes is not None and getattr(slopes, "shape", None) not in (None, (Hq,)):
             raise ValueError("attn_opts: slopes of %r expected" % ((Hq,),))
         if doc is not None and getattr(doc, "shape", None) not in (None, (cache.n_seqs, cache.max_ctx)):
             raise ValueError("attn_opts: doc of %r expected" % ((cache.n_seqs, cache.max_ctx),))
-    st = lib.ms_attention_q(_ref(cache), _rows(q, "q", 2, cache, T * Hq), T, Hq, pos0, _span(span, cache), _ref(opts),
-                            _rows(out, "out", 2, cache, T * Hq), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
+    st = lib.ms_attention_q(cache, _rows(q, "q", 2, n), T, Hq, pos0, None if span is None else _span(span, cache), opts,
+                            _rows(out, "out", 2, n), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
                             _stream(stream))
     if st:
         _check(st, what="ms_attention_q")
