@@ -245,3 +245,17 @@ def test_scales_that_pass_fp32_in_powers_of_two_are_refused():
     """exp(scale x) is taken as 2^(scale log2(e) x): an infinite factor would make NaN of a product of zero."""
     from paper_2509_08342_amd import moesplit as ms
     assert _status(lambda: ms.ms_attention_q(_cache(), 4096, 1, 4, 0, 1 << 20, None, ms.attn_opts(scale=3e38))) == ms.MS_E_INVALID
+
+
+def test_workspace_sizes_and_what_they_guard():
+    """A result, an exponent and a sum for every row and share: 64 shares of a token behind 2^20 positions of one head, none
+    for a call that fills the chip; and a workspace that is smaller, missing or not aligned is refused."""
+    from paper_2509_08342_amd import moesplit as ms
+    c = _cache(S=1, H=1, ctx=1 << 20)
+    n = ms.ms_attention_q_workspace(c, 1, 4, (1 << 20) - 1)
+    assert n == 4 * 64 * (64 + 2) * 4
+    call = lambda size, at: ms._check(ms.lib.ms_attention_q(  # noqa: E731
+        ctypes.byref(c), 4096, 1, 4, (1 << 20) - 1, None, None, 1 << 20, at, size, None))
+    for size, at in ((n - 1, 1 << 30), (0, 1 << 30), (n, None), (n, (1 << 30) + 8)):
+        assert _status(call, size, at) == ms.MS_E_INVALID
+    assert ms.ms_attention_q_workspace(_cache(S=1 << 12, H=1, ctx=2048), 1024, 1, 0) == 0
