@@ -1413,9 +1413,9 @@ ms_status launch_attention_q(const AttArgs& a, const Plan& p, bool mods, hipStre
   if (p.splits > 1) {
     const int rows = a.heads * a.T * a.G;
     if (rows >= kJoinManyRows)
-      hipLaunchKernelGGL((attention_q_join_kernel<D, 1>), dim3((rows + 3) / 4), dim3(kJoinThreads), 0, s, a, rows);
+      hipLaunchKernelGGL((attention_q_join_kernel<D, 1>), dim3((rows + 3) / 4), dim3(kJoinThreads), msk::kGuardLds, s, a, rows);
     else
-      hipLaunchKernelGGL((attention_q_join_kernel<D, 4>), dim3(rows), dim3(kJoinThreads), 0, s, a, rows);
+      hipLaunchKernelGGL((attention_q_join_kernel<D, 4>), dim3(rows), dim3(kJoinThreads), msk::kGuardLds, s, a, rows);
   }
   return hipGetLastError() == hipSuccess ? MS_OK : MS_E_HIP;
 }

@@ -259,3 +259,14 @@ def test_workspace_sizes_and_what_they_guard():
     for size, at in ((n - 1, 1 << 30), (0, 1 << 30), (n, None), (n, (1 << 30) + 8)):
         assert _status(call, size, at) == ms.MS_E_INVALID
     assert ms.ms_attention_q_workspace(_cache(S=1 << 12, H=1, ctx=2048), 1024, 1, 0) == 0
+
+
+def test_every_launch_asks_for_lds():
+    """A work-group without LDS may land on the compute units that copies of experts hold, and waits behind their reads."""
+    import os
+    import re
+    import paper_2509_08342_amd
+    text = open(os.path.join(os.path.dirname(paper_2509_08342_amd.__file__), "csrc", "kvcache.hip")).read()
+    lds = [re.split(r",(?![^(<]*[)>])", re.sub(r"\s+", " ", call))[3].strip()
+           for call in re.findall(r"hipLaunchKernelGGL\((.*?)\);", text, re.S)]
+    assert len(lds) == text.count("hipLaunchKernelGGL(") and set(lds) <= {"lds", "tile_lds(D)", "msk::kGuardLds"}, lds
