@@ -576,7 +576,11 @@ ms_status ms_kv_read_q(const ms_kv_cache_q* cache, int32_t pos0, int32_t n, void
  *   and later queries alike), as far as the sequence has keys (its last token
  *   of this call included), and, with docs_dev (device int32
  *   [n_seqs][max_ctx], 16-byte aligned), only if docs_dev[i] == docs_dev[j] >= 0.
- * A query that sees no key (a negative docs_dev[i]) gives zeros. */
+ * A query that sees no key (a negative docs_dev[i]) gives zeros.
+ *   A prefix is seen both ways, so its tokens belong into one call: cut up, its
+ * first queries would see fewer keys.  It is not the kept first tokens of a
+ * causal window, whose own queries see no later key.  It counts from position
+ * 0: with docs_dev only the documents that reach into it have one. */
 typedef struct {
   float scale;
   float softcap;
@@ -603,7 +607,9 @@ ms_status ms_attention_q_workspace(const ms_kv_cache_q* cache, int32_t T, int32_
  * workspace_dev: 16-byte aligned, at least ms_attention_q_workspace bytes,
  * used until the call has finished on `stream`; calls that may overlap in
  * time need one each.  What masked keys and values hold (NaN included) does
- * not reach a query. */
+ * not reach a query.  How many work-groups share a context follows pos0: a graph
+ * captured with the largest pos0 gives the short contexts that it replays later
+ * one or two. */
 ms_status ms_attention_q(const ms_kv_cache_q* cache, const void* q, int32_t T, int32_t Hq, int32_t pos0,
                          const int32_t* span_dev, const ms_attn_opts* opts, void* out, void* workspace_dev,
                          uint64_t workspace_bytes, void* stream);

@@ -287,8 +287,8 @@ __global__ __launch_bounds__(append_threads(D)) void rope_kv_q_kernel(AppendArgs
 
 // ------------------------------------------------------------- read back
 //
-// 16 codes per thread.  Bound by the bytes written; 2048 positions of 8 heads of 128
-// (13 MB) take 4.8 to 5.5 us, one position 2.6.
+// 16 codes per thread.  Half its start and end, half its bytes: 2048 positions of 8 heads
+// of 128 (12.6 MB, 2.7 us at a copy's rate) take 4.8 to 5.5 us, one position 2.6.
 constexpr int kReadThreads = 256;
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -501,8 +501,8 @@ __device__ __forceinline__ void attend_row(const AttArgs& a, int head, const Spa
 // value block's 2^ev goes into the probability's exponent.  A probability enters as two
 // fp16 parts, rounded and the rest rounded, 22 bits or more together: one would be off by
 // up to 2^-11, more than all the fp32 steps before it.  The second part's products and
-// sums cost nothing where the bytes bound the kernel and a fifth to a third of a prompt
-// (2048 tokens 52.7 -> 63.6 us, 512 behind 32256 271 -> 351).
+// sums cost nothing where the bytes bound the kernel and a tenth to a third of a prompt
+// (2048 tokens 52.7 -> 63.6 us, 512 behind 32256 271 -> 351, packed documents 68 -> 75).
 //
 // A score's exponent is y = c S, c = mul 2^ek.  A row keeps its sum l = sum 2^(y - L) and O = sum
 // 2^(y + ev - A) code; L and A are whole numbers, so that c S + ev - A is one fma
@@ -966,12 +966,12 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
 // its share of the tiles of 64 keys.  Codes come to LDS by direct loads, a tile
 // ahead, and become operands when a wave reads them, as above: the conversions
 // run beside the matrix instructions, and LDS holds and moves a byte per value.
-//   Bound by the issue of vector and matrix instructions (some 300 and 68 a wave and
-// tile of 32 rows): 512 tokens behind 32256, 32 heads over 8 of 128, take 275 us, 1.0
-// PFLOP/s of products; 2048 behind none 52, the 32 tiles of the longest block one after
-// another.  Tiles converted once by all waves and kept in LDS as 16-bit values were
-// slower, as were two groups of four waves with a share of the keys each (357 us for
-// 338 of 2048 tokens behind 8192).
+//   Bound by the issue of vector and matrix instructions (311 and 104 a wave and tile of
+// 32 rows): 512 tokens behind 32256, 32 heads over 8 of 128, take 351 to 361 us, 0.78
+// PFLOP/s of products (1.2 with the probabilities' second parts); 2048 behind none 64, the
+// 32 tiles of the longest block one after another.  Tiles converted once by all waves and
+// kept in LDS as 16-bit values were slower, as were two groups of four waves with a share
+// of the keys each (357 us for 338 of 2048 tokens behind 8192, probabilities in one part).
 constexpr int kTileWaves = 4;
 constexpr size_t tile_lds(int D) { return size_t{4} * kKvBlock * D; }  // two stages of keys and values
 
@@ -1361,8 +1361,9 @@ struct Plan {
 // 1500 11.4 and 9.5; 16 over 4 of 256 at 400 14.0 and 13.8, at 700 17.3 and 14.2.
 //   More: row blocks of 128 (more matrix instructions to a converted code) if their
 // work-groups, with shares of sixteen tiles or more on average, fill the chip twice
-// over, else of 64: 2048 tokens behind 8192, 32 heads over 8 of 128, 315 and 384 us; 512
-// behind 4096 58.7 and 67.7; but 1024 behind none 29 and 21.4, and 100 6.7 against 9.6.
+// over, else of 64: 2048 tokens behind 8192, 32 heads over 8 of 128, 403 and 462 us; 512
+// behind 4096 68.3 and 76.1; 4096 behind none 186 and 204; but 2048 behind none 64.0 and
+// 59.2, 1024 32.6 and 23.5, and 100 10.1 and 7.5.
 Plan plan_of(int64_t heads, int T, int G, int D, int pos0, bool spans, int window, int prefix) {
   Plan p;
   const int64_t rows = static_cast<int64_t>(T) * G;
@@ -1488,7 +1489,8 @@ ms_status ms_rope_kv_q(const ms_kv_cache_q* cache, const ms_rope_desc* rope, con
   if (heads > INT32_MAX) return MS_E_UNSUPPORTED;
   // heads that share a work-group's angles: as many as leave kAppendGroups work-groups, two
   // per compute unit.  2048 tokens of 48 heads: 28.1 us with 256, 22.0 with 512, 31.1 with
-  // 1024; 16 pieces of 41 tokens 13.4, 9.7, 13.0
+  // 1024; 16 pieces of 41 tokens 13.4, 9.7, 13.0.  (Heads of 128, all of them turned: LDS
+  // admits two there, more where heads are narrower or turned in part.)
   const int64_t all = heads * a.blocks;  // at most 2^31 * 2^26; in steps, so that no product passes 64 bits
   const int threads = append_threads(D);
   if (all > UINT32_MAX / threads || all * cache->n_seqs > UINT32_MAX / threads) return MS_E_UNSUPPORTED;
