@@ -356,19 +356,18 @@ __device__ __forceinline__ Tiles tiles_of(const AttArgs& a, int p0, int p1, int 
   return t;
 }
 
-// tanh.  Up to kSeries in size its series, off by less than 2^-22 of itself.
+// tanh, off by less than 2^-20 of itself.  Up to kSeries in size its series, off by 2^-22;
+// above, where 1 - e does not cancel, the exponential's form.
 constexpr float kSeries = 0.25f;
 __device__ __forceinline__ float tanh_series(float x) {
   const float y = x * x;
   return x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
 }
-// Off by less than 2^-20 of itself from kSeries on, and by 2^-25 near zero, where the
-// exponential is nearly 1.
-__device__ __forceinline__ float tanh_exp(float x) {
+__device__ __forceinline__ float tanh_of(float x) {
   const float e = __builtin_amdgcn_exp2f(fabsf(x) * (-2.0f * kLog2e));
-  return copysignf((1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e), x);
+  const float far = (1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e);
+  return fabsf(x) < kSeries ? tanh_series(x) : copysignf(far, x);
 }
-__device__ __forceinline__ float tanh_of(float x) { return fabsf(x) < kSeries ? tanh_series(x) : tanh_exp(x); }
 
 // Whether the query at position i sees key j of n (document di, dj).
 __device__ __forceinline__ bool sees(const AttArgs& a, int i, int j, int n, int di, int dj) {
@@ -689,9 +688,9 @@ __device__ __forceinline__ void modify(const AttArgs& a, const Row& w, int k0, i
   if (a.scores) {
     float f = ks * a.pre;
     if (a.cap > 0.0f) {
-      // Where all of a wave's scores are far below the cap, none is rounded to steps of the
-      // cap's; else 2^-25 of the cap is as small as the largest one's own rounding.  (2048
-      // tokens behind 8192, 16 heads of 128 over 2: 354 and 402 us; 259 without a cap.)
+      // Where all of a wave's scores are far below the cap, no exponential: 2048 tokens
+      // behind 8192, 16 heads of 128 over 2, take 354 us, else 478 (261 without a cap).  Either
+      // way a score has the same value, whatever the others of its wave, masked ones too.
       f *= 1.0f / a.cap;
       float top = 0.0f;
 #pragma unroll
@@ -705,7 +704,7 @@ __device__ __forceinline__ void modify(const AttArgs& a, const Row& w, int k0, i
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) S[b][r] = a.cap * tanh_exp(S[b][r]);
+          for (int r = 0; r < 4; ++r) S[b][r] = a.cap * tanh_of(S[b][r]);
       } else {
 #pragma unroll
         for (int b = 0; b < NB; ++b)

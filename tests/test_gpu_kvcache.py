@@ -729,6 +729,26 @@ def test_capped_scores_are_as_exact_as_their_size(S, Hq, Hkv, D, T, pos0, cap):
     _check_cancelling(S, Hq, Hkv, D, T, pos0, 2.0 ** -20 + 2.0 ** -20 + 2.0 ** -21, softcap=cap)
 
 
+@pytest.mark.parametrize("S,Hq,Hkv,D,T,pos0", [(2, 4, 2, 64, 1, 700), (1, 8, 2, 128, 3, 1000), (1, 8, 2, 128, 150, 260),
+                                               (1, 8, 1, 256, 100, 90), (64, 8, 8, 64, 40, 100)])
+@pytest.mark.parametrize("cap", [0.0, 30.0, 1000.0])
+def test_masked_keys_do_not_touch_the_others_roundings(S, Hq, Hkv, D, T, pos0, cap):
+    """Keys outside of every window, small or of the largest codes beside visible ones of the same scales: the same results,
+    bit by bit."""
+    rng = np.random.default_rng(T)
+    n = pos0 + T
+    ref = kv.Cache(S, Hkv, -(-n // 64) * 64 + 64, D)
+    ref.k[...] = kv.encode(rng.standard_normal(ref.k.shape))
+    ref.v[...] = kv.encode(rng.standard_normal(ref.v.shape))
+    q, _ = _bf16(rng.standard_normal((S, T, Hq, D)))
+    opts = _ms().attn_opts(softcap=cap, window=30)
+    want = _run(_cache(ref), q, T, Hq, pos0, opts)
+    for far in (slice(0, pos0 - 29), slice(n, None)):
+        ref.k[:, :, far] = np.where(rng.random(ref.k[:, :, far].shape) < 0.5, 0x7e, 0xfe)
+        ref.v[:, :, far] = 0x7e
+    assert torch.equal(_run(_cache(ref), q, T, Hq, pos0, opts), want)
+
+
 # --------------------------------------------------------- turned positions
 
 @pytest.mark.parametrize("Hq,Hkv,D,rot,inter,T,pos0", [(32, 8, 128, 128, False, 2048, 0), (16, 2, 256, 256, True, 3000, 70000),
