@@ -966,7 +966,7 @@ __global__ __launch_bounds__(64 * few_waves(D)) void attention_q_few_kernel(AttA
 // ahead, and become operands when a wave reads them, as above: the conversions
 // run beside the matrix instructions, and LDS holds and moves a byte per value.
 //   Bound by the issue of vector and matrix instructions (311 and 104 a wave and tile of
-// 32 rows): 512 tokens behind 32256, 32 heads over 8 of 128, take 351 to 361 us, 0.78
+// 32 rows): 512 tokens behind 32256, 32 heads over 8 of 128, take 351 to 363 us, 0.78
 // PFLOP/s of products (1.2 with the probabilities' second parts); 2048 behind none 64, the
 // 32 tiles of the longest block one after another.  Tiles converted once by all waves and
 // kept in LDS as 16-bit values were slower, as were two groups of four waves with a share
