@@ -614,6 +614,83 @@ ms_status ms_attention_q(const ms_kv_cache_q* cache, const void* q, int32_t T, i
                          const int32_t* span_dev, const ms_attn_opts* opts, void* out, void* workspace_dev,
                          uint64_t workspace_bytes, void* stream);
 
+/* ---- the dense path in 8 bits ----------------------------------------------
+ *
+ * Projections and the head stay in VRAM whatever the budget: in half the bytes
+ * they leave room for experts.  Stateless calls like those of the 8-bit cache
+ * (nothing allocated, waited for or read on the host: all can be captured into a
+ * graph).
+ *
+ * A matrix in 8 bits: e4m3 codes [rows][n], 16-byte aligned, n a multiple of 16, at
+ * most 16384 (MS_E_UNSUPPORTED otherwise), and one byte x per 128 columns of R
+ * rows (the last ones may be fewer), [(rows + R - 1) / R][(n + 127) / 128]: a value
+ * is its code times 2^(x - 127).  R is 1 for activations, 128 for weights.  The
+ * exponent of a block is the least in [-40, 40] with the largest finite magnitude
+ * at most 448 * 2^e, codes are rounded to the nearest, ties to even; larger finite
+ * values become the largest code, infinities and NaN the code of NaN.  Stored
+ * exponents outside that range count as its ends. */
+
+/* x [rows][n] (dtype MS_F32 or MS_BF16, 16-byte aligned) as a matrix in 8 bits,
+ * block_rows = R (1 or 128): weights once, activations such as the attention's
+ * output on their way to a product.  Outputs overlap nothing. */
+ms_status ms_quant_q(const void* x, int32_t dtype, int32_t rows, int32_t n, int32_t block_rows, void* codes, void* exps,
+                     void* stream);
+
+/* Residual and norm: x = h + y, v = x weight / sqrt(mean(x^2) + eps) per row of d
+ * values (as n above).  h [T][d] bf16, y [T][d] y_dtype or NULL (none), weight [d]
+ * bf16 or NULL (1).  Outputs, each or NULL but not all: sum_out [T][d] bf16, x;
+ * out [T][d] bf16, v; codes [T][d] and exps [T][(d + 127) / 128], v in 8 bits (R =
+ * 1), both or neither.  Computed in double precision, so that each output is
+ * rounded once.  A row with NaN or an infinity gives NaN where that reaches.
+ * Pointers 16-byte aligned (exps: any).  sum_out or out may be h, or y in bf16;
+ * other overlaps are MS_E_INVALID. */
+ms_status ms_residual_norm_q(const void* h, const void* y, int32_t y_dtype, const void* weight, double eps, int32_t T,
+                             int32_t d, void* sum_out, void* out, void* codes, void* exps, void* stream);
+
+/* y[t][o] = sum_i x[t][i] w[o][i] (+ add[t][o] if add is not NULL): x [T][n_in] in
+ * 8 bits with R = 1, w [n_out][n_in] with R = 128, y and add [T][n_out] y_dtype
+ * (add may be y; other overlaps with y are MS_E_INVALID).  Sums in fp32.  An fp32 y is as exact as fp32 products and
+ * sums are; a bf16 y may be off, before its rounding, by 2^-12 of the largest of
+ * every eight neighbouring products (relative to a result about 2e-5): it is
+ * computed on the 8-bit matrix cores where there are many tokens.  A code of NaN
+ * makes the results of its row NaN. */
+ms_status ms_dense_q(const void* x, const void* x_exp, const void* w, const void* w_exp, int32_t T, int32_t n_in,
+                     int32_t n_out, void* y, int32_t y_dtype, const void* add, void* stream);
+
+/* ---- a token drawn from logits ---------------------------------------------
+ *
+ * Settings per row, device arrays of T or NULL (without), so that the rows of a
+ * batch have their own and a captured graph can be replayed with others:
+ * temperature (1 if NULL; 0, less or NaN: the arg max, as ms_argmax); top_k (0 or
+ * less, or n and more: off); top_p (1 and more or NaN: off); min_p (0, less or
+ * NaN: off). */
+typedef struct {
+  const float* temperature_dev;
+  const int32_t* top_k_dev;
+  const float* top_p_dev;
+  const float* min_p_dev;
+} ms_sample_opts;
+
+/* Device bytes that ms_sample needs at workspace_dev (0: none), whatever the
+ * settings; pure host arithmetic. */
+ms_status ms_sample_workspace(int32_t T, int32_t n, uint64_t* bytes_out);
+
+/* A token per row of logits [T][n] (fp32; n at most 524287, MS_E_UNSUPPORTED beyond;
+ * NaN counts as -infinity).  Tokens in descending order of their logits, ties to the
+ * lower index, weigh exp((l - max) / temperature); of them are kept the first top_k,
+ * of those the fewest whose weights reach top_p of theirs (at least one), and of all
+ * those with at least min_p of the largest weight.  idx_out[t] is the first kept
+ * token at which the running weight passes u_dev[t] (fp32 in [0, 1): others count as
+ * the nearest, NaN as 0) times the kept weight, prob_out[t] (or NULL) its share of
+ * the kept weight; the arg max has 1.  Infinite maxima share the weight; a row
+ * without a logit above -infinity gives 0.  Weights are whole numbers of 2^-45 of
+ * the largest, smaller ones zero: the same inputs give the same token whatever else
+ * runs, and whatever T.  opts NULL: temperature 1.
+ * workspace_dev: 16-byte aligned, used until the call has finished on `stream`;
+ * calls that may overlap in time need one each. */
+ms_status ms_sample(const float* logits, int32_t T, int32_t n, const ms_sample_opts* opts, const float* u_dev,
+                    int32_t* idx_out, float* prob_out, void* workspace_dev, uint64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

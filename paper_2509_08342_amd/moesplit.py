@@ -76,6 +76,10 @@ class ms_attn_opts(ctypes.Structure):
                 ("prefix", ctypes.c_int32), ("slopes_dev", ctypes.c_void_p), ("docs_dev", ctypes.c_void_p)]
 
 
+class ms_sample_opts(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("temperature_dev", "top_k_dev", "top_p_dev", "min_p_dev")]
+
+
 MS_CACHE_STATIC, MS_CACHE_LCP, MS_CACHE_LRU, MS_CACHE_LFU, MS_CACHE_RND = range(5)
 MS_COPY_KERNEL, MS_COPY_DMA = range(2)
 
@@ -131,6 +135,11 @@ def _load():
         "ms_kv_read_q": [ctypes.POINTER(ms_kv_cache_q), I32, I32, P, P, P],
         "ms_attention_q_workspace": [ctypes.POINTER(ms_kv_cache_q), I32, I32, I32, ctypes.POINTER(U64)],
         "ms_attention_q": [ctypes.POINTER(ms_kv_cache_q), P, I32, I32, I32, P, ctypes.POINTER(ms_attn_opts), P, P, U64, P],
+        "ms_quant_q": [P, I32, I32, I32, I32, P, P, P],
+        "ms_residual_norm_q": [P, P, I32, P, ctypes.c_double, I32, I32, P, P, P, P, P],
+        "ms_dense_q": [P, P, P, P, I32, I32, I32, P, I32, P, P],
+        "ms_sample_workspace": [I32, I32, ctypes.POINTER(U64)],
+        "ms_sample": [P, I32, I32, ctypes.POINTER(ms_sample_opts), P, P, P, P, U64, P],
         "ms_timeline_begin": [P, P, I32],
         "ms_timeline_end": [P, ctypes.POINTER(ms_interval), I32, ctypes.POINTER(I32)],
     }
@@ -509,3 +518,91 @@ def ms_attention_q(cache, q, T, Hq, pos0, out, workspace=None, opts=None, span=N
                             _stream(stream))
     if st:
         _check(st, what="ms_attention_q")
+
+
+# ------------------------------------------------- the dense path in 8 bits
+
+BLOCK_Q = 128  # columns that share a scale, and rows of a weight's block
+
+_VALUE_TYPES = {"torch.float32": (MS_F32, 4), "torch.bfloat16": (MS_BF16, 2)}
+
+
+def _value_type(x, name):
+    """(MS_F32 or MS_BF16, its size) of a tensor."""
+    try:
+        return _VALUE_TYPES[str(x.dtype)]
+    except (AttributeError, KeyError):
+        raise ValueError("%s: a float32 or bfloat16 tensor expected" % name) from None
+
+
+def new_matrix_q(rows, n, block_rows=1, device="cuda"):
+    """(codes [rows][n], exponents) of a matrix in 8 bits; block_rows 1, or 128 for weights."""
+    import torch
+    return (torch.empty(rows, n, dtype=torch.uint8, device=device),
+            torch.empty(-(-rows // block_rows), -(-n // BLOCK_Q), dtype=torch.uint8, device=device))
+
+
+def _blocks(n):
+    return -(-n // BLOCK_Q)
+
+
+def ms_quant_q(x, rows, n, block_rows, codes, exps, stream=None):
+    dtype, size = _value_type(x, "x")
+    st = lib.ms_quant_q(_rows(x, "x", size, rows * n), dtype, rows, n, block_rows, _rows(codes, "codes", 1, rows * n),
+                        _rows(exps, "exps", 1, -(-rows // max(block_rows, 1)) * _blocks(n)), _stream(stream))
+    if st:
+        _check(st, what="ms_quant_q")
+
+
+def ms_residual_norm_q(h, y, weight, eps, T, d, sum_out=None, out=None, codes=None, exps=None, stream=None):
+    dtype, size = (MS_F32, 4) if y is None else _value_type(y, "y")
+    opt = lambda x, name, size, n: None if x is None else _rows(x, name, size, n)  # noqa: E731
+    st = lib.ms_residual_norm_q(_rows(h, "h", 2, T * d), opt(y, "y", size, T * d), dtype, opt(weight, "weight", 2, d), eps, T, d,
+                                opt(sum_out, "sum_out", 2, T * d), opt(out, "out", 2, T * d), opt(codes, "codes", 1, T * d),
+                                opt(exps, "exps", 1, T * _blocks(d)), _stream(stream))
+    if st:
+        _check(st, what="ms_residual_norm_q")
+
+
+def ms_dense_q(x, x_exp, w, w_exp, T, n_in, n_out, y, add=None, stream=None):
+    """y (and add): float32 or bfloat16."""
+    dtype, size = _value_type(y, "y")
+    if add is not None and add.dtype != y.dtype:
+        raise ValueError("add: the type of y expected")
+    st = lib.ms_dense_q(_rows(x, "x", 1, T * n_in), _rows(x_exp, "x_exp", 1, T * _blocks(n_in)), _rows(w, "w", 1, n_out * n_in),
+                        _rows(w_exp, "w_exp", 1, _blocks(n_out) * _blocks(n_in)), T, n_in, n_out, _rows(y, "y", size, T * n_out),
+                        dtype, None if add is None else _rows(add, "add", size, T * n_out), _stream(stream))
+    if st:
+        _check(st, what="ms_dense_q")
+
+
+# ---------------------------------------------------------------- sampling
+
+def sample_opts(temperature=None, top_k=None, top_p=None, min_p=None):
+    """Settings of every row: device tensors [T], float32 (top_k: int32), or None."""
+    ts = (temperature, top_k, top_p, min_p)
+    for x, name in zip(ts, ("torch.float32", "torch.int32", "torch.float32", "torch.float32")):
+        if x is not None and str(getattr(x, "dtype", name)) != name:
+            raise ValueError("sample_opts: %s expected" % name)
+    o = ms_sample_opts(*[_ptr(x) for x in ts])
+    o.tensors = ts
+    return o
+
+
+def ms_sample_workspace(T, n):
+    out = ctypes.c_uint64()
+    _check(lib.ms_sample_workspace(T, n, ctypes.byref(out)), what="ms_sample_workspace")
+    return out.value
+
+
+def ms_sample(logits, T, n, opts, u, idx_out, prob_out=None, workspace=None, stream=None):
+    """workspace: a device tensor of at least ms_sample_workspace bytes."""
+    if opts is not None:
+        for x in getattr(opts, "tensors", ()):
+            if x is not None and getattr(x, "shape", None) not in (None, (T,)):
+                raise ValueError("sample_opts: [%d] expected" % T)
+    st = lib.ms_sample(_rows(logits, "logits", 4, T * n), T, n, opts, _rows(u, "u", 4, T), _rows(idx_out, "idx_out", 4, T),
+                       None if prob_out is None else _rows(prob_out, "prob_out", 4, T), _ptr(workspace),
+                       0 if workspace is None else workspace.nbytes, _stream(stream))
+    if st:
+        _check(st, what="ms_sample")

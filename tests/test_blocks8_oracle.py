@@ -1,0 +1,180 @@
+"""Without a GPU: the oracles of the dense path in 8 bits and of the drawn token,
+and the calls that the library and its binding refuse."""
+import numpy as np
+import pytest
+
+from oracle import blocks8 as b8
+from oracle import sample as osm
+
+torch = pytest.importorskip("torch")
+
+
+def _ms():
+    from paper_2509_08342_amd import moesplit
+    return moesplit
+
+
+# ------------------------------------------------------------------ oracles
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_blocks_hold_their_values(block_rows):
+    """Within half a step of the code, and of the least code times the scale; scales the least that hold the block."""
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((150, 300)) * np.exp2(rng.integers(-20, 20, (150, 1)))
+    c, e = b8.quantize(x, block_rows)
+    assert c.shape == x.shape and e.shape == (-(-150 // block_rows), 3)
+    unit = b8.spread(e.astype(int) - b8.BIAS, 150, 300, block_rows)
+    assert np.all(np.abs(b8.values(c, e, block_rows) - x) <= np.maximum(2.0 ** -4 * np.abs(x), 2.0 ** -10 * unit))
+    top = np.pad(np.abs(x), ((0, -150 % block_rows), (0, 84))).reshape(-1, block_rows, 3, 128).max(axis=(1, 3))
+    s = np.exp2(e.astype(float) - b8.BIAS)
+    assert np.all(top <= 448 * s) and np.all(top > 224 * s)
+
+
+def test_values_at_the_ends():
+    x = np.zeros((1, 128))
+    x[0, :5] = 448, -449, np.inf, np.nan, 1e-3
+    c, e = b8.quantize(x)
+    assert e[0, 0] == b8.BIAS + 1 and list(c[0, :4]) == [0x76, 0xf6, 0x7f, 0x7f]
+    assert b8.exponents(np.full((1, 1), 1e30), 1)[0, 0] == b8.EMAX and b8.exponents(np.zeros((1, 1)), 1)[0, 0] == b8.EMIN
+
+
+def test_norm_and_product():
+    rng = np.random.default_rng(1)
+    h, y, g = rng.standard_normal((3, 20)), rng.standard_normal((3, 20)), rng.standard_normal(20)
+    x, v = b8.residual_norm(h, y, g, 0.0)
+    assert np.allclose(x, h + y) and np.allclose(np.mean((v / g) ** 2, axis=1), 1.0)
+    p, mags = b8.dense(h, y, np.ones((3, 3)))
+    assert np.allclose(p, h @ y.T + 1) and np.all(mags >= np.abs(p))
+
+
+def test_draws():
+    """The shares of a small row, by hand; filters keep prefixes of the descending order, ties by index."""
+    l = np.log([1.0, 4.0, 2.0, 2.0, 0.5])
+    grid = (np.arange(950) + 0.5) / 950
+    got = np.bincount([osm.draw(l, u)[0] for u in grid], minlength=5)
+    assert list(got) == [100, 400, 200, 200, 50]
+    assert [osm.kept(l, top_k=k)[2] for k in (0, 1, 3, 5, 9)] == [5, 1, 3, 5, 5]
+    assert list(osm.kept(l)[0]) == [1, 2, 3, 0, 4]
+    assert [osm.kept(l, top_p=p)[2] for p in (0.0, 0.4, 0.43, 0.64, 0.99, 1.0)] == [1, 1, 2, 3, 5, 5]
+    assert osm.kept(l, top_k=3, top_p=0.7)[2] == 2 and osm.kept(l, min_p=0.3)[2] == 3 and osm.kept(l, min_p=1.0)[2] == 1
+    assert osm.draw(l, 0.999, temperature=0.0)[:2] == (1, 1.0)
+    assert osm.draw([np.nan, -np.inf], 0.5)[0] == 0 and osm.draw([0.0, np.inf, np.inf], 0.6)[0] == 2
+
+
+# ----------------------------------------------------------------- refusals
+
+def _status(call, *args, **kw):
+    ms = _ms()
+    with pytest.raises(ms.MoeSplitError) as e:
+        call(*args, **kw)
+    return e.value.status
+
+
+def _z(*shape, dtype=torch.uint8, shift=0):
+    n = int(np.prod(shape))
+    return torch.zeros(n + 64, dtype=dtype)[shift:shift + n].view(shape)
+
+
+def test_quant_refusals():
+    ms = _ms()
+    x, c, e = _z(4, 256, dtype=torch.float32), _z(4, 256), _z(4, 2)
+    assert _status(ms.ms_quant_q, x, 4, 256, 2, c, e) == ms.MS_E_INVALID
+    assert _status(ms.ms_quant_q, x, 4, 256, 0, c, e) == ms.MS_E_INVALID
+    assert _status(ms.ms_quant_q, x, -1, 256, 1, c, e) == ms.MS_E_INVALID
+    assert _status(ms.ms_quant_q, x, 4, 0, 1, c, e) == ms.MS_E_INVALID
+    assert _status(ms.ms_quant_q, x, 4, 200, 1, c, e) == ms.MS_E_UNSUPPORTED
+    assert _status(ms.ms_quant_q, _z(1, 16400, dtype=torch.float32), 1, 16400, 1, _z(1, 16400), _z(1, 129)) == ms.MS_E_UNSUPPORTED
+    assert _status(ms.ms_quant_q, _z(4, 256, dtype=torch.float32, shift=1), 4, 256, 1, c, e) == ms.MS_E_INVALID
+    assert _status(ms.ms_quant_q, x, 4, 256, 1, _z(4, 256, shift=8), e) == ms.MS_E_INVALID
+    assert ms.lib.ms_quant_q(None, ms.MS_F32, 4, 256, 1, c.data_ptr(), e.data_ptr(), None) == ms.MS_E_INVALID
+    assert ms.lib.ms_quant_q(x.data_ptr(), 2, 4, 256, 1, c.data_ptr(), e.data_ptr(), None) == ms.MS_E_INVALID
+    assert _status(ms.ms_quant_q, x, 4, 256, 1, x.view(torch.uint8).view(-1)[:1024], e) == ms.MS_E_INVALID
+    ms.ms_quant_q(_z(0, 256, dtype=torch.float32), 0, 256, 128, _z(0, 256), _z(0, 2))  # nothing to do
+    for bad in ((x.half(), c, e), (x[:3], c, e), (x, c[:3], e), (x, c, e[:3]), (x, c.float(), e), (x.t(), c, e)):
+        with pytest.raises(ValueError):
+            ms.ms_quant_q(bad[0], 4, 256, 1, *bad[1:])
+
+
+def test_norm_refusals():
+    ms = _ms()
+    T, d = 3, 256
+    bf = lambda **k: _z(T, d, dtype=torch.bfloat16, **k)  # noqa: E731
+    h, y, out, c, e = bf(), _z(T, d, dtype=torch.float32), bf(), _z(T, d), _z(T, 2)
+    n = ms.ms_residual_norm_q
+    assert _status(n, h, y, None, 1e-6, T, d) == ms.MS_E_INVALID  # no output
+    assert _status(n, h, y, None, 1e-6, T, d, codes=c) == ms.MS_E_INVALID
+    assert _status(n, h, y, None, 1e-6, T, d, out=out, exps=e) == ms.MS_E_INVALID
+    assert _status(n, h, y, None, -1e-6, T, d, out=out) == ms.MS_E_INVALID
+    assert _status(n, h, y, None, float("nan"), T, d, out=out) == ms.MS_E_INVALID
+    assert _status(n, h, y, None, 1e-6, -1, d, out=out) == ms.MS_E_INVALID
+    assert _status(n, h, y, None, 1e-6, 1, 100, out=out) == ms.MS_E_UNSUPPORTED
+    assert _status(n, bf(shift=1), y, None, 1e-6, T, d, out=out) == ms.MS_E_INVALID
+    assert _status(n, h, y, _z(d, dtype=torch.bfloat16, shift=4), 1e-6, T, d, out=out) == ms.MS_E_INVALID
+    assert _status(n, h, y, None, 1e-6, T, d, sum_out=out, out=out) == ms.MS_E_INVALID
+    both = torch.zeros(2 * T * d, dtype=torch.bfloat16)
+    assert _status(n, both[:T * d], y, None, 1e-6, T, d, out=both[d:d + T * d]) == ms.MS_E_INVALID  # another row's values
+    assert _status(n, h, y, None, 1e-6, T, d, out=y.view(torch.bfloat16).view(-1)[:T * d]) == ms.MS_E_INVALID
+    assert _status(n, h, y, None, 1e-6, T, d, codes=h.view(torch.uint8).view(-1)[:T * d], exps=e) == ms.MS_E_INVALID
+    ms.ms_residual_norm_q(_z(0, d, dtype=torch.bfloat16), None, None, 1e-6, 0, d, out=_z(0, d, dtype=torch.bfloat16))
+    for bad in (dict(h=h[:2]), dict(h=h.float()), dict(y=y.half()), dict(y=y[:2]), dict(weight=out[0, :100]),
+                dict(out=out[:1]), dict(codes=c[:2], exps=e), dict(codes=c, exps=e[:2])):
+        a = dict(h=h, y=y, weight=None, out=out)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            n(a.pop("h"), a.pop("y"), a.pop("weight"), 1e-6, T, d, **a)
+
+
+def test_dense_refusals():
+    ms = _ms()
+    T, n_in, n_out = 3, 256, 130
+    x, xe, w, we = _z(T, n_in), _z(T, 2), _z(n_out, n_in), _z(2, 2)
+    y = _z(T, n_out, dtype=torch.float32)
+    f = ms.ms_dense_q
+    assert _status(f, x, xe, w, we, T, n_in, 0, y) == ms.MS_E_INVALID
+    assert _status(f, x, xe, w, we, -1, n_in, n_out, y) == ms.MS_E_INVALID
+    assert _status(f, x, xe, w, we, 1, 0, n_out, y) == ms.MS_E_INVALID
+    assert _status(f, x, xe, w, we, T, 250, n_out, y) == ms.MS_E_UNSUPPORTED
+    assert _status(f, _z(1, 16400), _z(1, 129), _z(1, 16400), _z(1, 129), 1, 16400, 1, y) == ms.MS_E_UNSUPPORTED
+    assert _status(f, _z(T, n_in, shift=4), xe, w, we, T, n_in, n_out, y) == ms.MS_E_INVALID
+    assert _status(f, x, xe, _z(n_out, n_in, shift=8), we, T, n_in, n_out, y) == ms.MS_E_INVALID
+    p = [t.data_ptr() for t in (x, xe, w, we)]
+    assert ms.lib.ms_dense_q(p[0], None, p[2], p[3], T, n_in, n_out, y.data_ptr(), ms.MS_F32, None, None) == ms.MS_E_INVALID
+    assert ms.lib.ms_dense_q(*p, T, n_in, n_out, y.data_ptr(), 5, None, None) == ms.MS_E_INVALID
+    wide = torch.zeros(2 * T * n_out)
+    assert _status(f, x, xe, w, we, T, n_in, n_out, wide[:T * n_out], add=wide[1:1 + T * n_out]) == ms.MS_E_INVALID
+    room = torch.zeros(T * n_out * 4 + 64, dtype=torch.uint8)  # results over the tokens' codes
+    assert _status(f, room[:T * n_in], xe, w, we, T, n_in, n_out, room[:T * n_out * 4].view(torch.float32)) == ms.MS_E_INVALID
+    f(_z(0, n_in), _z(0, 2), w, we, 0, n_in, n_out, _z(0, n_out, dtype=torch.float32))
+    for bad in (dict(x=x[:2]), dict(xe=xe[:2]), dict(w=w[:100]), dict(we=we[:1]), dict(y=y[:2]), dict(y=y.half()),
+                dict(add=y[:2]), dict(add=y.bfloat16()), dict(w=w.t())):
+        a = dict(x=x, xe=xe, w=w, we=we, y=y, add=None)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            f(a["x"], a["xe"], a["w"], a["we"], T, n_in, n_out, a["y"], add=a["add"])
+
+
+def test_sample_refusals():
+    ms = _ms()
+    l, u, i = _z(2, 50, dtype=torch.float32), _z(2, dtype=torch.float32), _z(2, dtype=torch.int32)
+    assert _status(ms.ms_sample, l, -1, 50, None, u, i) == ms.MS_E_INVALID
+    assert _status(ms.ms_sample, l, 2, 0, None, u, i) == ms.MS_E_INVALID
+    assert _status(ms.ms_sample_workspace, 1, 1 << 19) == ms.MS_E_UNSUPPORTED
+    assert _status(ms.ms_sample_workspace, 1, -3) == ms.MS_E_INVALID
+    assert ms.lib.ms_sample_workspace(1, 5, None) == ms.MS_E_INVALID
+    assert ms.lib.ms_sample(l.data_ptr(), 2, 50, None, None, i.data_ptr(), None, None, 0, None) == ms.MS_E_INVALID
+    ms.ms_sample(_z(0, 50, dtype=torch.float32), 0, 50, None, _z(0, dtype=torch.float32), _z(0, dtype=torch.int32))
+    for T, n in ((1, 32000), (1, 524287), (3, 150000), (64, 100000)):  # a workspace too small, or not aligned
+        need = ms.ms_sample_workspace(T, n)
+        if need:
+            big = [_z(T, n, dtype=torch.float32), _z(T, dtype=torch.float32), _z(T, dtype=torch.int32)]
+            for ws in (None, _z(need - 1), _z(need, shift=8)):
+                assert _status(ms.ms_sample, big[0], T, n, None, big[1], big[2], None, ws) == ms.MS_E_INVALID
+    with pytest.raises(ValueError):
+        ms.sample_opts(top_k=u)
+    with pytest.raises(ValueError):
+        ms.sample_opts(temperature=i)
+    with pytest.raises(ValueError):
+        ms.ms_sample(l, 2, 50, ms.sample_opts(temperature=u[:1]), u, i)
+    for bad in ((l[:1], u, i), (l, u[:1], i), (l, u, i[:1]), (l.half(), u, i)):
+        with pytest.raises(ValueError):
+            ms.ms_sample(bad[0], 2, 50, None, *bad[1:])
