@@ -286,42 +286,579 @@ __device__ __forceinline__ void to_bf16(uint4 c, float scale, msk::bf16x8_t (&o)
   o[1] = msk::as_bf16x8(make_uint4(pair(c.z, false), pair(c.z, true), pair(c.w, false), pair(c.w, true)));
 }
 
-__device__ __forceinline__ float stored_scale(uint8_t e) {
-  return pow2(min(max(static_cast<int>(e) - kExpBias, kExpMin), kExpMax));
-}
-
 __device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_value(uint16_t* p, float v) { *p = static_cast<uint16_t>(bf16_bits(v)); }
 
-// y^T = W x^T, a wave per 16 outputs x 16 tokens: lane l has sixteen codes of row l % 16 at
-// k + 16 (l / 16).
+constexpr uint32_t scale_bits(int e) { return static_cast<uint32_t>(e + kExpBias); }
+
+// a stored exponent, kept in range whatever the byte holds
+__device__ __forceinline__ uint32_t exponent_in_range(uint32_t x) {
+  return min(max(x, scale_bits(kExpMin)), scale_bits(kExpMax));
+}
+__device__ __forceinline__ float scale_of(uint32_t x) { return __uint_as_float(x << 23); }
+
+__device__ const uint4 kZeroCodes = {0, 0, 0, 0};
+
+// Four neighbouring outputs of a token.
 template <typename Y>
-__global__ __launch_bounds__(64) void dense_q_simple_kernel(DenseArgs a) {
-  const int lane = threadIdx.x, t = blockIdx.x * 16 + (lane & 15), o0 = blockIdx.y * 16, o = o0 + (lane & 15);
-  const int tr = min(t, a.T - 1), orow = min(o, a.n_out - 1);
-  msk::f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = 0; k0 < a.n_in; k0 += 64) {
-    const int k = k0 + 16 * (lane >> 4), kb = k0 / kBlock;
-    uint4 cx = make_uint4(0, 0, 0, 0), cw = cx;
-    if (k < a.n_in) {
-      cx = *reinterpret_cast<const uint4*>(a.x + static_cast<size_t>(tr) * a.n_in + k);
-      cw = *reinterpret_cast<const uint4*>(a.w + static_cast<size_t>(orow) * a.n_in + k);
-    }
-    msk::bf16x8_t A[2], B[2];
-    to_bf16(cw, stored_scale(a.w_exp[static_cast<size_t>(orow / kBlock) * a.nb + kb]), A);
-    to_bf16(cx, stored_scale(a.x_exp[static_cast<size_t>(tr) * a.nb + kb]), B);
-    acc = msk::mfma16(A[0], B[0], acc);
-    acc = msk::mfma16(A[1], B[1], acc);
-  }
-  if (t >= a.T) return;
+__device__ __forceinline__ void store4(const DenseArgs& a, int t, int o, msk::f32x4_t v, int vec) {
+  const size_t i = static_cast<size_t>(t) * a.n_out + o;
+  Y* y = static_cast<Y*>(a.y) + i;
+  const Y* add = a.add ? static_cast<const Y*>(a.add) + i : nullptr;
+  if (!vec) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int c = o0 + 4 * (lane >> 4) + r;
-    if (c >= a.n_out) continue;
-    const size_t i = static_cast<size_t>(t) * a.n_out + c;
-    const float add = a.add ? load_value(static_cast<const Y*>(a.add)[i]) : 0.0f;
-    store_value(static_cast<Y*>(a.y) + i, acc[r] + add);
+    for (int r = 0; r < 4; ++r)
+      if (o + r < a.n_out) store_value(y + r, v[r] + (add ? load_value(add[r]) : 0.0f));
+  } else if (o < a.n_out) {  // n_out a multiple of 4, rows aligned to four values
+    if constexpr (sizeof(Y) == 4) {
+      float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (add) b = *reinterpret_cast<const float4*>(add);
+      *reinterpret_cast<float4*>(y) = make_float4(v[0] + b.x, v[1] + b.y, v[2] + b.z, v[3] + b.w);
+    } else {
+      uint2 b = make_uint2(0, 0);
+      if (add) b = *reinterpret_cast<const uint2*>(add);
+      v[0] += __uint_as_float(b.x << 16), v[1] += __uint_as_float(b.x & 0xffff0000u);
+      v[2] += __uint_as_float(b.y << 16), v[3] += __uint_as_float(b.y & 0xffff0000u);
+      *reinterpret_cast<uint2*>(y) = make_uint2(bf16_bits(v[0]) | bf16_bits(v[1]) << 16, bf16_bits(v[2]) | bf16_bits(v[3]) << 16);
+    }
   }
+}
+
+// Eight.
+template <typename Y>
+__device__ __forceinline__ void store8(const DenseArgs& a, int t, int o, msk::f32x4_t u, msk::f32x4_t v, int vec) {
+  const size_t i = static_cast<size_t>(t) * a.n_out + o;
+  if (sizeof(Y) == 4 || !vec || a.n_out % 8 != 0 || ((reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.add)) & 15)) {
+    store4<Y>(a, t, o, u, vec);
+    store4<Y>(a, t, o + 4, v, vec);
+  } else if (o < a.n_out) {
+    float f[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]}, b[8] = {};
+    if (a.add) load8(static_cast<const uint16_t*>(a.add) + i, b);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) f[r] += b[r];
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.y) + i) = pack_bf16(f);
+  }
+}
+
+// Few tokens: MO blocks of 16 outputs x NT of 16 tokens (the last one repeated) per
+// work-group, its KW waves every KW-th 128 columns.  Codes go from memory to registers: lane l has pieces l / 16 and 4 + l / 16 of sixteen
+// codes of row l % 16.
+template <typename Y, int KW, int MO, int NT>
+__global__ __launch_bounds__(64 * KW) void dense_q_few_kernel(DenseArgs a, int vec) {
+  __shared__ __align__(16) float red[KW][MO * NT][64][4];
+  const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int o0 = blockIdx.x * 16 * MO;  // (MO a power of two: of one block of 128)
+  const uint8_t* w_exp = a.w_exp + static_cast<size_t>(o0 / kBlock) * a.nb;
+  const uint8_t *w[MO], *x[NT], *x_exp[NT];
+#pragma unroll
+  for (int m = 0; m < MO; ++m) w[m] = a.w + static_cast<size_t>(min(o0 + 16 * m + r16, a.n_out - 1)) * a.n_in;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const size_t t = min(16 * n + r16, a.T - 1);
+    x[n] = a.x + t * a.n_in, x_exp[n] = a.x_exp + t * a.nb;
+  }
+  msk::f32x4_t acc[MO][NT];
+#pragma unroll
+  for (int m = 0; m < MO; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[m][n] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int b = wv; b < a.nb; b += KW) {
+    uint4 cw[MO][2], cx[NT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = b * kBlock + 16 * (4 * h + g4);
+      const bool in = k < a.n_in;
+#pragma unroll
+      for (int m = 0; m < MO; ++m) cw[m][h] = in ? *reinterpret_cast<const uint4*>(w[m] + k) : kZeroCodes;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) cx[n][h] = in ? *reinterpret_cast<const uint4*>(x[n] + k) : kZeroCodes;
+    }
+    const float sw = scale_of(exponent_in_range(w_exp[b]));
+    float sx[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) sx[n] = scale_of(exponent_in_range(x_exp[n][b]));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      msk::bf16x8_t A[MO][2], B[2];
+#pragma unroll
+      for (int m = 0; m < MO; ++m) to_bf16(cw[m][h], sw, A[m]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        to_bf16(cx[n][h], sx[n], B);
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int m = 0; m < MO; ++m) acc[m][n] = msk::mfma16(A[m][q], B[q], acc[m][n]);
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MO; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) *reinterpret_cast<msk::f32x4_t*>(red[wv][m * NT + n][lane]) = acc[m][n];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 64 * MO * NT; i += 64 * KW) {
+    const int p = i / 64, l = i & 63, t = 16 * (p % NT) + (l & 15);
+    msk::f32x4_t v = *reinterpret_cast<const msk::f32x4_t*>(red[0][p][l]);
+#pragma unroll
+    for (int k = 1; k < KW; ++k) v += *reinterpret_cast<const msk::f32x4_t*>(red[k][p][l]);
+    if (t < a.T) store4<Y>(a, t, o0 + 16 * (p / NT) + 4 * (l >> 4), v, vec);
+  }
+}
+
+// More: y^T = W x^T, a work-group takes BM tokens x BN outputs; both operands go to LDS as
+// codes by direct loads (a row's 128 columns of a stage are a cache line; piece p of sixteen
+// codes of row r sits in slot p ^ (r % 8), so the lanes that an LDS read serves together hit
+// distinct banks), in a ring of NST stages.  WM x WN waves split the tile.
+//   An fp32 result: codes become bf16, times their scale, as operands are read; every
+// product is exact and sums are fp32.  A bf16 result (EIGHT): the matrix cores take the codes
+// and the scales as they are, at twice the rate; they align the products of eight neighbouring
+// columns to about 2^-13 of the largest before they add them in fp32, which leaves 2e-5 of a
+// result, a hundredth of what its rounding to bf16 takes and too much for an fp32 one.
+constexpr int kStageLoad = 64 * 16;      // one load: 8 rows
+constexpr int kRows16 = 16 * kBlock;     // bytes of 16 staged rows
+constexpr int kTileExps = 16384;         // exponents of a tile's tokens that fit: blocks of columns x BM
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
+// The exponents of a tile's tokens t0 .. t0 + BM - 1, put(token, block of columns, exponent): the
+// rows follow each other in memory, and eight are requested before the first is used.
+template <int BM, int THREADS, typename Put>
+__device__ __forceinline__ void stage_exponents(const DenseArgs& a, int t0, Put put) {
+  const uint8_t* e = a.x_exp + static_cast<size_t>(t0) * a.nb;
+  const int n = min(BM, a.T - t0) * a.nb;
+  for (int i0 = threadIdx.x; i0 < n; i0 += 8 * THREADS) {
+    uint32_t v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = e[min(i0 + i * THREADS, n - 1)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i0 + i * THREADS < n)
+        put((i0 + i * THREADS) / a.nb, (i0 + i * THREADS) % a.nb, static_cast<uint8_t>(exponent_in_range(v[i])));
+  }
+}
+
+template <typename Y, bool EIGHT, int BM, int BN, int WM, int WN, int NST>
+__global__ __launch_bounds__(64 * WM * WN) void dense_q_tile_kernel(DenseArgs a, int m_tiles, int vec) {
+  constexpr int NWV = WM * WN;
+  constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // 16-wide blocks per wave
+  constexpr int NL = (BM + BN) / 8 / NWV;              // loads per wave and stage
+  constexpr int SBYTES = (BM + BN) * kBlock;
+  constexpr int WB = (BN + kBlock - 1) / kBlock + 1;   // weights' scales that a tile may touch
+  constexpr int EXPS = BM * (kMostColumns / kBlock) < kTileExps ? BM * (kMostColumns / kBlock) : kTileExps;
+  static_assert(TM * WM * 16 == BM && TN * WN * 16 == BN && NL * 8 * NWV == BM + BN, "tile split");
+  static_assert(NST >= 2 && NST * SBYTES + EXPS + WB * (kMostColumns / kBlock) <= 160 * 1024 && (NST - 2) * NL < 64, "ring");
+  __shared__ __align__(16) unsigned char lds[NST * SBYTES];
+  __shared__ uint8_t xe[EXPS], we[WB * (kMostColumns / kBlock)];  // [blocks of columns][BM], [WB][blocks of columns]
+  const int lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wv % WM, wn = wv / WM;
+  const int tile = msk::xcd_local(blockIdx.x, gridDim.x);
+  const int t0 = (tile % m_tiles) * BM, o0 = (tile / m_tiles) * BN;
+  const int lrow = lane >> 3, lk = 16 * ((lane & 7) ^ lrow);
+  const uint8_t* src[NL];  // staged rows: the tile's BM tokens, then its BN outputs
+#pragma unroll
+  for (int j = 0; j < NL; ++j) {
+    const int r = 8 * (wv + NWV * j) + lrow;
+    src[j] = (r < BM ? a.x + static_cast<size_t>(min(t0 + r, a.T - 1)) * a.n_in
+                     : a.w + static_cast<size_t>(min(o0 + r - BM, a.n_out - 1)) * a.n_in) + lk;
+  }
+  const uint32_t lbase = msk::lds_address(lds) + wv * kStageLoad;
+  auto issue = [&](int sl, int buf) {  // stages past the last reload it (in bounds, never read)
+    const int k0 = min(sl, a.nb - 1) * kBlock;
+    if (k0 + kBlock <= a.n_in) {
+#pragma unroll
+      for (int j = 0; j < NL; ++j) msk::lds_load16(src[j] + k0, lbase + buf * SBYTES + NWV * j * kStageLoad);
+    } else {  // zeros past the rows' ends: what follows in memory may be NaN
+#pragma unroll
+      for (int j = 0; j < NL; ++j)
+        msk::lds_load16(k0 + lk < a.n_in ? src[j] + k0 : reinterpret_cast<const uint8_t*>(&kZeroCodes),
+                        lbase + buf * SBYTES + NWV * j * kStageLoad);
+    }
+  };
+#pragma unroll
+  for (int p = 0; p < NST - 1; ++p) issue(p, p);
+  stage_exponents<BM, 64 * NWV>(a, t0, [&](int r, int b, uint8_t e) { xe[b * BM + r] = e; });
+  const int wb0 = o0 / kBlock, wbn = (a.n_out - 1) / kBlock;
+  for (int i = threadIdx.x; i < WB * a.nb; i += 64 * NWV)
+    we[i] = static_cast<uint8_t>(exponent_in_range(a.w_exp[static_cast<size_t>(min(wb0 + i / a.nb, wbn)) * a.nb + i % a.nb]));
+  int fo[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) fo[h] = (lane & 15) * kBlock + 16 * ((4 * h + (lane >> 4)) ^ (lane & 7));
+  int wb[TN];  // the scale's row of each block of outputs
+#pragma unroll
+  for (int n = 0; n < TN; ++n) wb[n] = ((o0 + (wn * TN + n) * 16) / kBlock - wb0) * a.nb;
+  const uint8_t* xel = xe + wm * TM * 16 + (lane & 15);
+  msk::f32x4_t acc[TN][TM];
+#pragma unroll
+  for (int n = 0; n < TN; ++n)
+#pragma unroll
+    for (int m = 0; m < TM; ++m) acc[n][m] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
+  auto compute = [&](int sl, int buf) {
+    const unsigned char* sx = lds + buf * SBYTES + wm * TM * kRows16;
+    const unsigned char* sw = lds + buf * SBYTES + BM * kBlock + wn * TN * kRows16;
+    if constexpr (EIGHT) {
+      auto codes = [&](const unsigned char* p) {
+        const uint4 lo = *reinterpret_cast<const uint4*>(p + fo[0]), hi = *reinterpret_cast<const uint4*>(p + fo[1]);
+        return i32x8_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
+                       static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
+      };
+      i32x8_t A[TN];
+      int ea[TN];
+#pragma unroll
+      for (int n = 0; n < TN; ++n) A[n] = codes(sw + n * kRows16), ea[n] = we[wb[n] + sl];
+#pragma unroll
+      for (int m = 0; m < TM; ++m) {
+        const i32x8_t B = codes(sx + m * kRows16);
+        const int eb = xel[sl * BM + 16 * m];
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+          acc[n][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A[n], B, acc[n][m], 0, 0, 0, ea[n], 0, eb);
+      }
+    } else {
+      float sa[TN], sb[TM];
+#pragma unroll
+      for (int n = 0; n < TN; ++n) sa[n] = scale_of(we[wb[n] + sl]);
+#pragma unroll
+      for (int m = 0; m < TM; ++m) sb[m] = scale_of(xel[sl * BM + 16 * m]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        msk::bf16x8_t A[TN][2];
+#pragma unroll
+        for (int n = 0; n < TN; ++n) to_bf16(*reinterpret_cast<const uint4*>(sw + n * kRows16 + fo[h]), sa[n], A[n]);
+#pragma unroll
+        for (int m = 0; m < TM; ++m) {
+          msk::bf16x8_t B[2];
+          to_bf16(*reinterpret_cast<const uint4*>(sx + m * kRows16 + fo[h]), sb[m], B);
+#pragma unroll
+          for (int n = 0; n < TN; ++n) acc[n][m] = msk::mfma16(A[n][0], B[0], acc[n][m]);
+#pragma unroll
+          for (int n = 0; n < TN; ++n) acc[n][m] = msk::mfma16(A[n][1], B[1], acc[n][m]);
+        }
+      }
+    }
+  };
+  __syncthreads();  // the exponents are there
+  int cur = 0, nxt = NST - 1;
+  for (int sl = 0; sl < a.nb; ++sl) {
+    msk::wait_vm<(NST - 2) * NL>();
+    msk::bare_barrier();
+    issue(sl + NST - 1, nxt);
+    compute(sl, cur);
+    cur = cur + 1 == NST ? 0 : cur + 1;
+    nxt = nxt + 1 == NST ? 0 : nxt + 1;
+  }
+  msk::wait_vm<0>();  // the reloads past the last stage land before the work-group ends
+#pragma unroll
+  for (int m = 0; m < TM; ++m) {
+    const int t = t0 + (wm * TM + m) * 16 + (lane & 15);
+    if (t >= a.T) continue;
+#pragma unroll
+    for (int n = 0; n < TN; ++n) store4<Y>(a, t, o0 + (wn * TN + n) * 16 + 4 * (lane >> 4), acc[n][m], vec);
+  }
+}
+
+// Prompts: tiles of 256 tokens in eight waves, two to a SIMD, of which one reads a stage's
+// operands from LDS while the other's matrix instructions run; they change places at every
+// barrier.  Both read a stage: waves 0 .. 3 in phase 2 s, waves 4 .. 7 in phase 2 s + 1, so
+// its buffer is loaded again from phase 2 s + 2 on and read from 2 s + 4 on.  A stage's loads
+// are spread over what else a wave does in the phase: the CU takes one per 16 cycles, and
+// in a row they would hold up what stands behind them.
+//   A row of a matrix instruction's block n of outputs, for bf16 results, is one of 32 that
+// blocks n and n ^ 1 share, so that a lane ends with eight neighbouring outputs of a token
+// and four lanes with 64 bytes in a row (with fp32 results they do as it is).
+template <typename Y, bool EIGHT, int BN>
+__global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m_tiles, int vec) {
+  constexpr int BM = 256, WM = EIGHT ? 2 : 4, NWV = 8, WN = NWV / WM;
+  constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+  constexpr int NX = BM / 8 / NWV, NL = (BM + BN) / 8 / NWV;  // loads per wave and stage: tokens', all
+  constexpr int SBYTES = (BM + BN) * kBlock;
+  constexpr int EW = TN <= 4 ? 4 : 8;  // bytes of a wave's weight exponents
+  static_assert(TM % 4 == 0 && TM <= 8 && TN <= 8 && TN * WN * 16 == BN && BN % (8 * NWV) == 0 && NL <= 8, "tile split");
+  static_assert(2 * SBYTES + kTileExps + 2 * EW * WN * (kMostColumns / kBlock) <= 160 * 1024, "LDS");
+  constexpr auto paired = [](int n) { return sizeof(Y) == 2 && (n | 1) < TN; };
+  __shared__ __align__(16) unsigned char lds[2 * SBYTES];
+  __shared__ __align__(4) uint8_t xe[kTileExps];  // [blocks of columns][WM][16 lanes][TM]
+  __shared__ __align__(4) uint8_t we[2 * EW * WN * (kMostColumns / kBlock)];  // [blocks of columns][WN][lanes' halves][EW]
+  const int lane = threadIdx.x & 63, i16 = lane & 15, g4 = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool second = wv >= 4;
+  const int wm = wv % WM, wn = wv / WM;
+  const int tile = msk::xcd_local(blockIdx.x, gridDim.x);
+  // (the division is the vector unit's)
+  const int t0 = __builtin_amdgcn_readfirstlane(tile % m_tiles * BM), o0 = __builtin_amdgcn_readfirstlane(tile / m_tiles * BN);
+  const uint8_t *x0 = a.x + static_cast<size_t>(t0) * a.n_in, *w0 = a.w + static_cast<size_t>(o0) * a.n_in;
+
+  // Staged rows: the tile's tokens, then its outputs, the last of either again.  Piece p of a
+  // token's row r sits in slot p ^ (r % 8), of an output's in that with its halves changed
+  // where r / 8 is odd: so the eight rows that are read together have distinct slots in either
+  // order.  A load takes eight rows from a uniform address on; lanes' offsets to them are all
+  // alike but where the rows end, and from there on.
+  const int x_end = min(BM, a.T - t0) - 1, w_end = min(BN, a.n_out - o0) - 1;
+  const int lrow = lane >> 3, xk = 16 * ((lane & 7) ^ lrow), wk = xk ^ 64 * (wv & 1);
+  const uint32_t x_off = lrow * a.n_in + xk, w_off = lrow * a.n_in + wk;
+  const uint32_t x_last = min(lrow, x_end % 8) * a.n_in + xk, w_last = min(lrow, w_end % 8) * a.n_in + wk;
+  const uint32_t lbase = msk::lds_address(lds) + wv * kStageLoad;
+  // Load j of a stage, into the buffer sl % 2; stages past the last reload it (never read).
+  // Pieces past a row's end load its first one instead: clear_ends puts zeros in their place.
+  auto issue = [&](int sl, int j) {
+    const bool x = j < NX;
+    const int k0 = min(sl, a.nb - 1) * kBlock, g = wv + NWV * (x ? j : j - NX), last = (x ? x_end : w_end) / 8, k = x ? xk : wk;
+    const uint32_t o = g < last ? (x ? x_off : w_off) : (x ? x_last : w_last);
+    msk::lds_load16((x ? x0 : w0) + min(g, last) * 8 * a.n_in, o + (k0 + k < a.n_in ? k0 : -k),
+                    lbase + (sl & 1) * SBYTES + NWV * j * kStageLoad);
+  };
+  auto clear_ends = [&](int sl) {  // of the loads of this wave, which have landed
+    if (sl != a.nb - 1 || a.n_in % kBlock == 0) return;
+#pragma unroll
+    for (int j = 0; j < NL; ++j)
+      if (sl * kBlock + (j < NX ? xk : wk) >= a.n_in)
+        *reinterpret_cast<uint4*>(lds + (sl & 1) * SBYTES + (wv + NWV * j) * kStageLoad + 16 * lane) = make_uint4(0, 0, 0, 0);
+  };
+#pragma unroll
+  for (int j = 0; j < NL; ++j) issue(0, j);
+  stage_exponents<BM, 64 * NWV>(a, t0, [&](int r, int b, uint8_t e) {
+    xe[b * BM + (r / (16 * TM) * 16 + r % 16) * TM + r / 16 % TM] = e;
+  });
+  for (int i = threadIdx.x; i < 2 * EW * WN * a.nb; i += 64 * NWV) {
+    const int n = i % EW, half = i / EW % 2, b = i / (2 * EW * WN);
+    const int o = min(o0 + (i / (2 * EW) % WN * TN + (paired(n) ? (n & ~1) + half : n)) * 16, a.n_out - 1);
+    we[i] = static_cast<uint8_t>(exponent_in_range(a.w_exp[static_cast<size_t>(o / kBlock) * a.nb + b]));
+  }
+  int xo[2], wo[3][2];  // a lane's pieces of a block of tokens, and of an even, an odd and an unpaired one of outputs
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int piece = 4 * h + g4;
+    xo[h] = i16 * kBlock + 16 * (piece ^ (i16 & 7));
+#pragma unroll
+    for (int n = 0; n < 3; ++n) {
+      const int r = n < 2 ? i16 / 4 * 8 + n * 4 + i16 % 4 : i16;
+      wo[n][h] = r * kBlock + 16 * (piece ^ (r & 7) ^ (r >> 3 & 1) << 2);
+    }
+  }
+
+  msk::f32x4_t acc[TN][TM];
+#pragma unroll
+  for (int n = 0; n < TN; ++n)
+#pragma unroll
+    for (int m = 0; m < TM; ++m) acc[n][m] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
+  // A stage's operands: codes, or the tokens' in bf16
+  uint4 A[TN][2], B[EIGHT ? TM : 1][2];
+  msk::bf16x8_t xb[EIGHT ? 1 : TM][2][2];
+  uint32_t ea[EW / 4], eb[TM / 4];  // a byte per block of 16 outputs, and of 16 tokens
+  auto output_scale = [&](int n) { return ea[n / 4] >> (8 * (n % 4)); };
+  auto token_scale = [&](int m) { return eb[m / 4] >> (8 * (m % 4)); };
+  msk::bf16x8_t wa[2][2][2];  // two blocks of outputs, the next one made while the last is multiplied
+  auto convert = [&](int n) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) to_bf16(A[n][h], scale_of(output_scale(n) & 255), wa[n % 2][h]);
+  };
+  auto read = [&](int sl, auto load) {
+    const unsigned char* sx = lds + (sl & 1) * SBYTES + wm * TM * kRows16;
+    const unsigned char* sw = lds + (sl & 1) * SBYTES + BM * kBlock + wn * TN * kRows16;
+#pragma unroll
+    for (int i = 0; i < EW / 4; ++i) ea[i] = *reinterpret_cast<const uint32_t*>(we + ((sl * WN + wn) * 2 + (i16 >> 3)) * EW + 4 * i);
+#pragma unroll
+    for (int i = 0; i < TM / 4; ++i) eb[i] = *reinterpret_cast<const uint32_t*>(xe + ((sl * WM + wm) * 16 + i16) * TM + 4 * i);
+    int j = 0;
+#pragma unroll
+    for (int i = 0; i < TM + TN; ++i) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (i >= TM) {
+          const int n = i - TM;
+          A[n][h] = *reinterpret_cast<const uint4*>(sw + (paired(n) ? n & ~1 : n) * kRows16 + wo[paired(n) ? n & 1 : 2][h]);
+          continue;
+        }
+        const uint4 c = *reinterpret_cast<const uint4*>(sx + i * kRows16 + xo[h]);
+        if constexpr (EIGHT)
+          B[i][h] = c;
+        else
+          to_bf16(c, scale_of(token_scale(i) & 255), xb[i][h]);
+      }
+      while ((i + 1) * NL / (TN + TM) > j) load(j++);
+    }
+    if constexpr (!EIGHT) convert(0);
+  };
+  auto pin = []() { __builtin_amdgcn_sched_barrier(0); };
+  auto multiply = [&](auto load) {
+    int j = 0;
+    if constexpr (EIGHT) {
+      auto codes = [](const uint4 (&p)[2]) {
+        return i32x8_t{static_cast<int>(p[0].x), static_cast<int>(p[0].y), static_cast<int>(p[0].z), static_cast<int>(p[0].w),
+                       static_cast<int>(p[1].x), static_cast<int>(p[1].y), static_cast<int>(p[1].z), static_cast<int>(p[1].w)};
+      };
+#pragma unroll
+      for (int m = 0; m < TM; ++m) {
+#pragma unroll
+        for (int n = 0; n < TN; ++n)  // (of a scale the lowest byte counts)
+          acc[n][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(codes(A[n]), codes(B[m]), acc[n][m], 0, 0, 0,
+                                                                       static_cast<int>(output_scale(n)), 0,
+                                                                       static_cast<int>(token_scale(m)));
+        while ((m + 1) * NL / TM > j) load(j++);
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < TN; ++n) {
+        if (n + 1 < TN) convert(n + 1);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int m = 0; m < TM; ++m) acc[n][m] = msk::mfma16(wa[n % 2][q / 2][q % 2], xb[m][q / 2][q % 2], acc[n][m]);
+        if (n + 1 < TN) {
+#pragma unroll
+          for (int i = 0; i < 4 * TM; ++i) {  // a conversion behind every matrix instruction
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x2, 2, 0);
+          }
+        }
+        pin();
+        while ((n + 1) * NL / TN > j) load(j++);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+      for (int m = 0; m < TM; ++m) asm volatile("" : "+v"(acc[n][m]));  // here, and not behind a barrier or wait
+  };
+  auto change = [&]() {  // to the next phase
+    pin();
+    msk::bare_barrier();
+    pin();
+  };
+  msk::wait_vm<0>();
+  clear_ends(0);
+  __syncthreads();  // the first stage and the exponents are there
+  auto none = [](int) {};
+  if (second) {
+#pragma unroll
+    for (int j = 0; j < NL; ++j) issue(1, j);
+    change();
+    for (int sl = 0; sl < a.nb; ++sl) {
+      read(sl, none);
+      msk::wait_vm<0>();
+      clear_ends(sl + 1);
+      change();
+      multiply([&](int j) { pin(); issue(sl + 2, j); pin(); });
+      change();
+    }
+  } else {
+    for (int sl = 0; sl < a.nb; ++sl) {
+      read(sl, [&](int j) { issue(sl + 1, j); });
+      change();
+      multiply(none);
+      msk::wait_vm<0>();
+      clear_ends(sl + 1);
+      change();
+    }
+    change();
+  }
+  msk::wait_vm<0>();  // the reloads past the last stage land before the work-group ends
+#pragma unroll
+  for (int m = 0; m < TM; ++m) {
+    const int t = t0 + (wm * TM + m) * 16 + i16;
+    if (t >= a.T) continue;
+#pragma unroll
+    for (int n = 0; n < TN; ++n) {
+      const int o = o0 + wn * TN * 16;
+      if (!paired(n))
+        store4<Y>(a, t, o + n * 16 + 4 * g4, acc[n][m], vec);
+      else if (n % 2 == 0)
+        store8<Y>(a, t, o + n * 16 + 8 * g4, acc[n][m], acc[n + 1 < TN ? n + 1 : n][m], vec);
+    }
+  }
+}
+
+// Tile of a launch: the one whose rounds over the CUs cost least, by the times (0.1 us) of
+// one full launch at 4096 columns, fp32 and bf16 results, with one work-group per CU and
+// with two, of which the small tiles' overlap.
+constexpr int kCus = 256;
+struct Tile {
+  int bm, bn, threads;  // tokens, outputs
+  int one[2], two[2];   // cost of a round
+};
+constexpr Tile kTiles[] = {{32, 32, 256, {124, 84}, {148, 102}},   {64, 64, 256, {193, 124}, {262, 167}},
+                           {128, 128, 512, {406, 256}, {785, 496}}, {256, 128, 512, {622, 425}, {1187, 824}},
+                           {256, 192, 512, {803, 499}, {1588, 984}}, {256, 256, 512, {0, 589}, {0, 1179}}};
+
+template <typename Y, bool EIGHT>
+ms_status launch_tiles(const DenseArgs& a, int vec, hipStream_t s) {
+  auto count = [&](const Tile& t) {
+    return ((static_cast<int64_t>(a.T) + t.bm - 1) / t.bm) * ((static_cast<int64_t>(a.n_out) + t.bn - 1) / t.bn);
+  };
+  int best = -1;
+  int64_t best_cost = INT64_MAX;
+  for (int i = 0; i < (EIGHT ? 6 : 5); ++i) {
+    const Tile& t = kTiles[i];
+    const int64_t n = count(t), rest = n % (2 * kCus);
+    if (n * t.threads > UINT32_MAX || a.nb * t.bm > kTileExps) continue;  // past a launch, or the exponents' LDS
+    const int64_t cost = n / (2 * kCus) * t.two[EIGHT] + (rest == 0 ? 0 : rest <= kCus ? t.one[EIGHT] : t.two[EIGHT]);
+    if (cost < best_cost) best = i, best_cost = cost;
+  }
+  if (best < 0) return MS_E_UNSUPPORTED;
+  const int m_tiles = (a.T - 1) / kTiles[best].bm + 1;
+  const dim3 grid(static_cast<unsigned>(count(kTiles[best]))), block(kTiles[best].threads);
+#define MSK_TILE_CASE(I_, BM_, BN_, WM_, WN_, NST_)                                                                  \
+  case I_:                                                                                                           \
+    static_assert(kTiles[I_].bm == BM_ && kTiles[I_].bn == BN_ && kTiles[I_].threads == 64 * WM_ * WN_, "tiles");        \
+    hipLaunchKernelGGL((dense_q_tile_kernel<Y, EIGHT, BM_, BN_, WM_, WN_, NST_>), grid, block, 0, s, a, m_tiles, vec); \
+    break;
+#define MSK_PAIR_CASE(I_, BN_)                                                                               \
+  case I_:                                                                                                   \
+    static_assert(kTiles[I_].bm == 256 && kTiles[I_].bn == BN_ && kTiles[I_].threads == 512, "tiles");           \
+    if constexpr (EIGHT || BN_ < 256)                                                                        \
+      hipLaunchKernelGGL((dense_q_pair_kernel<Y, EIGHT, BN_>), grid, block, 0, s, a, m_tiles, vec);      \
+    break;
+  switch (best) {
+    MSK_TILE_CASE(0, 32, 32, 2, 2, 4)
+    MSK_TILE_CASE(1, 64, 64, 2, 2, 3)
+    MSK_TILE_CASE(2, 128, 128, 2, 4, 4)
+    MSK_PAIR_CASE(3, 128)
+    MSK_PAIR_CASE(4, 192)
+    MSK_PAIR_CASE(5, 256)
+  }
+#undef MSK_TILE_CASE
+#undef MSK_PAIR_CASE
+  return hipGetLastError() == hipSuccess ? MS_OK : MS_E_HIP;
+}
+
+// Blocks of 16 outputs per work-group: the fewest, up to four, whose work-groups have a CU each;
+// waves: eight where they have, else four.  us with 1 | 2 | 4 blocks, one token: 4096 -> 4096 5.5 |
+// 6.5 | 10.3, 4096 -> 6144 7.0 | 6.5 | 10.4, 4096 -> 32000 23.9 | 22.7 | 20.4, 16 tokens: 6.8 | 8.2
+// | 11.8, 10.8 | 8.3 | 11.8, 38 | 27 | 22.7.  With more than one stage in flight per wave they
+// were no faster, and fewer of them fit.
+template <typename Y, int NT>
+void launch_few(const DenseArgs& a, int vec, hipStream_t s) {
+  const unsigned blocks = (a.n_out - 1) / 16 + 1;
+  if (blocks <= kCus)
+    hipLaunchKernelGGL((dense_q_few_kernel<Y, 8, 1, NT>), dim3(blocks), dim3(512), 0, s, a, vec);
+  else if (blocks <= 2 * kCus)
+    hipLaunchKernelGGL((dense_q_few_kernel<Y, 8, 2, NT>), dim3((blocks + 1) / 2), dim3(512), 0, s, a, vec);
+  else if constexpr (NT < 4)
+    hipLaunchKernelGGL((dense_q_few_kernel<Y, 4, 4, NT>), dim3((blocks + 3) / 4), dim3(256), 0, s, a, vec);
+  else
+    hipLaunchKernelGGL((dense_q_few_kernel<Y, 4, 2, NT>), dim3((blocks + 1) / 2), dim3(256), 0, s, a, vec);
+}
+
+// Which calls dense_q_few_kernel takes: up to 16 tokens all, up to 64 those of short rows, and
+// up to 32 with fp32 results, us of it | tiles, fp32 and bf16 results: 16 tokens 4096 -> 4096 6.8 |
+// 11.8, 6.8 | 8.4; 32 tokens 4096 -> 6144 11.2 | 12.0, 11.2 | 8.5, 2048 -> 2048 5.1 | 7.8, 5.1 | 6.2;
+// 61 tokens 2000 -> 5003 6.8 | 9.2, 6.6 | 7.2; 64 tokens 4096 -> 4096 15.2 | 12.5, 15.9 | 8.7.
+bool takes_few(int T, int n_in, bool eight) { return T <= 16 || (T <= 64 && n_in <= 2048) || (T <= 32 && !eight); }
+
+template <typename Y, bool EIGHT>
+ms_status launch_dense_q(const DenseArgs& a, hipStream_t s) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.add);
+  const int vec = a.n_out % 4 == 0 && (at & (4 * sizeof(Y) - 1)) == 0;
+  if (!takes_few(a.T, a.n_in, EIGHT)) return launch_tiles<Y, EIGHT>(a, vec, s);
+  if (a.T <= 16)
+    launch_few<Y, 1>(a, vec, s);
+  else if (a.T <= 32)
+    launch_few<Y, 2>(a, vec, s);
+  else
+    launch_few<Y, 4>(a, vec, s);
+  return hipGetLastError() == hipSuccess ? MS_OK : MS_E_HIP;
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -437,15 +974,8 @@ ms_status ms_dense_q(const void* x, const void* x_exp, const void* w, const void
     return MS_E_INVALID;
   const DenseArgs a = {static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(x_exp), static_cast<const uint8_t*>(w),
                        static_cast<const uint8_t*>(w_exp), add, y, T, n_in, n_out, static_cast<int>(nb)};
-  const int64_t tiles = (static_cast<int64_t>(n_out) + 15) / 16;
-  if (tiles > 65535 * int64_t{64}) return MS_E_UNSUPPORTED;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const dim3 grid((T + 15) / 16, static_cast<unsigned>(tiles));
-  if (y_dtype == MS_F32)
-    hipLaunchKernelGGL(dense_q_simple_kernel<float>, grid, dim3(64), msk::kGuardLds, s, a);
-  else
-    hipLaunchKernelGGL(dense_q_simple_kernel<uint16_t>, grid, dim3(64), msk::kGuardLds, s, a);
-  return launched();
+  return y_dtype == MS_F32 ? launch_dense_q<float, false>(a, s) : launch_dense_q<uint16_t, true>(a, s);
 }
 
 }  // extern "C"

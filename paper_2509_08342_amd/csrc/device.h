@@ -48,6 +48,20 @@ __device__ __forceinline__ void lds_load16(const void* g, uint32_t lds) {
       : "memory");
 }
 
+// The same from a uniform address and 32-bit offsets.
+__device__ __forceinline__ void lds_load16(const void* base, uint32_t offset, uint32_t lds) {
+  uint32_t keep;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %3\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(keep)
+      : "v"(offset), "s"(base), "s"(lds)
+      : "memory");
+}
+
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)(p)));
 }
