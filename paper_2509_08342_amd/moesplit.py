@@ -530,7 +530,10 @@ _VALUE_TYPES = {"torch.float32": (MS_F32, 4), "torch.bfloat16": (MS_BF16, 2)}
 def _value_type(x, name):
     """(MS_F32 or MS_BF16, its size) of a tensor."""
     try:
-        return _VALUE_TYPES[str(x.dtype)]
+        t = _VALUE_TYPES.get(x.dtype)
+        if t is None:  # the first of its type
+            t = _VALUE_TYPES[x.dtype] = _VALUE_TYPES[str(x.dtype)]
+        return t
     except (AttributeError, KeyError):
         raise ValueError("%s: a float32 or bfloat16 tensor expected" % name) from None
 
