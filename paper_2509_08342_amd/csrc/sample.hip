@@ -61,8 +61,7 @@ struct Scale {
   // exp((l - top) / temperature) in units: 2^(-j / kPowers) from the table and the series of the
   // rest, |r| <= 1/2, to its fourth power (the next term is 2^-54)
   __device__ __forceinline__ uint64_t weight(float l) const {
-    const double y = (static_cast<double>(top) - l) * inv;
-    if (!(y < kFar)) return 0;
+    const double y = fmin((static_cast<double>(top) - l) * inv, kFar + kPowers);  // (NaN, of an endless temperature, too)
     constexpr double L = 0.69314718055994530942 / kPowers;
     const double j = rint(y), r = y - j;
     double s = fma(r, L * L * L * L / 24, -L * L * L / 6);
@@ -116,8 +115,8 @@ struct Shared {
 // Bin b's place: a thread's bins, which follow each other, lie kThreads apart.
 template <int BINS>
 __device__ __forceinline__ int place(int b) {
-  constexpr int PER = BINS / kThreads;
-  return b % PER * kThreads + b / PER;
+  constexpr unsigned PER = BINS / kThreads;
+  return static_cast<unsigned>(b) % PER * kThreads + static_cast<unsigned>(b) / PER;
 }
 
 // Exclusive sums of mass and count in place; the totals to sh.all and sh.all_count.  Returns
@@ -328,6 +327,19 @@ struct Logits {
       }
     }
   }
+  // f(four logits)
+  template <typename F>
+  __device__ __forceinline__ void fours(F f) {
+    for (int from = i0; from < i1; from += kHold * kThreads) {
+      if (!once()) fetch(from);
+#pragma unroll
+      for (int g = 0; g < kHold; g += 4) {
+        if (from + g * kThreads >= i1) break;
+        const float x[4] = {hold[g], hold[g + 1], hold[g + 2], hold[g + 3]};
+        f(x);
+      }
+    }
+  }
 };
 
 // The largest and the smallest of a work-group's logits.
@@ -352,7 +364,7 @@ struct Settings {
   float temp, drawn, p, min_p;
   int k;
   bool by_k, by_p, by_min;
-  double least;  // units that min_p asks for
+  uint64_t least;  // units that min_p asks for
 
   __device__ __forceinline__ Settings(const SampleArgs& a, int t)
       : temp(a.temperature ? a.temperature[t] : 1.0f),
@@ -363,7 +375,7 @@ struct Settings {
         by_k(k > 0 && k < a.n),
         by_p(p < 1.0f),
         by_min(min_p > 0.0f),
-        least(fmin(static_cast<double>(min_p), 1.0) * kUnit) {}
+        least(by_min ? static_cast<uint64_t>(ceil(fmin(static_cast<double>(min_p), 1.0) * kUnit)) : 0) {}
   __device__ __forceinline__ double number() const { return fmin(fmax(drawn, 0.0f), 0x1.fffffep-1f); }  // NaN draws as 0
   __device__ __forceinline__ double share() const { return fmax(static_cast<double>(p), 0.0); }
   __device__ __forceinline__ bool greedy(float top) const { return !(temp > 0.0f) || top == -INFINITY; }
@@ -398,15 +410,29 @@ __device__ __forceinline__ void count_token(Shared& sh, int b) {
 template <bool COUNT>
 __device__ __forceinline__ void weigh(Shared& sh, const Scale& sc, const Settings& st, Logits& l, int last) {
   uint64_t kept = 0;
-  l.every([&](float x, int) {
-    const int b = sc.bin(x), at = place<kBins>(b);
-    if (COUNT && st.by_k) count_token(sh, b);
-    if (b > last) return;
-    const uint64_t w = sc.weight(x);
-    if (!w) return;
-    atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[at]), w);
-    if (st.by_min && static_cast<double>(w) >= st.least) kept += w;
-  });
+  auto add = [&](int b, uint64_t w) {
+    atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[place<kBins>(b)]), w);
+    kept += w >= st.least ? w : 0;
+  };
+  if (last < kBins - 1) {  // few
+    l.every([&](float x, int) {
+      const int b = sc.bin(x);
+      if (b > last) return;
+      if (const uint64_t w = sc.weight(x)) add(b, w);
+    });
+  } else {
+    l.fours([&](const float (&x)[4]) {  // a token's chain of operations beside the others'
+      uint64_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = sc.weight(x[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int b = sc.bin(x[i]);
+        if (COUNT && st.by_k) count_token(sh, b);
+        if (w[i]) add(b, w[i]);
+      }
+    });
+  }
   if (st.by_min) {
 #pragma unroll
     for (int s = 32; s >= 1; s >>= 1) kept += __shfl_xor(static_cast<unsigned long long>(kept), s, 64);
@@ -626,14 +652,14 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs a) {
   SplitRow& ws = split_row(a, t);
   Logits l = share_of(a, s, t);
   const Settings st(a, t);
+#pragma unroll
+  for (int b = 0; b < kBins; b += kThreads) sh.mass[b + tid] = ws.mass[b + tid], sh.count[b + tid] = ws.count[b + tid];
+  if (tid == 0) sh.least = ws.least;
   tabulate(sh);
   float2 r = ws.whole(a.splits);
   if (st.greedy(r.x)) return;
   if (r.x == INFINITY) l.make_infinite(), r = make_float2(0.0f, -INFINITY);
   const Scale sc = st.scale(sh, r.x, r.y);
-#pragma unroll
-  for (int b = 0; b < kBins; b += kThreads) sh.mass[b + tid] = ws.mass[b + tid], sh.count[b + tid] = ws.count[b + tid];
-  if (tid == 0) sh.least = ws.least;
   __syncthreads();
   int bk = -1;
   if (st.by_k) {

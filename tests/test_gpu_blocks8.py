@@ -100,7 +100,7 @@ def test_quant_of_extreme_values(block_rows):
 
 # --------------------------------------------------------------------- norm
 
-@pytest.mark.parametrize("T,d", [(1, 16), (1, 4096), (3, 144), (7, 2000), (2, 16384), (33, 8192), (5, 2064), (300, 256)])
+@pytest.mark.parametrize("T,d", [(1, 16), (1, 4096), (3, 144), (7, 2000), (2, 16384), (33, 8192), (5, 2064), (300, 256), (5, 1024), (4, 528)])
 @pytest.mark.parametrize("y_dtype,gain", [("f32", False), ("bf16", True), (None, True), (None, False)])
 def test_norm(T, d, y_dtype, gain):
     ms = _ms()
@@ -327,3 +327,94 @@ def test_a_run_of_them():
         graph.replay()
         torch.cuda.synchronize()
         check(hf)
+
+
+# ------------------------------------------------------------- the decoder
+
+def _decoder(P, **kw):
+    from decoder import Decoder
+    shape, attn = synth.ModelShape("dec-tiny", 2, 256, 512, 8, 2, "bf16"), synth.TINY_ATTN
+    return shape, attn, Decoder(shape, attn, seed=4, n_sets=2, max_tokens=P, max_ctx=P + 20,
+                                budget_total=2 * 8 * shape.expert_bytes, dense_bits=8, **kw)
+
+
+def _ready(dec):
+    from workload import top_bytes
+    ms = _ms()
+    dec.stack.configure(0.5, 2 * 4 * top_bytes(dec.stack.rig, 0.5))
+    for l in range(2):
+        dec.stack.rig.load_tops(l, [0, 1, 2, 3])
+    ms.ms_sync(dec.ctx)
+
+
+@pytest.mark.parametrize("kv_bits", [16, 8])
+def test_decoder_in_8_bits(kv_bits):
+    """A two-layer decoder around the experts with dense_bits=8, a prompt and drawn tokens: every layer's attention module
+    against the oracle from the layer's input, with weights and activations quantized as the library says, and the logits
+    from the codes of the last layer's result; the token from those logits."""
+    from decoder import Sampling
+    from gpu_helpers import check_close
+    from oracle import decoder as od
+    from oracle import sample as osm
+    P, n_dec = 70, 4
+    shape, attn, dec = _decoder(P, kv_bits=kv_bits)
+    Hq, Hkv, D = attn.n_heads, attn.n_kv_heads, attn.head_dim
+    settings = dict(temperature=0.8, top_k=40, top_p=0.95, min_p=0.01)
+    with dec:
+        _ready(dec)
+        draw = Sampling(attn.vocab, seed=7, n=3, **settings)
+        quantized = lambda w: b8.values(*b8.quantize(w.astype(np.float64), 128), 128)  # noqa: E731
+        weights = [[quantized(w) for w in dec.f32[s]] for s in range(dec.n_sets)]
+        x = torch.empty(P, shape.d_model, dtype=torch.bfloat16, device="cuda")
+        x1 = torch.empty(1, shape.d_model, dtype=torch.bfloat16, device="cuda")
+        dec.embed_ids(torch.from_numpy(synth.prompt_tokens(attn, 4, P)).cuda(), P, x)
+        caches = [od.Cache(Hkv, P + 20, D) for _ in range(2)]
+        for step in range(1 + n_dec):
+            T, pos0 = (P if step == 0 else 1), dec.pos
+            cap = dec.step(x if step == 0 else x1, T, capture=(0, 1), sampling=draw)
+            torch.cuda.synchronize()
+            for l in range(2):
+                xin = cap[l]["x"].astype(np.float64)
+                w_qkv, w_o = weights[l % dec.n_sets]
+                # the library's codes are of the norm before its rounding to bf16, the oracle's of bf16 (a few move by one
+                # step), and the 8-bit cache's values are off by 2^-4 at most: of an attention module's result, which the
+                # weights leave under a third of the layer's largest value, that is averaged over rows of 64 and more
+                a = od.attention(b8.values(*b8.quantize(xin)), w_qkv, w_o, caches[l], pos0, Hq, Hkv, D, attn.rope_base)
+                att = b8.dense(b8.values(*b8.quantize(a["o"])), w_o)[0]
+                check_close(cap[l]["h"], od.bf16_round(od.rmsnorm(xin + att)), "bf16", "step %d layer %d h" % (step, l))
+            last = b8.values(*[t[T - 1:T].cpu().numpy() for t in dec.xq])
+            ref, mags = b8.dense(last, quantized(dec.head_f32))
+            logits = dec.logits.cpu().numpy().astype(np.float64)
+            assert np.all(np.abs(logits - ref) <= 16 * 2.0 ** -23 * mags)
+            token, share, near = osm.draw(logits[0], draw.numbers[draw.used - 1].item(), **{
+                k: np.float64(np.float32(v)) if k != "top_k" else v for k, v in settings.items()})
+            if near > 1e-9:
+                assert int(dec.ids[0]) == token and abs(float(dec.prob[0]) - share) <= 2.0 ** -23
+            dec.embed_ids(dec.ids, 1, x1)
+        assert dec.pos == P + n_dec
+
+
+def test_decoder_in_8_bits_allocates_nothing_and_repeats():
+    """Steps on a stream that is not the current one allocate no device memory; the same seed draws the same tokens."""
+    from decoder import Sampling
+    _, attn, dec = _decoder(40, kv_bits=8, keep_f32=False)
+    with dec:
+        _ready(dec)
+        prompt = synth.prompt_tokens(attn, 1, 40)
+        stream = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        got = []
+        for _ in range(2):
+            dec.reset()
+            draw = Sampling(attn.vocab, temperature=1.5, top_p=0.9, seed=3, n=4)
+            got.append(dec.generate(prompt, 9, stream=stream, sampling=draw)[0])
+        assert got[0] == got[1] and all(0 <= t < attn.vocab for t in got[0])
+        dec.reset()
+        x = torch.randn(1, 256, device="cuda").to(torch.bfloat16)
+        torch.cuda.synchronize()
+        dec.step(x, 1, stream=stream, sampling=draw)
+        before = torch.cuda.memory_stats()["allocation.all.allocated"]
+        for _ in range(12):
+            dec.step(x, 1, stream=stream, sampling=draw)
+        stream.synchronize()
+        assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
