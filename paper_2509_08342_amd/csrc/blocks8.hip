@@ -406,6 +406,14 @@ constexpr int kTileExps = 16384;         // exponents of a tile's tokens that fi
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
+// Tile w of a launch: an XCD takes neighbouring ones, and of up to four blocks of tokens the
+// blocks of outputs follow each other, so that the tiles of a moment share both.
+__device__ __forceinline__ int2 tile_of(int w, int n, int m_tiles) {
+  const int i = msk::xcd_local(w, n), wide = n / m_tiles, band = 4 * wide;
+  const int m0 = i / band * 4, rows = min(m_tiles - m0, 4), at = i % band;
+  return make_int2(m0 + at % rows, at / rows);
+}
+
 // The exponents of a tile's tokens t0 .. t0 + BM - 1, put(token, block of columns, exponent): the
 // rows follow each other in memory, and eight are requested before the first is used.
 template <int BM, int THREADS, typename Put>
@@ -438,8 +446,8 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q_tile_kernel(DenseArgs a,
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wv % WM, wn = wv / WM;
-  const int tile = msk::xcd_local(blockIdx.x, gridDim.x);
-  const int t0 = (tile % m_tiles) * BM, o0 = (tile / m_tiles) * BN;
+  const int2 tile = tile_of(blockIdx.x, gridDim.x, m_tiles);
+  const int t0 = tile.x * BM, o0 = tile.y * BN;
   const int lrow = lane >> 3, lk = 16 * ((lane & 7) ^ lrow);
   const uint8_t* src[NL];  // staged rows: the tile's BM tokens, then its BN outputs
 #pragma unroll
@@ -569,9 +577,9 @@ __global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool second = wv >= 4;
   const int wm = wv % WM, wn = wv / WM;
-  const int tile = msk::xcd_local(blockIdx.x, gridDim.x);
-  // (the division is the vector unit's)
-  const int t0 = __builtin_amdgcn_readfirstlane(tile % m_tiles * BM), o0 = __builtin_amdgcn_readfirstlane(tile / m_tiles * BN);
+  const int2 tile = tile_of(blockIdx.x, gridDim.x, m_tiles);
+  // (the divisions are the vector unit's)
+  const int t0 = __builtin_amdgcn_readfirstlane(tile.x) * BM, o0 = __builtin_amdgcn_readfirstlane(tile.y) * BN;
   const uint8_t *x0 = a.x + static_cast<size_t>(t0) * a.n_in, *w0 = a.w + static_cast<size_t>(o0) * a.n_in;
 
   // Staged rows: the tile's tokens, then its outputs, the last of either again.  Piece p of a
@@ -602,6 +610,8 @@ __global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m
   };
 #pragma unroll
   for (int j = 0; j < NL; ++j) issue(0, j);
+#pragma unroll
+  for (int j = 0; j < NL; ++j) issue(1, j);
   stage_exponents<BM, 64 * NWV>(a, t0, [&](int r, int b, uint8_t e) {
     xe[b * BM + (r / (16 * TM) * 16 + r % 16) * TM + r / 16 % TM] = e;
   });
@@ -668,6 +678,7 @@ __global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m
   auto pin = []() { __builtin_amdgcn_sched_barrier(0); };
   auto multiply = [&](auto load) {
     int j = 0;
+    __builtin_amdgcn_s_setprio(1);
     if constexpr (EIGHT) {
       auto codes = [](const uint4 (&p)[2]) {
         return i32x8_t{static_cast<int>(p[0].x), static_cast<int>(p[0].y), static_cast<int>(p[0].z), static_cast<int>(p[0].w),
@@ -705,6 +716,7 @@ __global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m
     for (int n = 0; n < TN; ++n)
 #pragma unroll
       for (int m = 0; m < TM; ++m) asm volatile("" : "+v"(acc[n][m]));  // here, and not behind a barrier or wait
+    __builtin_amdgcn_s_setprio(0);
   };
   auto change = [&]() {  // to the next phase
     pin();
@@ -713,27 +725,26 @@ __global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m
   };
   msk::wait_vm<0>();
   clear_ends(0);
-  __syncthreads();  // the first stage and the exponents are there
+  clear_ends(1);
+  __syncthreads();  // two stages and the exponents are there
   auto none = [](int) {};
   if (second) {
-#pragma unroll
-    for (int j = 0; j < NL; ++j) issue(1, j);
     change();
     for (int sl = 0; sl < a.nb; ++sl) {
       read(sl, none);
       msk::wait_vm<0>();
-      clear_ends(sl + 1);
+      if (sl > 0) clear_ends(sl + 1);
       change();
-      multiply([&](int j) { pin(); issue(sl + 2, j); pin(); });
+      multiply([&](int j) { issue(sl + 2, j); });
       change();
     }
   } else {
     for (int sl = 0; sl < a.nb; ++sl) {
-      read(sl, [&](int j) { issue(sl + 1, j); });
+      read(sl, [&](int j) { if (sl > 0) issue(sl + 1, j); });
       change();
       multiply(none);
       msk::wait_vm<0>();
-      clear_ends(sl + 1);
+      if (sl > 0) clear_ends(sl + 1);
       change();
     }
     change();
@@ -807,22 +818,34 @@ ms_status launch_tiles(const DenseArgs& a, int vec, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? MS_OK : MS_E_HIP;
 }
 
-// Blocks of 16 outputs per work-group: the fewest, up to four, whose work-groups have a CU each;
-// waves: eight where they have, else four.  us with 1 | 2 | 4 blocks, one token: 4096 -> 4096 5.5 |
-// 6.5 | 10.3, 4096 -> 6144 7.0 | 6.5 | 10.4, 4096 -> 32000 23.9 | 22.7 | 20.4, 16 tokens: 6.8 | 8.2
-// | 11.8, 10.8 | 8.3 | 11.8, 38 | 27 | 22.7.  With more than one stage in flight per wave they
-// were no faster, and fewer of them fit.
+// Blocks of 16 outputs per work-group, and waves.  us with 1 x 8 | 2 x 8 | 2 x 16 | 4 x 4, weights
+// not in the caches: one token 4096 -> 4096 5.5 | 6.5 | 6.7 | 10.3 (cached), 4096 -> 6144 8.4 | 7.4 |
+// 7.9 | 12.3, 4096 -> 14336 15.1 | 14.3 | 13.3 | 14.5, 4096 -> 32000 30.3 | 26.6 | 24.5 | 29.7, 1024 ->
+// 32000 7.6 | 7.6 | 9.6 | 8.2; 16 tokens 4096 -> 6144 12.4 | 9.2 | 9.5 | 13.2, -> 32000 40.0 | 32.0 | 31.0 |
+// 31.4.  Long rows of one token want one block and sixteen waves, 8192 -> 8192 14.2 for 18.1
+// with 2 x 16, and of 16 tokens not, 21.1 for 18.1.  32 tokens 4096 -> 32000 46.4 with 2 x 8, 34.5
+// with 4 x 8; 64 tokens 2048 -> 32000 30.5 and 25.9 (4 x 4).
 template <typename Y, int NT>
 void launch_few(const DenseArgs& a, int vec, hipStream_t s) {
   const unsigned blocks = (a.n_out - 1) / 16 + 1;
-  if (blocks <= kCus)
-    hipLaunchKernelGGL((dense_q_few_kernel<Y, 8, 1, NT>), dim3(blocks), dim3(512), 0, s, a, vec);
-  else if (blocks <= 2 * kCus)
-    hipLaunchKernelGGL((dense_q_few_kernel<Y, 8, 2, NT>), dim3((blocks + 1) / 2), dim3(512), 0, s, a, vec);
-  else if constexpr (NT < 4)
-    hipLaunchKernelGGL((dense_q_few_kernel<Y, 4, 4, NT>), dim3((blocks + 3) / 4), dim3(256), 0, s, a, vec);
-  else
-    hipLaunchKernelGGL((dense_q_few_kernel<Y, 4, 2, NT>), dim3((blocks + 1) / 2), dim3(256), 0, s, a, vec);
+#define MSK_FEW(KW_, MO_)                                                                                              \
+  hipLaunchKernelGGL((dense_q_few_kernel<Y, (KW_), (MO_), NT>), dim3((blocks + (MO_) - 1) / (MO_)), dim3(64 * (KW_)), 0, s, \
+                     a, vec)
+  if (blocks <= kCus) {
+    MSK_FEW(8, 1);
+  } else if constexpr (NT == 1) {
+    if (a.n_in > 4096 && a.T <= 4)
+      MSK_FEW(16, 1);
+    else if (a.n_in > 4096 || (a.n_in > 2048 && blocks > 2 * kCus))
+      MSK_FEW(16, 2);
+    else
+      MSK_FEW(8, 2);
+  } else if (blocks <= 2 * kCus) {
+    MSK_FEW(8, 2);
+  } else {
+    MSK_FEW(NT == 2 ? 8 : 4, 4);
+  }
+#undef MSK_FEW
 }
 
 // Which calls dense_q_few_kernel takes: up to 16 tokens all, up to 64 those of short rows, and
