@@ -26,6 +26,7 @@ constexpr int kExpBias = 127;
 constexpr int kExpMin = -40, kExpMax = 40;
 constexpr float kCodeMax = 448.0f;
 constexpr int kMostColumns = 16384;
+constexpr int kMostOutputs = 1 << 25, kMostRows = 1 << 24;  // of a launch
 
 __device__ __forceinline__ uint32_t bf16_bits(float f) {
   return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f));  // to nearest even, NaN stays NaN
@@ -972,6 +973,7 @@ ms_status ms_residual_norm_q(const void* h, const void* y, int32_t y_dtype, cons
   a.T = T;
   a.d = d;
   a.nb = static_cast<int>(nb);
+  if (T > kMostRows - 1) return MS_E_UNSUPPORTED;
   if (y_dtype == MS_F32)
     launch_norm<float>(a, static_cast<hipStream_t>(stream));
   else
@@ -992,6 +994,7 @@ ms_status ms_dense_q(const void* x, const void* x_exp, const void* w, const void
     return MS_E_INVALID;
   const DenseArgs a = {static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(x_exp), static_cast<const uint8_t*>(w),
                        static_cast<const uint8_t*>(w_exp), add, y, T, n_in, n_out, static_cast<int>(nb)};
+  if (n_out > kMostOutputs) return MS_E_UNSUPPORTED;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   return y_dtype == MS_F32 ? launch_dense_q<float, false>(a, s) : launch_dense_q<uint16_t, true>(a, s);
 }

@@ -3,8 +3,10 @@
 //
 // With the logits l in descending order, ties to the lower index, and weights
 // exp((l - max) / temperature), every filter keeps a prefix, so the kept mass M is the least
-// of the filters' masses, and the token is the first whose running mass passes u M.  No row
-// is sorted: a histogram over the distance from the maximum gives the running mass at 2048
+// of the filters' masses, and the token is the first whose running mass passes u M: top-k
+// keeps the mass of the first k, top-p of the fewest that reach p of that, min-p of the weights
+// from min-p on.  No row
+// is sorted: a histogram over the distance from the maximum gives the running mass at 8192
 // borders; only the tokens of the few bins in which a filter or the drawn mass ends are
 // gathered, and each of them finds its own running mass by comparing itself with the others.
 //
@@ -30,7 +32,7 @@ constexpr int kList = kThreads;  // gathered tokens
 constexpr int kSubBins = 1024;   // of rows whose tokens crowd into few bins
 constexpr int kMostTokens = (1 << 19) - 1;  // n 2^45 < 2^64
 constexpr double kUnit = 35184372088832.0;  // 2^45
-constexpr int kCus = 256;
+constexpr int kCus = 256, kXcds = 8;
 constexpr double kFar = 46 * 256;  // 2^-46 rounds to zero units (in 256ths of powers of two)
 constexpr int kHold = 32;          // logits of a thread in registers at a time
 
@@ -81,7 +83,7 @@ struct SampleArgs {
   const int32_t* top_k;
   int32_t* idx;
   float* prob;
-  int n;
+  int T, n;
   int splits, share;  // work-groups of a row, and their logits
   void* workspace;
 };
@@ -607,9 +609,20 @@ __device__ __forceinline__ Logits share_of(const SampleArgs& a, int s, int t) {
   return Logits(a.logits + static_cast<size_t>(t) * a.n, min(s * a.share, a.n), min((s + 1) * a.share, a.n));
 }
 
+// A work-group's part and row.  Work-groups go to the 8 XCDs in turn, and a row's stay on one: its
+// L2 has what the launch before read and what the others wrote.
+struct Part {
+  int s, t;
+};
+__device__ __forceinline__ Part part_of(const SampleArgs& a) {
+  const int i = blockIdx.x / kXcds;
+  return {i % a.splits, i / a.splits * kXcds + static_cast<int>(blockIdx.x % kXcds)};
+}
+
 __global__ __launch_bounds__(kThreads) void sample_range_kernel(SampleArgs a) {
   __shared__ Shared sh;
-  const int s = blockIdx.x % a.splits, t = blockIdx.x / a.splits;
+  const auto [s, t] = part_of(a);
+  if (t >= a.T) return;
   SplitRow& ws = split_row(a, t);
   Logits l = share_of(a, s, t);
   for (int b = s * kThreads + static_cast<int>(threadIdx.x); b < kBins; b += a.splits * kThreads) ws.mass[b] = 0, ws.count[b] = 0;
@@ -620,7 +633,9 @@ __global__ __launch_bounds__(kThreads) void sample_range_kernel(SampleArgs a) {
 
 __global__ __launch_bounds__(kThreads) void sample_weigh_kernel(SampleArgs a) {
   __shared__ Shared sh;
-  const int s = blockIdx.x % a.splits, t = blockIdx.x / a.splits, tid = threadIdx.x;
+  const auto [s, t] = part_of(a);
+  const int tid = threadIdx.x;
+  if (t >= a.T) return;
   SplitRow& ws = split_row(a, t);
   Logits l = share_of(a, s, t);
   const Settings st(a, t);
@@ -648,7 +663,9 @@ __global__ __launch_bounds__(kThreads) void sample_weigh_kernel(SampleArgs a) {
 
 __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs a) {
   __shared__ Shared sh;
-  const int s = blockIdx.x % a.splits, t = blockIdx.x / a.splits, tid = threadIdx.x;
+  const auto [s, t] = part_of(a);
+  const int tid = threadIdx.x;
+  if (t >= a.T) return;
   SplitRow& ws = split_row(a, t);
   Logits l = share_of(a, s, t);
   const Settings st(a, t);
@@ -697,10 +714,13 @@ __global__ __launch_bounds__(kThreads) void sample_choose_kernel(SampleArgs a) {
 }
 
 // Work-groups of a row: one where it holds the row in registers, else as many as leave one a
-// CU, of at least kLeastShare logits each.
+// CU of the XCD that the row's are on, of at least kLeastShare logits each.  One | several, us:
+// one row of 50257 47 | 28, of 131071 73 | 29; 64 rows of 131071 95 | 53; 128 rows of 131071 100 | 86;
+// but of 32000 one row 18 | 29, 64 rows 19 | 44, 128 rows 19 | 50.
 constexpr int kLeastShare = 4096;
 int splits_of(int T, int n) {
-  return n <= kHold * kThreads ? 1 : std::max(1, std::min(kCus / std::max(T, 1), n / kLeastShare));
+  const int rows = (std::max(T, 1) - 1) / kXcds + 1;  // of an XCD
+  return n <= kHold * kThreads ? 1 : std::max(1, std::min(kCus / kXcds / rows, n / kLeastShare));
 }
 
 }  // namespace
@@ -725,10 +745,10 @@ ms_status ms_sample(const float* logits, int32_t T, int32_t n, const ms_sample_o
     return MS_E_INVALID;
   if (T > UINT32_MAX / kThreads) return MS_E_UNSUPPORTED;
   const int splits = splits_of(T, n);
-  SampleArgs a = {logits, u_dev, nullptr, nullptr, nullptr, nullptr, idx_out, prob_out, n, splits, (n - 1) / splits + 1, workspace_dev};
+  SampleArgs a = {logits, u_dev, nullptr, nullptr, nullptr, nullptr, idx_out, prob_out, T, n, splits, (n - 1) / splits + 1, workspace_dev};
   if (opts) a.temperature = opts->temperature_dev, a.top_p = opts->top_p_dev, a.min_p = opts->min_p_dev, a.top_k = opts->top_k_dev;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const dim3 rows(static_cast<unsigned>(T)), all(static_cast<unsigned>(T) * splits), block(kThreads);
+  const dim3 rows(static_cast<unsigned>(T)), all((static_cast<unsigned>(T) + kXcds - 1) / kXcds * kXcds * splits), block(kThreads);
   if (splits == 1) {
     hipLaunchKernelGGL(sample_kernel, rows, block, 0, s, a);
   } else {

@@ -115,6 +115,8 @@ def test_norm_refusals():
     assert _status(n, both[:T * d], y, None, 1e-6, T, d, out=both[d:d + T * d]) == ms.MS_E_INVALID  # another row's values
     assert _status(n, h, y, None, 1e-6, T, d, out=y.view(torch.bfloat16).view(-1)[:T * d]) == ms.MS_E_INVALID
     assert _status(n, h, y, None, 1e-6, T, d, codes=h.view(torch.uint8).view(-1)[:T * d], exps=e) == ms.MS_E_INVALID
+    assert ms.lib.ms_residual_norm_q(1 << 44, None, ms.MS_F32, None, 1e-6, 1 << 24, 16, None, 1 << 45, None, None,
+                                     None) == ms.MS_E_UNSUPPORTED
     ms.ms_residual_norm_q(_z(0, d, dtype=torch.bfloat16), None, None, 1e-6, 0, d, out=_z(0, d, dtype=torch.bfloat16))
     for bad in (dict(h=h[:2]), dict(h=h.float()), dict(y=y.half()), dict(y=y[:2]), dict(weight=out[0, :100]),
                 dict(out=out[:1]), dict(codes=c[:2], exps=e), dict(codes=c, exps=e[:2])):
@@ -144,6 +146,8 @@ def test_dense_refusals():
     assert _status(f, x, xe, w, we, T, n_in, n_out, wide[:T * n_out], add=wide[1:1 + T * n_out]) == ms.MS_E_INVALID
     room = torch.zeros(T * n_out * 4 + 64, dtype=torch.uint8)  # results over the tokens' codes
     assert _status(f, room[:T * n_in], xe, w, we, T, n_in, n_out, room[:T * n_out * 4].view(torch.float32)) == ms.MS_E_INVALID
+    p = [t.data_ptr() for t in (x, xe, w, we)]  # more outputs, and rows, than a launch may have
+    assert ms.lib.ms_dense_q(*p, 1, 16, (1 << 25) + 1, 1 << 44, ms.MS_F32, None, None) == ms.MS_E_UNSUPPORTED
     f(_z(0, n_in), _z(0, 2), w, we, 0, n_in, n_out, _z(0, n_out, dtype=torch.float32))
     for bad in (dict(x=x[:2]), dict(xe=xe[:2]), dict(w=w[:100]), dict(we=we[:1]), dict(y=y[:2]), dict(y=y.half()),
                 dict(add=y[:2]), dict(add=y.bfloat16()), dict(w=w.t())):

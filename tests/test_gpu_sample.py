@@ -129,6 +129,27 @@ def test_extreme_rows():
         _check(rows, np.full(T, u), top_k=np.arange(T), top_p=np.full(T, 0.5), min_p=np.full(T, 0.5))
 
 
+@pytest.mark.parametrize("n", [3000, 32768, 32769, 70001])
+def test_extreme_values_in_long_rows(n):
+    """Greedy rows, rows without a logit above -infinity, infinite maxima and ties at the ends of the work-groups' parts,
+    rows whose other logits are all far below, NaN among them."""
+    rng = np.random.default_rng(n)
+    x = (2 * rng.standard_normal((9, n))).astype(np.float32)
+    x[0] = np.nan
+    x[1] = -np.inf
+    x[2, [n - 1, n // 2, 7]] = np.inf
+    x[3, rng.random(n) < 0.3] = np.nan
+    x[4, [n - 1, n // 3]] = 50.0
+    x[5] = -1e30
+    x[5, n - 2] = 3.0
+    x[6, :n - 1] = -np.inf
+    x[7, n // 2:] = -np.inf
+    for u in (0.0, 0.4, 0.67, 1 - 2.0 ** -24):
+        _check(x, np.full(9, u))
+        _check(x, np.full(9, u), temperature=np.zeros(9), top_k=np.full(9, 5))
+        _check(x, np.full(9, u), top_k=np.full(9, 2), top_p=np.full(9, 0.9), min_p=np.full(9, 0.2))
+
+
 def test_filters_at_their_ends():
     """top_k of one, negative and past the row; top_p of nothing, all, more and NaN; min_p of one, more and NaN."""
     rng = np.random.default_rng(6)
@@ -155,12 +176,13 @@ def test_greedy_is_argmax():
     assert np.array_equal(idx, ref.cpu().numpy()) and np.all(prob == 1.0)
 
 
-def test_a_row_does_not_depend_on_its_batch():
+@pytest.mark.parametrize("n", [20011, 40009])
+def test_a_row_does_not_depend_on_its_batch(n):
     rng = np.random.default_rng(9)
-    T, n = 400, 20011
+    T = 400
     logits = (3 * rng.standard_normal((T, n))).astype(np.float32)
     s, u = _settings(rng, T), rng.random(T)
-    idx, prob = _run(logits, u, **s)
+    idx, prob = _run(logits, u, **s)  # a work-group per row; from n = 32769 on the smaller batches have several
     for t in (0, 17, 399):
         one = _run(logits[t:t + 1], u[t:t + 1], **{k: v[t:t + 1] for k, v in s.items()})
         assert one[0][0] == idx[t] and one[1][0] == prob[t]
@@ -168,7 +190,7 @@ def test_a_row_does_not_depend_on_its_batch():
     assert np.array_equal(some[0], idx[100:140]) and np.array_equal(some[1], prob[100:140])
 
 
-@pytest.mark.parametrize("T,n", [(1, 32000), (3, 7001), (200, 3001)])
+@pytest.mark.parametrize("T,n", [(1, 32000), (3, 7001), (200, 3001), (1, 40001), (11, 33000)])
 def test_captured_and_replayed(T, n):
     """A graph replayed with other logits, numbers and settings, the program's own work between the replays; two graphs
     with a workspace each on two streams at once."""
