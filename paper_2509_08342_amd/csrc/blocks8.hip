@@ -86,9 +86,10 @@ __device__ __forceinline__ uint32_t max_of_lanes(uint32_t v, int lanes) {  // gr
 
 // ----------------------------------------------------------------- rows to blocks
 //
-// Sixteen lanes take 128 columns of a row, eight values each.  ROWS = 1: a block is theirs.
-// ROWS = 128: a work-group takes a block, its values in registers until its largest
-// magnitude is known.
+// Sixteen lanes take 128 columns of a row, eight values each.  Blocks of one row are theirs; one
+// of 128 rows is a work-group's, its values in registers until its largest magnitude is known.
+// Bound by the bytes: 32000 x 4096 from bf16 (393 MB) 80 us, 4.9 TB/s, as fast as a copy; 4096
+// x 4096 10.9; a row of 4096 2.1.
 constexpr int kQuantThreads = 256;
 
 template <typename X>
@@ -152,10 +153,14 @@ __global__ __launch_bounds__(kQuantThreads) void quant_blocks_kernel(const X* __
 
 // ------------------------------------------------------------ residual and norm
 //
-// A work-group per row, sixteen lanes to 128 columns.  The sum of squares, the norm and the
-// choice of a block's exponent are in double precision (a code is the nearest to the exact
-// normalised value, and no exponent depends on how fp32 would have rounded next to a power
-// of two); h and y stay in registers between the two uses.
+// One to four waves per row, sixteen lanes to 128 columns; the sum h + y stays in registers
+// between its two uses.  The sum of squares and the norm are in double precision, and each value
+// is rounded once, to an fp32 that leaves the second rounding to bf16 or a code exact: a code is
+// the nearest to the exact normalised value, and no exponent depends on how fp32 would have
+// rounded next to a power of two.  2048 x 4096 with a bf16 y, gain, running sum and codes (75 MB)
+// 21 us, 3.6 TB/s, and 4096 rows 33; with an fp32 y and no running sum 17.  Between the bytes (15
+// us) and the double precision's instructions: the exponents chosen and codes made in it too
+// took 27.  A row of 4096 3.7 us: latency.
 constexpr int kNormThreads = 256;
 
 // d as fp32 that a second rounding, to bf16 or a code, cannot tell from d, nor a comparison
@@ -392,7 +397,7 @@ __global__ __launch_bounds__(64 * KW) void dense_q_few_kernel(DenseArgs a, int v
   }
 }
 
-// More: y^T = W x^T, a work-group takes BM tokens x BN outputs; both operands go to LDS as
+// Some tokens: y^T = W x^T, a work-group takes BM tokens x BN outputs; both operands go to LDS as
 // codes by direct loads (a row's 128 columns of a stage are a cache line; piece p of sixteen
 // codes of row r sits in slot p ^ (r % 8), so the lanes that an LDS read serves together hit
 // distinct banks), in a ring of NST stages.  WM x WN waves split the tile.
@@ -401,6 +406,9 @@ __global__ __launch_bounds__(64 * KW) void dense_q_few_kernel(DenseArgs a, int v
 // and the scales as they are, at twice the rate; they align the products of eight neighbouring
 // columns to about 2^-13 of the largest before they add them in fp32, which leaves 2e-5 of a
 // result, a hundredth of what its rounding to bf16 takes and too much for an fp32 one.
+//   Bound by the latency of a stage (loads, a barrier, LDS reads, then few matrix instructions
+// of a wave): 100 tokens 4096 -> 4096 15 us with fp32 results, 10.5 with bf16 ones; 512 tokens 4096
+// -> 6144 38 and 25 us.
 constexpr int kStageLoad = 64 * 16;      // one load: 8 rows
 constexpr int kRows16 = 16 * kBlock;     // bytes of 16 staged rows
 constexpr int kTileExps = 16384;         // exponents of a tile's tokens that fit: blocks of columns x BM
@@ -560,7 +568,18 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q_tile_kernel(DenseArgs a,
 // in a row they would hold up what stands behind them.
 //   A row of a matrix instruction's block n of outputs, for bf16 results, is one of 32 that
 // blocks n and n ^ 1 share, so that a lane ends with eight neighbouring outputs of a token
-// and four lanes with 64 bytes in a row (with fp32 results they do as it is).
+// and four lanes with 64 bytes in a row (with fp32 results they do as it is): 4096 tokens 128 ->
+// 14336, little but results, 51 us without and 37 with it.
+//   fp32 results: the tokens' codes become bf16 in the reading phase, the outputs' in the
+// multiplying one, a conversion or two behind every matrix instruction (in a row before them
+// they cost 84 us for 80 below), and a wave takes 64 x 64 to 64 x 96, which has the fewest
+// conversions to a product.
+//   2048 tokens 4096 -> 6144 fp32 79-85 us (1.2-1.3 PFLOP/s; a library product of bf16 matrices
+// 76), bf16 49 (2.1 PFLOP/s; a library product of e4m3 matrices with one scale 43); 4096 tokens
+// 4096 -> 14336 375 and 219 us (1.3 and 2.2 PFLOP/s; 314 and 182); 8192 cubed 905 and 420.  Of
+// the last but one's 1.4 us per stage and CU, the matrix instructions alone take 1.2 and the
+// loads alone 1.1 (15 TB/s from the L2s); a tile's start and end 8 us of 55.  Fetching stages ahead
+// into the L2, without waiting for them, made it slower (259 -> 292 us at the time).
 template <typename Y, bool EIGHT, int BN>
 __global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m_tiles, int vec) {
   constexpr int BM = 256, WM = EIGHT ? 2 : 4, NWV = 8, WN = NWV / WM;
