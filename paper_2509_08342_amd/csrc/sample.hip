@@ -5,10 +5,9 @@
 // exp((l - max) / temperature), every filter keeps a prefix, so the kept mass M is the least
 // of the filters' masses, and the token is the first whose running mass passes u M: top-k
 // keeps the mass of the first k, top-p of the fewest that reach p of that, min-p of the weights
-// from min-p on.  No row
-// is sorted: a histogram over the distance from the maximum gives the running mass at 8192
-// borders; only the tokens of the few bins in which a filter or the drawn mass ends are
-// gathered, and each of them finds its own running mass by comparing itself with the others.
+// from min-p on.  No row is sorted: a histogram over the distance from the maximum gives the
+// running mass at 4096 borders; only the tokens of the few bins in which a filter or the drawn
+// mass ends are gathered and sorted.
 //
 // Weights are whole numbers of 2^-45, computed in double precision: their sums do not depend
 // on the order of additions (so atomics may build them), and a border between two tokens is
@@ -27,20 +26,21 @@
 namespace {
 
 constexpr int kThreads = 1024;
-constexpr int kBins = 8192;
+constexpr int kWaves = kThreads / 64;  // as many as a row of lanes
+// (8192 bins sort fewer tokens and take longer to scan and merge: 64 rows of 131071 logits 44-50 us
+// rather than 40-43.)
+constexpr int kBins = 4096;
 constexpr int kList = kThreads;  // gathered tokens
 constexpr int kSubBins = 1024;   // of rows whose tokens crowd into few bins
 constexpr int kMostTokens = (1 << 19) - 1;  // n 2^45 < 2^64
 constexpr double kUnit = 35184372088832.0;  // 2^45
 constexpr int kCus = 256, kXcds = 8;
 constexpr double kFar = 46 * 256;  // 2^-46 rounds to zero units (in 256ths of powers of two)
-constexpr int kHold = 32;          // logits of a thread in registers at a time
 
-// A logit as it counts: NaN as -infinity; where the largest is infinite, its likes are 0 and all
-// others -infinity.
+// A logit as it counts: NaN where it is infinite (no comparison with NaN holds, and its weight is 0);
+// where the largest is infinite, its likes are 0 and all others NaN.
 __device__ __forceinline__ float logit(float x, bool infinite) {
-  if (infinite) x = x == INFINITY ? 0.0f : -INFINITY;
-  return x == x ? x : -INFINITY;
+  return infinite ? (x == INFINITY ? 0.0f : NAN) : fmaf(x, 0.0f, x);
 }
 
 // order of fp32 values as unsigned numbers; -0 and 0 alike
@@ -50,31 +50,101 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
+// Sums and scans of a wave by DPP moves, a tenth of a shuffle's latency.  moved(x): a lane's value
+// goes on as CTRL says, to the rows of 16 lanes in ROWS; other lanes get 0.
+enum { kShr = 0x110, kRor = 0x120, kNextRow = 0x142, kNextRows = 0x143 };
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint32_t moved(uint32_t x, uint32_t other = 0) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(static_cast<int>(other), static_cast<int>(x), CTRL, ROWS, 0xf, false));
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint64_t moved(uint64_t x) {
+  return static_cast<uint64_t>(moved<CTRL, ROWS>(static_cast<uint32_t>(x >> 32))) << 32 | moved<CTRL, ROWS>(static_cast<uint32_t>(x));
+}
+// of the lanes up to each
+template <typename T>
+__device__ __forceinline__ T wave_scan(T x) {
+  x += moved<kShr + 1>(x);
+  x += moved<kShr + 2>(x);
+  x += moved<kShr + 4>(x);
+  x += moved<kShr + 8>(x);
+  x += moved<kNextRow, 0xa>(x);
+  return x + moved<kNextRows, 0xc>(x);
+}
+// of 16 lanes, to each
+template <typename T>
+__device__ __forceinline__ T row_sum(T x) {
+  x += moved<kRor + 8>(x);
+  x += moved<kRor + 4>(x);
+  x += moved<kRor + 2>(x);
+  return x + moved<kRor + 1>(x);
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float moved(float x) {  // or stays
+  return __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(x), __float_as_uint(x)));
+}
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float x, F f) {
+  x = f(x, moved<kRor + 8>(x));
+  x = f(x, moved<kRor + 4>(x));
+  x = f(x, moved<kRor + 2>(x));
+  x = f(x, moved<kRor + 1>(x));
+  x = f(x, moved<kNextRow, 0xa>(x));
+  x = f(x, moved<kNextRows, 0xc>(x));
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
+}
+// A value that the lanes of a wave share, kept in scalar registers.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(uniform(__float_as_uint(x))); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+  return static_cast<uint64_t>(uniform(static_cast<uint32_t>(x >> 32))) << 32 | uniform(static_cast<uint32_t>(x));
+}
+__device__ __forceinline__ double uniform(double x) { return __longlong_as_double(uniform(static_cast<uint64_t>(__double_as_longlong(x)))); }
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
+
+// of groups of P lanes (a power of two, the same in the wave), to each
+template <typename T>
+__device__ __forceinline__ T group_sum(T x, int P) {
+  enum { kPairs = 0xb1, kFours = 0x4e, kMirror8 = 0x141, kMirror16 = 0x140 };
+  if (P > 1) x += moved<kPairs>(x);
+  if (P > 2) x += moved<kFours>(x);
+  if (P > 4) x += moved<kMirror8>(x);
+  if (P > 8) x += moved<kMirror16>(x);
+  if (P > 16) x += __shfl_xor(x, 16, 64);
+  if (P > 32) x += __shfl_xor(x, 32, 64);
+  return x;
+}
+
 // What a row's tokens are weighed with.
 constexpr int kPowers = 256;
 struct Scale {
   double inv;   // kPowers / (ln 2 temperature)
-  float top;    // the largest logit (finite)
-  float bins;   // per unit of logits
-  const double* powers;  // 2^(-i / kPowers)
+  double top;   // the largest logit (finite)
+  float half;   // half of it
+  float bins;   // per half a unit of logits
+  const double* powers;  // 2^(45 + i / kPowers)
 
-  // by the distance from the maximum in fp32: never less for a smaller logit
-  __device__ __forceinline__ int bin(float l) const { return static_cast<int>(fminf((top - l) * bins, kBins - 1)); }
-  // exp((l - top) / temperature) in units: 2^(-j / kPowers) from the table and the series of the
+  // by the distance from the maximum in fp32: never less for a smaller logit (of halves, as a
+  // difference may pass the largest number)
+  __device__ __forceinline__ float distance(float l) const { return fmaf(-0.5f, l, half) * bins; }
+  __device__ __forceinline__ int bin(float l) const { return static_cast<int>(fminf(distance(l), kBins - 1)); }
+  // exp((l - top) / temperature) in units: 2^(j / kPowers) from the table and the series of the
   // rest, |r| <= 1/2, to its fourth power (the next term is 2^-54)
   __device__ __forceinline__ uint64_t weight(float l) const {
-    const double y = fmin((static_cast<double>(top) - l) * inv, kFar + kPowers);  // (NaN, of an endless temperature, too)
+    const double y = fmax((l - top) * inv, -kFar - kPowers);  // (NaN, of an endless temperature, too)
     constexpr double L = 0.69314718055994530942 / kPowers;
-    const double j = rint(y), r = y - j;
-    double s = fma(r, L * L * L * L / 24, -L * L * L / 6);
+    constexpr double kWhole = 6755399441055744.0;  // 1.5 2^52: a sum with it is rounded to whole numbers
+    const double z = y + kWhole, r = y - (z - kWhole);
+    double s = fma(r, L * L * L * L / 24, L * L * L / 6);
     s = fma(r, s, L * L / 2);
-    s = fma(r, s, -L);
+    s = fma(r, s, L);
     s = fma(r, s, 1.0);
-    const int i = static_cast<int>(j);
+    const int i = __double2loint(z);
     const double e = s * powers[i & (kPowers - 1)];
-    const long long scaled = __double_as_longlong(e) + (static_cast<long long>(45 - i / kPowers) << 52);
+    const double scaled = __hiloint2double(__double2hiint(e) + ((i & -kPowers) << 12), __double2loint(e));  // times 2^(i / kPowers), rounded down
     // rounds to a whole number in the low bits
-    return static_cast<uint64_t>(__double_as_longlong(__longlong_as_double(scaled) + 4503599627370496.0)) & ((1ull << 52) - 1);
+    return static_cast<uint64_t>(__double_as_longlong(scaled + 4503599627370496.0)) & ((1ull << 52) - 1);
   }
 };
 
@@ -94,83 +164,66 @@ struct Token {
   uint64_t weight;
 };
 
-struct Shared {
+struct RangeShared {
+  float wave_top[kWaves], wave_low[kWaves];
+};
+struct Shared : RangeShared {
   uint64_t mass[kBins];   // then exclusive sums
   uint32_t count[kBins];
   union {
-    Token list[kList];
+    struct {  // gathered tokens, and their places in descending order
+      uint64_t order[kList], weight[kList];
+      uint32_t sorted[kList];
+    };
     struct {
       uint64_t mass[kSubBins];
       uint32_t count[kSubBins];
     } sub;
   };
+  float near[kList];       // tokens before they are weighed: the logit and the index
+  int32_t near_at[kList];
   double powers[kPowers];
-  uint64_t wave_mass[kThreads / 64];
-  uint32_t wave_count[kThreads / 64];
-  float wave_top[kThreads / 64], wave_low[kThreads / 64];
-  int32_t wave_at[kThreads / 64];
-  uint64_t all, least, found_mass, found_weight;
-  uint32_t all_count, n_list;
-  int32_t found_at, found_bin[2];
+  uint64_t wave_mass[kWaves];
+  uint32_t wave_count[kWaves];
+  uint64_t all, least;
+  struct {
+    uint64_t mass, weight;
+    int32_t at;
+  } found[3];
+  uint32_t all_count, n_list, n_near, key_low, key_top;
+  int32_t at;  // of the arg max
+  int32_t found_bin[3][2];
 };
 
-// Bin b's place: a thread's bins, which follow each other, lie kThreads apart.
-template <int BINS>
-__device__ __forceinline__ int place(int b) {
-  constexpr unsigned PER = BINS / kThreads;
-  return static_cast<unsigned>(b) % PER * kThreads + static_cast<unsigned>(b) / PER;
-}
-
 // Exclusive sums of mass and count in place; the totals to sh.all and sh.all_count.  Returns
-// the sums before and behind the thread's own bins.
+// the sums before and behind the thread's own bins, which follow each other.
 struct Span {
   uint64_t mass0, mass1;
   uint32_t count0, count1;
 };
 template <int BINS, bool MASS, bool COUNT>
 __device__ __forceinline__ Span scan_bins(Shared& sh, uint64_t* mass, uint32_t* count, uint64_t mass0, uint32_t count0) {
-  constexpr int PER = BINS / kThreads, WAVES = kThreads / 64;
+  constexpr int PER = BINS / kThreads;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  uint64_t m = 0;
-  uint32_t c = 0;
+  uint64_t x[PER], m = 0;
+  uint32_t y[PER], c = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    if (MASS) m += mass[i * kThreads + tid];
-    if (COUNT) c += count[i * kThreads + tid];
+    if (MASS) m += x[i] = mass[tid * PER + i];
+    if (COUNT) c += y[i] = count[tid * PER + i];
   }
-  uint64_t im = m;
-  uint32_t ic = c;
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const uint64_t om = MASS ? __shfl_up(static_cast<unsigned long long>(im), s, 64) : 0;
-    const uint32_t oc = COUNT ? __shfl_up(ic, s, 64) : 0;
-    if (lane >= s) im += om, ic += oc;
-  }
+  const uint64_t im = MASS ? wave_scan(m) : 0;
+  const uint32_t ic = COUNT ? wave_scan(c) : 0;
   if (lane == 63) sh.wave_mass[wave] = im, sh.wave_count[wave] = ic;
   __syncthreads();
-  uint64_t wm = MASS && lane < WAVES && lane < wave ? sh.wave_mass[lane] : 0;  // of the waves before
-  uint32_t wc = COUNT && lane < WAVES && lane < wave ? sh.wave_count[lane] : 0;
-#pragma unroll
-  for (int s = WAVES / 2; s >= 1; s >>= 1) {
-    if (MASS) wm += __shfl_xor(static_cast<unsigned long long>(wm), s, 64);
-    if (COUNT) wc += __shfl_xor(wc, s, 64);
-  }
-  uint64_t base = mass0 + __shfl(static_cast<unsigned long long>(wm), 0, 64) + im - m;
-  uint32_t bc = count0 + __shfl(wc, 0, 64) + ic - c;
+  const bool earlier = lane % kWaves < wave;
+  uint64_t base = mass0 + (MASS ? row_sum(earlier ? sh.wave_mass[lane % kWaves] : 0) : 0) + im - m;
+  uint32_t bc = count0 + (COUNT ? row_sum(earlier ? sh.wave_count[lane % kWaves] : 0) : 0) + ic - c;
   const Span own = {base, base + m, bc, bc + c};
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int at = i * kThreads + tid;
-    if (MASS) {
-      const uint64_t x = mass[at];
-      mass[at] = base;
-      base += x;
-    }
-    if (COUNT) {
-      const uint32_t y = count[at];
-      count[at] = bc;
-      bc += y;
-    }
+    if (MASS) mass[tid * PER + i] = base, base += x[i];
+    if (COUNT) count[tid * PER + i] = bc, bc += y[i];
   }
   if (tid == kThreads - 1) {
     if (MASS) sh.all = base;
@@ -184,32 +237,29 @@ __device__ __forceinline__ Span scan_bins(Shared& sh, uint64_t* mass, uint32_t* 
 enum Cut { kCount, kReach, kPass };
 
 // Whether the prefix before `mass` and `count` is still short of the cut.
-template <Cut CUT>
-__device__ __forceinline__ bool is_short(double t, uint64_t mass, uint32_t count) {
-  return CUT == kCount ? count < t : CUT == kReach ? static_cast<double>(mass) < t : static_cast<double>(mass) <= t;
+__device__ __forceinline__ bool is_short(Cut cut, double t, uint64_t mass, uint32_t count) {
+  return cut == kCount ? count < t : cut == kReach ? static_cast<double>(mass) < t : static_cast<double>(mass) <= t;
 }
 
 // The bins in which the cuts at t0 and t1 lie, from exclusive sums: of the threads whose bins
 // they may be in exactly one looks (the last where rounding leaves none).
-template <Cut CUT, int BINS>
-__device__ __forceinline__ int2 bins_of(Shared& sh, const uint64_t* mass, const uint32_t* count, const Span& own, double t0, double t1) {
+template <int BINS>  // (found_bin[cut] has to be free)
+__device__ __forceinline__ int2 bins_of(Cut cut, Shared& sh, const uint64_t* mass, const uint32_t* count, const Span& own, double t0, double t1) {
   constexpr int PER = BINS / kThreads;
   const int tid = threadIdx.x;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const double t = i ? t1 : t0;
-    if ((tid == 0 || is_short<CUT>(t, own.mass0, own.count0)) && (tid == kThreads - 1 || !is_short<CUT>(t, own.mass1, own.count1))) {
+    if ((tid == 0 || is_short(cut, t, own.mass0, own.count0)) && (tid == kThreads - 1 || !is_short(cut, t, own.mass1, own.count1))) {
       int b = tid * PER;
 #pragma unroll
       for (int j = 1; j < PER; ++j)
-        if (is_short<CUT>(t, mass[j * kThreads + tid], count[j * kThreads + tid])) b = tid * PER + j;
-      sh.found_bin[i] = b;
+        if (is_short(cut, t, mass[tid * PER + j], count[tid * PER + j])) b = tid * PER + j;
+      sh.found_bin[cut][i] = b;
     }
   }
   __syncthreads();
-  const int2 r = make_int2(sh.found_bin[0], sh.found_bin[1]);
-  __syncthreads();
-  return r;
+  return make_int2(sh.found_bin[cut][0], sh.found_bin[cut][1]);
 }
 
 struct End {
@@ -217,148 +267,117 @@ struct End {
   int token;
 };
 
-// A cut among the gathered tokens: each knows what is before it, and one of them is the end
-// (own is 0 for threads without one).
-template <Cut CUT>
-__device__ __forceinline__ End cut_in_list(Shared& sh, double t, uint64_t before, uint32_t rank, uint64_t own, int token) {
-  if (threadIdx.x == 0) sh.found_mass = ~0ull;  // none: all are kept
-  __syncthreads();
-  if (own && !is_short<CUT>(t, before + own, rank + 1) && (is_short<CUT>(t, before, rank) || before == 0))
-    sh.found_mass = before + own, sh.found_weight = own, sh.found_at = token;
-  __syncthreads();
-  const End e = {sh.found_mass, sh.found_weight, sh.found_at};
-  __syncthreads();
-  return e;
-}
-
-// The same for rows whose tokens crowd into few bins (many equal logits, or an outlier that
-// stretches the bins): the range of values is divided by 1024 until one value is left, then
-// its tokens are counted.
-template <Cut CUT>
-__device__ End cut_in_row(Shared& sh, Scale sc, const float* row, int n, bool infinite, float low, double t) {
-  const int tid = threadIdx.x;
-  uint32_t kmax = order_key(sc.top), kmin = order_key(low);
-  uint64_t base = 0;
-  uint32_t rank = 0;
-  while (kmax > kmin) {
-    const int shift = max(0, 32 - __clz(kmax - kmin) - 10);
-    sh.sub.mass[tid] = 0, sh.sub.count[tid] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
-      const float l = logit(row[i], infinite);
-      const uint32_t key = order_key(l);
-      if (!(l > -INFINITY) || key < kmin || key > kmax) continue;
-      const uint64_t w = sc.weight(l);
-      if (!w) continue;
-      atomicAdd(reinterpret_cast<unsigned long long*>(&sh.sub.mass[(kmax - key) >> shift]), w);
-      atomicAdd(&sh.sub.count[(kmax - key) >> shift], 1u);
-    }
-    __syncthreads();
-    const Span own = scan_bins<kSubBins, true, true>(sh, sh.sub.mass, sh.sub.count, base, rank);
-    const uint32_t b = bins_of<CUT, kSubBins>(sh, sh.sub.mass, sh.sub.count, own, t, t).x;
-    base = sh.sub.mass[b], rank = sh.sub.count[b];
-    kmax -= b << shift;
-    kmin = max(kmin, kmax - ((1u << shift) - 1));
-    __syncthreads();
-  }
-  // the tokens of one value, by their index: the first with enough before it
-  const uint64_t w = sc.weight(key_value(kmax));
-  if (tid == 0) sh.found_at = -1, sh.found_mass = ~0ull;
-  __syncthreads();
-  for (int i0 = 0; i0 < n; i0 += kThreads) {
-    const int i = i0 + tid;
-    const bool is = i < n && order_key(logit(row[i], infinite)) == kmax;
-    const uint64_t votes = __ballot(is);
-    if ((tid & 63) == 0) sh.wave_count[tid >> 6] = __popcll(votes);
-    __syncthreads();
-    uint32_t earlier = __popcll(votes & ((1ull << (tid & 63)) - 1)), every = 0;
-    for (int v = 0; v < kThreads / 64; ++v) {
-      if (v < tid >> 6) earlier += sh.wave_count[v];
-      every += sh.wave_count[v];
-    }
-    const uint64_t mass = base + earlier * w;
-    if (is && !is_short<CUT>(t, mass + w, rank + earlier + 1) && (is_short<CUT>(t, mass, rank + earlier) || mass == 0))
-      sh.found_mass = mass + w, sh.found_at = i;
-    base += every * w, rank += every;
-    __syncthreads();
-    if (sh.found_at >= 0) break;  // uniform
-  }
-  const End e = {sh.found_mass, w, sh.found_at};
-  __syncthreads();
-  return e;
-}
-
-// A thread's logits of [i0, i1) of a row, read kHold at a time, and only once where there are no
-// more.
+// A thread's logits of [i0, i1) of a row: held in registers for all passes, or read again for each,
+// AT_ONCE at a time.
+constexpr int kHold = 32, kRead = 8;
+template <int AT_ONCE>
 struct Logits {
+  static constexpr bool HELD = AT_ONCE == kHold;  // i1 - i0 <= kHold * kThreads
   const float* row;
   int i0, i1;
   bool infinite;
-  float hold[kHold];
+  float x[AT_ONCE];
 
-  __device__ __forceinline__ bool once() const { return i1 - i0 <= kHold * kThreads; }
   __device__ __forceinline__ void fetch(int from) {  // from + thread, from + thread + kThreads, ...
+    steps<8>(from, [&](int g) {
 #pragma unroll
-    for (int i = 0; i < kHold; ++i) {
-      const int j = from + static_cast<int>(threadIdx.x) + i * kThreads;
-      hold[i] = j < i1 ? row[j] : -INFINITY;
+      for (int i = g; i < g + 8; ++i) {
+        const uint32_t at = 4u * min(from + i * kThreads + static_cast<int>(threadIdx.x), i1 - 1);  // (less than 2^21)
+        x[i] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(row) + at);
+      }
+    });
+  }
+  __device__ __forceinline__ void end(int from) {  // NaN past the end
+#pragma unroll
+    for (int g = 0; g < AT_ONCE; g += 8) {
+      if (from + (g + 8) * kThreads <= i1) continue;
+#pragma unroll
+      for (int i = g; i < g + 8; ++i)
+        if (from + i * kThreads + static_cast<int>(threadIdx.x) >= i1) x[i] = NAN;
     }
+  }
+  __device__ __forceinline__ void settle() {
 #pragma unroll
-    for (int i = 0; i < kHold; ++i) hold[i] = logit(hold[i], infinite);
+    for (int i = 0; i < AT_ONCE; ++i) x[i] = logit(x[i], infinite);
   }
   __device__ __forceinline__ Logits(const float* r, int from, int to) : row(r), i0(from), i1(to), infinite(false) {
-    if (once()) fetch(i0);
+    if (HELD) fetch(i0);
   }
-  __device__ __forceinline__ void make_infinite() {
-    infinite = true;
-    if (once()) {
+  // Before the first pass: the largest, and the smallest that is finite.
+  __device__ __forceinline__ float2 range() {
+    float top = -INFINITY, low = INFINITY;
+    auto look = [&](int from) {
+      end(from);
+      steps<8>(from, [&](int g) {
 #pragma unroll
-      for (int i = 0; i < kHold; ++i) hold[i] = logit(hold[i], true);
+        for (int i = g; i < g + 8; ++i) top = fmaxf(top, x[i]), low = fminf(low, logit(x[i], false));
+      });
+    };
+    if (HELD) {
+      look(i0);
+      settle();
+    } else {
+      for (int from = i0; from < i1; from += AT_ONCE * kThreads) {
+        fetch(from);
+        look(from);
+      }
+    }
+    return make_float2(top, low);
+  }
+  // Before the first pass where the range is known already, and again where the largest is infinite.
+  __device__ __forceinline__ void know(bool is_infinite) {
+    infinite = is_infinite;
+    if (!HELD) return;
+    if (infinite) fetch(i0);
+    end(i0);
+    settle();
+  }
+  // f(from): x has the logits of from + thread, from + thread + kThreads, ...
+  template <typename F>
+  __device__ __forceinline__ void pass(F f) {
+    if (HELD) {
+      f(i0);
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) asm("" : "+v"(x[i]));  // (what a pass computes of a logit is not kept in registers for the next)
+    } else {
+      for (int from = i0; from < i1; from += AT_ONCE * kThreads) {
+        fetch(from);
+        end(from);
+        settle();
+        f(from);
+      }
     }
   }
-  // f(logit, index) for the thread's, and for -infinity past the end (eight at a time)
+  // f(first) for x[first .. first + STEP) up to the end
+  template <int STEP, typename F>
+  __device__ __forceinline__ void steps(int from, F f) {
+#pragma unroll
+    for (int g = 0; g < AT_ONCE; g += STEP) {
+      if (from + g * kThreads >= i1) break;
+      f(g);
+    }
+  }
+  // f(logit, index) for all of a thread's, and for NaN past the end (eight at a time)
   template <typename F>
   __device__ __forceinline__ void every(F f) {
-    for (int from = i0; from < i1; from += kHold * kThreads) {
-      if (!once()) fetch(from);
+    pass([&](int from) {
+      steps<8>(from, [&](int g) {
 #pragma unroll
-      for (int g = 0; g < kHold; g += 8) {
-        if (from + g * kThreads >= i1) break;
-#pragma unroll
-        for (int i = g; i < g + 8; ++i) f(hold[i], from + static_cast<int>(threadIdx.x) + i * kThreads);
-      }
-    }
-  }
-  // f(four logits)
-  template <typename F>
-  __device__ __forceinline__ void fours(F f) {
-    for (int from = i0; from < i1; from += kHold * kThreads) {
-      if (!once()) fetch(from);
-#pragma unroll
-      for (int g = 0; g < kHold; g += 4) {
-        if (from + g * kThreads >= i1) break;
-        const float x[4] = {hold[g], hold[g + 1], hold[g + 2], hold[g + 3]};
-        f(x);
-      }
-    }
+        for (int i = g; i < g + 8; ++i) f(x[i], from + static_cast<int>(threadIdx.x) + i * kThreads);
+      });
+    });
   }
 };
 
-// The largest and the smallest of a work-group's logits.
-__device__ __forceinline__ float2 range_of(Shared& sh, Logits& l) {
-  constexpr int WAVES = kThreads / 64;
+// The same of a work-group's.
+template <typename L>
+__device__ __forceinline__ float2 range_of(RangeShared& sh, L& l) {
   const int lane = threadIdx.x & 63;
-  float top = -INFINITY, low = INFINITY;
-  l.every([&](float x, int) { top = fmaxf(top, x), low = fminf(low, x); });
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, 64)), low = fminf(low, __shfl_xor(low, s, 64));
-  if (lane == 0) sh.wave_top[threadIdx.x >> 6] = top, sh.wave_low[threadIdx.x >> 6] = low;
+  float2 r = l.range();
+  r = make_float2(wave_reduce(r.x, larger), wave_reduce(r.y, smaller));
+  if (lane == 0) sh.wave_top[threadIdx.x >> 6] = r.x, sh.wave_low[threadIdx.x >> 6] = r.y;
   __syncthreads();
-  top = sh.wave_top[lane % WAVES], low = sh.wave_low[lane % WAVES];
-#pragma unroll
-  for (int s = WAVES / 2; s >= 1; s >>= 1)
-    top = fmaxf(top, __shfl_xor(top, s, 64)), low = fminf(low, __shfl_xor(low, s, 64));
-  return make_float2(top, low);
+  return make_float2(wave_reduce(sh.wave_top[lane % kWaves], larger), wave_reduce(sh.wave_low[lane % kWaves], smaller));
 }
 
 // A row's settings, and the scale that they and its range give.
@@ -377,81 +396,85 @@ struct Settings {
         by_k(k > 0 && k < a.n),
         by_p(p < 1.0f),
         by_min(min_p > 0.0f),
-        least(by_min ? static_cast<uint64_t>(ceil(fmin(static_cast<double>(min_p), 1.0) * kUnit)) : 0) {}
+        least(0) {
+    // (computed once: the compiler would do it again at every use)
+    if (by_min) least = uniform(static_cast<uint64_t>(ceil(fmin(static_cast<double>(min_p), 1.0) * kUnit)));
+  }
   __device__ __forceinline__ double number() const { return fmin(fmax(drawn, 0.0f), 0x1.fffffep-1f); }  // NaN draws as 0
   __device__ __forceinline__ double share() const { return fmax(static_cast<double>(p), 0.0); }
   __device__ __forceinline__ bool greedy(float top) const { return !(temp > 0.0f) || top == -INFINITY; }
   __device__ __forceinline__ Scale scale(const Shared& sh, float top, float low) const {
     constexpr double kLn2 = 0.69314718055994530942;
     Scale sc;
-    sc.inv = kPowers / kLn2 / temp;
-    sc.top = top;
+    sc.inv = uniform(kPowers / kLn2 / temp);
+    sc.top = uniform(static_cast<double>(top)), sc.half = uniform(0.5f * top);
     sc.powers = sh.powers;
-    const float span = fminf(top - low, static_cast<float>(kFar / kPowers * kLn2) * temp);
-    sc.bins = span > 0.0f ? fminf((kBins - 1) / span, 3e38f) : 0.0f;  // (finite: the maximum's bin is 0)
+    const float span = fminf(sc.half - 0.5f * low, static_cast<float>(kFar / kPowers * kLn2 / 2) * temp);
+    sc.bins = uniform(span > 0.0f ? fminf((kBins - 1) / span, 3e38f) : 0.0f);  // (finite: the maximum's bin is 0)
     return sc;
   }
 };
 
 // Before the first use of a Scale and of the histogram; a barrier has to follow.
 __device__ __forceinline__ void tabulate(Shared& sh) {
-  if (threadIdx.x < kPowers) sh.powers[threadIdx.x] = exp2(-static_cast<double>(threadIdx.x) / kPowers);
+  if (threadIdx.x < 3) sh.found[threadIdx.x].mass = ~0ull;
+  if (threadIdx.x < kPowers) sh.powers[threadIdx.x] = exp2(45 + static_cast<double>(threadIdx.x) / kPowers);
 }
 __device__ __forceinline__ void clear(Shared& sh) {
 #pragma unroll
   for (int b = 0; b < kBins; b += kThreads) sh.mass[b + threadIdx.x] = 0, sh.count[b + threadIdx.x] = 0;
-  if (threadIdx.x == 0) sh.least = 0;
+  if (threadIdx.x == 0) sh.least = 0, sh.n_list = 0, sh.n_near = 0;
 }
 
 // (The last bin's count nobody asks for, and in peaked rows most tokens are there.)
 __device__ __forceinline__ void count_token(Shared& sh, int b) {
-  if (b < kBins - 1) atomicAdd(&sh.count[place<kBins>(b)], 1u);
+  if (b < kBins - 1) atomicAdd(&sh.count[b], 1u);
 }
 
-// Weighs the tokens of bins 0 .. last into the histogram, and sums those that min_p keeps.
-template <bool COUNT>
-__device__ __forceinline__ void weigh(Shared& sh, const Scale& sc, const Settings& st, Logits& l, int last) {
+// The weights that min_p keeps, summed over the work-group.
+__device__ __forceinline__ void keep(Shared& sh, const Settings& st, uint64_t kept) {
+  if (!st.by_min) return;
+  kept = wave_scan(kept);
+  if ((threadIdx.x & 63) == 63 && kept) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.least), static_cast<unsigned long long>(kept));
+}
+__device__ __forceinline__ void add_weight(Shared& sh, int b, uint64_t w) {
+  if (w) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[b]), static_cast<unsigned long long>(w));
+}
+
+// Weighs all tokens into the histogram, two at a time: a token's chain of operations beside the
+// other's.
+template <bool COUNT, typename L>
+__device__ __forceinline__ void weigh(Shared& sh, const Scale& sc, const Settings& st, L& l) {
   uint64_t kept = 0;
-  auto add = [&](int b, uint64_t w) {
-    atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[place<kBins>(b)]), w);
-    kept += w >= st.least ? w : 0;
-  };
-  if (last < kBins - 1) {  // few
-    l.every([&](float x, int) {
-      const int b = sc.bin(x);
-      if (b > last) return;
-      if (const uint64_t w = sc.weight(x)) add(b, w);
-    });
-  } else {
-    l.fours([&](const float (&x)[4]) {  // a token's chain of operations beside the others'
-      uint64_t w[4];
+  l.pass([&](int from) {
+    l.template steps<2>(from, [&](int g) {
+      uint64_t w[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = sc.weight(x[i]);
+      for (int i = 0; i < 2; ++i) w[i] = sc.weight(l.x[g + i]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int b = sc.bin(x[i]);
+      for (int i = 0; i < 2; ++i) {
+        const int b = sc.bin(l.x[g + i]);
         if (COUNT && st.by_k) count_token(sh, b);
-        if (w[i]) add(b, w[i]);
+        add_weight(sh, b, w[i]);
+      }
+      if (st.by_min) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) kept += w[i] >= st.least ? w[i] : 0;
       }
     });
-  }
-  if (st.by_min) {
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) kept += __shfl_xor(static_cast<unsigned long long>(kept), s, 64);
-    if ((threadIdx.x & 63) == 0) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.least), static_cast<unsigned long long>(kept));
-  }
+  });
+  keep(sh, st, kept);
 }
 
 // The bins of the histogram in which the cuts lie.
 struct Cuts {
-  int k;     // the k-th token's bin, or -1
+  int k;      // the k-th token's bin, or -2
   int2 p, u;  // where top-p's and the drawn token may be, from bounds on the masses before them
-  int first, last;
   uint64_t all, from_min;
 
-  __device__ __forceinline__ bool has(int b) const {
-    if (b < first || b > last) return false;  // as most
-    return b == k || (b >= p.x && b <= p.y) || (b >= u.x && b <= u.y);
+  __device__ __forceinline__ bool has(float distance) const {  // (at most a bin past the last: no weights)
+    auto in = [&](int from, int to) { return distance >= from && distance < to + 1; };
+    return in(k, k) || in(p.x, p.y) || in(u.x, u.y);
   }
 };
 
@@ -461,126 +484,309 @@ __device__ __forceinline__ Cuts cuts_of(Shared& sh, const Settings& st, int bk) 
   Cuts c;
   c.all = sh.all, c.from_min = st.by_min ? sh.least : c.all;
   c.k = bk;
-  c.p = make_int2(-1, -2);
+  c.p = make_int2(-2, -2);
   const double u = st.number(), share = st.share();
-  auto at = [&](int b) { return sh.mass[place<kBins>(b)]; };
+  auto at = [&](int b) { return sh.mass[b]; };
   auto after = [&](int b) { return b + 1 < kBins ? at(b + 1) : c.all; };
   uint64_t lo = c.all, hi = c.all;
   if (bk >= 0) lo = at(bk), hi = after(bk);
   if (st.by_p) {
-    c.p = bins_of<kReach, kBins>(sh, sh.mass, sh.count, own, share * static_cast<double>(lo), share * static_cast<double>(hi));
+    c.p = bins_of<kBins>(kReach, sh, sh.mass, sh.count, own, share * static_cast<double>(lo), share * static_cast<double>(hi));
     lo = min(lo, at(c.p.x)), hi = min(hi, after(c.p.y));
   }
   lo = min(lo, c.from_min), hi = min(hi, c.from_min);
-  c.u = bins_of<kPass, kBins>(sh, sh.mass, sh.count, own, u * static_cast<double>(lo), u * static_cast<double>(hi));
-  c.first = st.by_p ? min(c.p.x, c.u.x) : c.u.x, c.last = max(max(c.k, c.p.y), c.u.y);
+  c.u = bins_of<kBins>(kPass, sh, sh.mass, sh.count, own, u * static_cast<double>(lo), u * static_cast<double>(hi));
   return c;
 }
 
-// The tokens of the cuts' bins, put(slot, token) in any order; counts them all.
-template <typename Put>
-__device__ __forceinline__ void gather(const Scale& sc, const Cuts& c, Logits& l, uint32_t* n_list, Put put) {
-  l.every([&](float x, int i) {
-    const int b = sc.bin(x);
-    if (!c.has(b)) return;
-    const uint64_t w = sc.weight(x);
-    if (!w) return;
-    const uint32_t slot = atomicAdd(n_list, 1u);
-    if (slot < kList)
-      put(slot, Token{static_cast<uint64_t>(order_key(x)) << 32 | static_cast<uint32_t>(b) << 19 | (kMostTokens - i), w}, b);
+__device__ __forceinline__ Token token_of(const Scale& sc, float l, int at) {
+  return {static_cast<uint64_t>(order_key(l)) << 32 | static_cast<uint32_t>(sc.bin(l)) << 19 | (kMostTokens - at), sc.weight(l)};
+}
+
+// Tokens whose distance a test holds for, to sh.near in any order; counts them all.
+template <typename L, typename Has>
+__device__ __forceinline__ void gather(Shared& sh, const Scale& sc, L& l, uint32_t* n, Has has) {
+  l.pass([&](int from) {
+    uint32_t mask = 0;
+    l.template steps<8>(from, [&](int g) {
+#pragma unroll
+      for (int i = g; i < g + 8; ++i) mask |= has(sc.distance(l.x[i])) ? 1u << i : 0;
+    });
+    const uint32_t own = __popc(mask), upto = wave_scan(own), all = __builtin_amdgcn_readlane(upto, 63);
+    if (!all) return;
+    uint32_t slot = 0;
+    if ((threadIdx.x & 63) == 0) slot = atomicAdd(n, all);
+    slot = uniform(slot) + upto - own;
+    l.template steps<8>(from, [&](int g) {
+#pragma unroll
+      for (int i = g; i < g + 8; ++i) {
+        if (!(mask >> i & 1)) continue;
+        if (slot < kList) sh.near[slot] = l.x[i], sh.near_at[slot] = from + static_cast<int>(threadIdx.x) + i * kThreads;
+        ++slot;
+      }
+    });
   });
 }
 
-// The choice among the m gathered tokens of sh.list; earlier(slot, mass, count): of the bins
-// before a token's.
-template <typename Earlier>
-__device__ __forceinline__ void choose(Shared& sh, const SampleArgs& a, const Settings& st, const Scale& sc, int t, int m, uint64_t all,
-                       uint64_t from_min, bool infinite, float low, Earlier earlier) {
+// A cut among the tokens of keys kmin to kmax, with base and rank before them, where they are more
+// than the list holds (many equal logits, or an outlier that stretches the bins): the range of keys
+// is divided by 1024 until one is left, then its tokens are counted.
+__device__ End cut_in_range(Cut cut, Shared& sh, Scale sc, const float* row, int n, bool infinite, uint32_t kmin, uint32_t kmax,
+                            uint64_t base, uint32_t rank, double t) {
   const int tid = threadIdx.x;
+  while (kmax > kmin) {
+    const int shift = max(0, 32 - __clz(kmax - kmin) - 10);
+    sh.sub.mass[tid] = 0, sh.sub.count[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += kThreads) {
+      const float l = logit(row[i], infinite);
+      const uint32_t key = order_key(l);
+      if (!(l > -INFINITY) || key < kmin || key > kmax) continue;
+      const uint64_t w = sc.weight(l);
+      if (!w) continue;
+      atomicAdd(reinterpret_cast<unsigned long long*>(&sh.sub.mass[(kmax - key) >> shift]), w);
+      atomicAdd(&sh.sub.count[(kmax - key) >> shift], 1u);
+    }
+    __syncthreads();
+    const Span own = scan_bins<kSubBins, true, true>(sh, sh.sub.mass, sh.sub.count, base, rank);
+    const uint32_t b = bins_of<kSubBins>(cut, sh, sh.sub.mass, sh.sub.count, own, t, t).x;
+    base = sh.sub.mass[b], rank = sh.sub.count[b];
+    kmax -= b << shift;
+    kmin = max(kmin, kmax - ((1u << shift) - 1));
+    __syncthreads();
+  }
+  // the tokens of one value, by their index: the first with enough before it
+  const uint64_t w = sc.weight(key_value(kmax));
+  auto& f = sh.found[cut];
+  if (tid == 0) f.at = -1, f.mass = ~0ull;
+  __syncthreads();
+  for (int i0 = 0; i0 < n; i0 += kThreads) {
+    const int i = i0 + tid;
+    const bool is = i < n && order_key(logit(row[i], infinite)) == kmax;
+    const uint64_t votes = __ballot(is);
+    if ((tid & 63) == 0) sh.wave_count[tid >> 6] = __popcll(votes);
+    __syncthreads();
+    uint32_t earlier = __popcll(votes & ((1ull << (tid & 63)) - 1)), every = 0;
+    for (int v = 0; v < kWaves; ++v) {
+      if (v < tid >> 6) earlier += sh.wave_count[v];
+      every += sh.wave_count[v];
+    }
+    const uint64_t mass = base + earlier * w;
+    if (is && !is_short(cut, t, mass + w, rank + earlier + 1) && (is_short(cut, t, mass, rank + earlier) || mass == 0))
+      f.mass = mass + w, f.at = i;
+    base += every * w, rank += every;
+    __syncthreads();
+    if (f.at >= 0) break;  // uniform
+  }
+  const End e = {f.mass, w, f.at};
+  __syncthreads();
+  return e;
+}
+
+// A thread's token in descending order, and what is before it in the row.
+struct Place {
+  uint64_t before, own;
+  uint32_t rank;
+  int token;
+};
+// Sorts the m gathered tokens of sh.order and sh.weight; earlier(slot, bin, mass, count): of the
+// bins before a token's.  Changes those bins of the histogram.
+template <typename Earlier>
+__device__ __forceinline__ Place sorted(Shared& sh, int m, Earlier earlier) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // each counts the earlier ones, with P threads, each of which looks at every P-th
+  int P = 64;
+  while (P > 1 && P * m > kThreads) P /= 2;
+  const int e = tid / P;
+  uint32_t r = 0;
+  if (e < m) {
+    const uint64_t order = sh.order[e];
+#pragma unroll 4
+    for (int j = tid % P; j < m; j += P) r += sh.order[j] > order;
+  }
+  r = group_sum(r, P);
+  if (e < m && tid % P == 0) sh.sorted[r] = e;
+  __syncthreads();
+  // thread i has the i-th: the mass before it in the list,
+  const int slot = tid < m ? sh.sorted[tid] : 0;
+  const uint64_t order = tid < m ? sh.order[slot] : 0, own = tid < m ? sh.weight[slot] : 0;
+  const uint32_t b = static_cast<uint32_t>(order) >> 19;
+  const bool leads = tid < m && (tid == 0 || static_cast<uint32_t>(sh.order[sh.sorted[tid - 1]]) >> 19 != b);
+  const uint64_t upto = wave_scan(own);
+  if (lane == 63) sh.wave_mass[wave] = upto;
+  __syncthreads();
+  uint64_t before = row_sum(lane % kWaves < wave ? sh.wave_mass[lane % kWaves] : 0) + upto - own;
+  // and in the row, from where the first of its bin is
+  if (leads) {
+    uint64_t mass;
+    uint32_t count;
+    earlier(slot, b, mass, count);
+    sh.mass[b] = mass - before, sh.count[b] = count - tid;
+  }
+  __syncthreads();
+  return {before + sh.mass[b], own, tid + sh.count[b], kMostTokens - static_cast<int>(order & kMostTokens)};
+}
+
+// A cut among them: each knows what is before it, and one of them is the end (own is 0 for
+// threads without one).
+__device__ __forceinline__ End cut_in_list(Cut cut, Shared& sh, double t, const Place& p) {
+  auto& f = sh.found[cut];  // as tabulate() left it where none is: all are kept
+  if (p.own && !is_short(cut, t, p.before + p.own, p.rank + 1) && (is_short(cut, t, p.before, p.rank) || p.before == 0))
+    f.mass = p.before + p.own, f.weight = p.own, f.at = p.token;
+  __syncthreads();
+  return {f.mass, f.weight, f.at};
+}
+
+// A cut by the exclusive sums of all bins and the tokens of the one that it lies in.
+template <typename L>
+__device__ __forceinline__ End cut_in_bin(Cut cut, Shared& sh, const Scale& sc, L& l, int n, double t) {
+  const int tid = threadIdx.x;
+  for (int b = tid; b < kBins; b += kThreads) {
+    if ((b == 0 || is_short(cut, t, sh.mass[b], sh.count[b])) &&
+        (b == kBins - 1 || !is_short(cut, t, sh.mass[b + 1], sh.count[b + 1])))
+      sh.found_bin[cut][0] = b;
+  }
+  if (tid == 0) sh.n_list = 0, sh.key_low = ~0u, sh.key_top = 0;
+  __syncthreads();
+  const int b = sh.found_bin[cut][0];
+  const uint64_t mass = sh.mass[b];
+  const uint32_t count = sh.count[b];
+  auto in = [&](float d) { return d >= b && d < b + 1; };
+  gather(sh, sc, l, &sh.n_list, in);
+  __syncthreads();
+  const int m = static_cast<int>(sh.n_list);
+  if (m <= kList) {
+    if (tid < m) {
+      const Token x = token_of(sc, sh.near[tid], sh.near_at[tid]);
+      sh.order[tid] = x.order, sh.weight[tid] = x.weight;
+    }
+    __syncthreads();
+    const Place p = sorted(sh, m, [&](int, uint32_t, uint64_t& x, uint32_t& y) { x = mass, y = count; });
+    const End e = cut_in_list(cut, sh, t, p);
+    if (tid == 0) sh.mass[b] = mass, sh.count[b] = count;
+    __syncthreads();
+    return e;
+  }
+  uint32_t low = ~0u, top = 0;
+  l.every([&](float x, int) {
+    if (!in(sc.distance(x))) return;
+    low = min(low, order_key(x)), top = max(top, order_key(x));
+  });
+  if (top) atomicMin(&sh.key_low, low), atomicMax(&sh.key_top, top);
+  __syncthreads();
+  return cut_in_range(cut, sh, sc, l.row, n, l.infinite, sh.key_low, sh.key_top, mass, count, t);
+}
+
+// The choice among the m gathered tokens of sh.order and sh.weight; where there are more than the
+// list holds, cut by cut, with the exclusive sums that all() leaves in the histogram.
+template <typename Earlier, typename All>
+__device__ __forceinline__ void choose(Shared& sh, const SampleArgs& a, const Settings& st, const Scale& sc, bool infinite, int t, int m,
+                                       uint64_t whole, uint64_t from_min, Earlier earlier, All all) {
   const double u = st.number(), share = st.share();
-  uint64_t M = all;
+  uint64_t M = whole;
   End end;
   if (m <= kList) {
-    // P threads to a token, each of which looks at every P-th of the others
-    int P = 64;
-    while (P > 1 && P * m > kThreads) P /= 2;
-    const int e = tid / P;
-    uint64_t before = 0, own = 0, order = 0;
-    uint32_t rank = 0;
-    if (e < m) {
-      order = sh.list[e].order, own = sh.list[e].weight;
-      for (int j = tid % P; j < m; j += P) {
-        const Token x = sh.list[j];
-        if (x.order > order && !(static_cast<uint32_t>(x.order ^ order) >> 19)) before += x.weight, ++rank;
-      }
-    }
-    for (int s = P / 2; s >= 1; s >>= 1) {
-      before += __shfl_xor(static_cast<unsigned long long>(before), s, 64);
-      rank += __shfl_xor(rank, s, 64);
-    }
-    if (e < m) earlier(e, static_cast<uint32_t>(order) >> 19, before, rank);
-    const int token = kMostTokens - static_cast<int>(order & kMostTokens);
-    if (st.by_k) M = min(M, cut_in_list<kCount>(sh, st.k, before, rank, own, token).mass);
-    if (st.by_p) M = min(M, cut_in_list<kReach>(sh, share * static_cast<double>(M), before, rank, own, token).mass);
+    const Place p = sorted(sh, m, earlier);
+    if (st.by_k) M = min(M, cut_in_list(kCount, sh, st.k, p).mass);
+    if (st.by_p) M = min(M, cut_in_list(kReach, sh, share * static_cast<double>(M), p).mass);
     M = min(M, from_min);
-    end = cut_in_list<kPass>(sh, u * static_cast<double>(M), before, rank, own, token);
+    end = cut_in_list(kPass, sh, u * static_cast<double>(M), p);
   } else {
-    const float* row = a.logits + static_cast<size_t>(t) * a.n;
-    if (st.by_k) M = min(M, cut_in_row<kCount>(sh, sc, row, a.n, infinite, low, st.k).mass);
-    if (st.by_p) M = min(M, cut_in_row<kReach>(sh, sc, row, a.n, infinite, low, share * static_cast<double>(M)).mass);
-    M = min(M, from_min);
-    end = cut_in_row<kPass>(sh, sc, row, a.n, infinite, low, u * static_cast<double>(M));
+    all();
+    Logits<kRead> l(a.logits + static_cast<size_t>(t) * a.n, 0, a.n);
+    l.know(infinite);
+#pragma unroll 1
+    for (int c = st.by_k ? kCount : st.by_p ? kReach : kPass; c <= kPass; ++c) {
+      if (c == kReach && !st.by_p) continue;
+      if (c == kPass) M = min(M, from_min);
+      end = cut_in_bin(static_cast<Cut>(c), sh, sc, l, a.n, c == kCount ? st.k : (c == kReach ? share : u) * static_cast<double>(M));
+      if (c < kPass) M = min(M, end.mass);
+    }
   }
-  if (tid == 0) {
+  if (threadIdx.x == 0) {
     a.idx[t] = end.token;
     if (a.prob) a.prob[t] = static_cast<float>(static_cast<double>(end.weight) / static_cast<double>(M));
   }
 }
 
-// A work-group per row.  What costs most is the weights, in double precision: with top-k, or
-// min-p alone, only the tokens down to a cut's bin are weighed.
+// A work-group per row, its logits in registers up to 32768.  Bound by the instructions of the
+// weights, some thirty a token of which half are in double precision, and by a chain of scans and
+// barriers: with top-k, or min-p alone, only the tokens down to a cut's bin are weighed, from a
+// list.  One row of 32000: 13.6 us with top-k of 50, 18 with all tokens (8 of them weights);
+// 500 rows with min-p: 27 us, 2.4 TB/s, in two rounds of work-groups.
+template <int AT_ONCE>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   __shared__ Shared sh;
   const int t = blockIdx.x, tid = threadIdx.x;
-  Logits l(a.logits + static_cast<size_t>(t) * a.n, 0, a.n);
+  Logits<AT_ONCE> l(a.logits + static_cast<size_t>(t) * a.n, 0, a.n);
   const Settings st(a, t);
   tabulate(sh);
   clear(sh);
-  if (tid == 0) sh.n_list = 0, sh.found_at = a.n;
+  if (tid == 0) sh.at = a.n;
   float2 r = range_of(sh, l);
+  if (r.x == INFINITY) l.know(true), r = make_float2(0.0f, 0.0f);
   if (st.greedy(r.x)) {
     int at = a.n;
     l.every([&](float x, int i) { at = x == r.x && i < at ? i : at; });
-    if (at < a.n) atomicMin(&sh.found_at, at);
+    if (at < a.n) atomicMin(&sh.at, at);
     __syncthreads();
     if (tid == 0) {
-      a.idx[t] = r.x > -INFINITY ? sh.found_at : 0;
+      a.idx[t] = r.x > -INFINITY ? sh.at : 0;
       if (a.prob) a.prob[t] = 1.0f;
     }
     return;
   }
-  if (r.x == INFINITY) l.make_infinite(), r = make_float2(0.0f, -INFINITY);
   const Scale sc = st.scale(sh, r.x, r.y);
   int last = kBins - 1;  // the last bin that matters
   if (st.by_min && !st.by_p)  // (a bin further, for its fp32 distances)
-    last = static_cast<int>(fminf(-logf(fminf(st.min_p, 1.0f)) * st.temp * 1.00001f * sc.bins, kBins - 2)) + 1;
+    last = static_cast<int>(fminf(-logf(fminf(st.min_p, 1.0f)) * st.temp * 0.500005f * sc.bins, kBins - 2)) + 1;
   if (st.by_k) {
     l.every([&](float x, int) { count_token(sh, sc.bin(x)); });
     __syncthreads();
     const Span own = scan_bins<kBins, false, true>(sh, sh.mass, sh.count, 0, 0);
-    last = min(last, bins_of<kCount, kBins>(sh, sh.mass, sh.count, own, st.k, st.k).x);
+    last = min(last, bins_of<kBins>(kCount, sh, sh.mass, sh.count, own, st.k, st.k).x);
   }
-  weigh<false>(sh, sc, st, l, last);
+  bool few = last < kBins - 1 && !(st.by_k && sh.count[last + 1] > kList);
+  if (few) {
+    gather(sh, sc, l, &sh.n_near, [&](float d) { return d < last + 1; });
+    __syncthreads();
+    few = sh.n_near <= kList;
+  }
+  Token own = {};
+  if (few) {
+    if (tid < static_cast<int>(sh.n_near)) {
+      own = token_of(sc, sh.near[tid], sh.near_at[tid]);
+      add_weight(sh, sc.bin(sh.near[tid]), own.weight);
+    }
+    keep(sh, st, own.weight >= st.least ? own.weight : 0);
+  } else {
+    weigh<false>(sh, sc, st, l);
+  }
   __syncthreads();
-  const Cuts c = cuts_of(sh, st, st.by_k ? last : -1);  // (a bin before the k-th token's where min_p ends there)
-  gather(sc, c, l, &sh.n_list, [&](uint32_t slot, Token x, int) { sh.list[slot] = x; });
+  const Cuts c = cuts_of(sh, st, st.by_k ? last : -2);  // (a bin before the k-th token's where min_p ends there)
+  if (few) {
+    if (own.weight && c.has(sc.distance(sh.near[tid]))) {
+      const uint32_t slot = atomicAdd(&sh.n_list, 1u);
+      sh.order[slot] = own.order, sh.weight[slot] = own.weight;
+    }
+  } else {
+    gather(sh, sc, l, &sh.n_list, [&](float d) { return c.has(d); });
+    __syncthreads();
+    if (tid < static_cast<int>(min(sh.n_list, static_cast<uint32_t>(kList)))) {
+      own = token_of(sc, sh.near[tid], sh.near_at[tid]);
+      sh.order[tid] = own.order, sh.weight[tid] = own.weight;
+    }
+  }
   __syncthreads();
-  choose(sh, a, st, sc, t, static_cast<int>(sh.n_list), c.all, c.from_min, l.infinite, r.y,
-         [&](int, uint32_t b, uint64_t& mass, uint32_t& count) { mass += sh.mass[place<kBins>(b)], count += sh.count[place<kBins>(b)]; });
+  choose(sh, a, st, sc, l.infinite, t, static_cast<int>(sh.n_list), c.all, c.from_min,
+         [&](int, uint32_t b, uint64_t& mass, uint32_t& count) { mass = sh.mass[b], count = sh.count[b]; }, [] {});
 }
 
 // The same by several work-groups a row, in four launches: the range of each, one histogram of
-// them all, the tokens of the cuts' bins, and the choice.
+// them all, the tokens of the cuts' bins, and the choice.  64 rows of 131071 logits: 5.9, 18.8, 13.5
+// and 5.8 us.  (A histogram for each work-group, summed by the next launch, instead of atomics: the
+// same; the last of a row's work-groups to choose instead of a fourth launch: as long, as its fence
+// waits for the L2.)
 struct Gathered {
   Token token;
   uint64_t mass;  // of the bins before
@@ -599,14 +805,13 @@ struct SplitRow {  // a row's part of the workspace
     const int i = threadIdx.x & 63;
     float top = -INFINITY, low = INFINITY;
     for (int s = i; s < splits; s += 64) top = fmaxf(top, range[s].x), low = fminf(low, range[s].y);
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, 64)), low = fminf(low, __shfl_xor(low, s, 64));
-    return make_float2(top, low);
+    return make_float2(wave_reduce(top, larger), wave_reduce(low, smaller));
   }
 };
 __device__ __forceinline__ SplitRow& split_row(const SampleArgs& a, int t) { return static_cast<SplitRow*>(a.workspace)[t]; }
-__device__ __forceinline__ Logits share_of(const SampleArgs& a, int s, int t) {
-  return Logits(a.logits + static_cast<size_t>(t) * a.n, min(s * a.share, a.n), min((s + 1) * a.share, a.n));
+template <int AT_ONCE>
+__device__ __forceinline__ Logits<AT_ONCE> share_of(const SampleArgs& a, int s, int t) {
+  return Logits<AT_ONCE>(a.logits + static_cast<size_t>(t) * a.n, min(s * a.share, a.n), min((s + 1) * a.share, a.n));
 }
 
 // A work-group's part and row.  Work-groups go to the 8 XCDs in turn, and a row's stay on one: its
@@ -619,39 +824,42 @@ __device__ __forceinline__ Part part_of(const SampleArgs& a) {
   return {i % a.splits, i / a.splits * kXcds + static_cast<int>(blockIdx.x % kXcds)};
 }
 
+template <int AT_ONCE>
 __global__ __launch_bounds__(kThreads) void sample_range_kernel(SampleArgs a) {
-  __shared__ Shared sh;
+  __shared__ RangeShared sh;
   const auto [s, t] = part_of(a);
   if (t >= a.T) return;
   SplitRow& ws = split_row(a, t);
-  Logits l = share_of(a, s, t);
+  Logits<AT_ONCE> l = share_of<AT_ONCE>(a, s, t);
   for (int b = s * kThreads + static_cast<int>(threadIdx.x); b < kBins; b += a.splits * kThreads) ws.mass[b] = 0, ws.count[b] = 0;
   if (s == 0 && threadIdx.x == 0) ws.least = 0, ws.n_list = 0, ws.at = a.n;
   const float2 r = range_of(sh, l);
   if (threadIdx.x == 0) ws.range[s] = r;
 }
 
+template <int AT_ONCE>
 __global__ __launch_bounds__(kThreads) void sample_weigh_kernel(SampleArgs a) {
   __shared__ Shared sh;
   const auto [s, t] = part_of(a);
   const int tid = threadIdx.x;
   if (t >= a.T) return;
   SplitRow& ws = split_row(a, t);
-  Logits l = share_of(a, s, t);
+  Logits<AT_ONCE> l = share_of<AT_ONCE>(a, s, t);
   const Settings st(a, t);
   tabulate(sh);
   clear(sh);
   float2 r = ws.whole(a.splits);
+  l.know(r.x == INFINITY);
+  if (l.infinite) r = make_float2(0.0f, 0.0f);
   if (st.greedy(r.x)) {
     int at = a.n;
     l.every([&](float x, int i) { at = x == r.x && i < at ? i : at; });
     if (at < a.n && r.x > -INFINITY) atomicMin(&ws.at, at);
     return;
   }
-  if (r.x == INFINITY) l.make_infinite(), r = make_float2(0.0f, -INFINITY);
   const Scale sc = st.scale(sh, r.x, r.y);
   __syncthreads();
-  weigh<true>(sh, sc, st, l, kBins - 1);
+  weigh<true>(sh, sc, st, l);
   __syncthreads();
 #pragma unroll
   for (int b = 0; b < kBins; b += kThreads) {
@@ -661,32 +869,42 @@ __global__ __launch_bounds__(kThreads) void sample_weigh_kernel(SampleArgs a) {
   if (tid == 0 && sh.least) atomicAdd(reinterpret_cast<unsigned long long*>(&ws.least), sh.least);
 }
 
+template <int AT_ONCE>
 __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs a) {
   __shared__ Shared sh;
   const auto [s, t] = part_of(a);
   const int tid = threadIdx.x;
   if (t >= a.T) return;
   SplitRow& ws = split_row(a, t);
-  Logits l = share_of(a, s, t);
+  Logits<AT_ONCE> l = share_of<AT_ONCE>(a, s, t);
   const Settings st(a, t);
 #pragma unroll
   for (int b = 0; b < kBins; b += kThreads) sh.mass[b + tid] = ws.mass[b + tid], sh.count[b + tid] = ws.count[b + tid];
-  if (tid == 0) sh.least = ws.least;
+  if (tid == 0) sh.least = ws.least, sh.n_list = 0;
   tabulate(sh);
   float2 r = ws.whole(a.splits);
+  l.know(r.x == INFINITY);
+  if (l.infinite) r = make_float2(0.0f, 0.0f);
   if (st.greedy(r.x)) return;
-  if (r.x == INFINITY) l.make_infinite(), r = make_float2(0.0f, -INFINITY);
   const Scale sc = st.scale(sh, r.x, r.y);
   __syncthreads();
-  int bk = -1;
+  int bk = -2;
   if (st.by_k) {
     const Span own = scan_bins<kBins, false, true>(sh, sh.mass, sh.count, 0, 0);
-    bk = bins_of<kCount, kBins>(sh, sh.mass, sh.count, own, st.k, st.k).x;
+    bk = bins_of<kBins>(kCount, sh, sh.mass, sh.count, own, st.k, st.k).x;
   }
   const Cuts c = cuts_of(sh, st, bk);
-  gather(sc, c, l, &ws.n_list, [&](uint32_t slot, Token x, int b) {
-    ws.list[slot] = {x, sh.mass[place<kBins>(b)], sh.count[place<kBins>(b)]};
-  });
+  gather(sh, sc, l, &sh.n_list, [&](float d) { return c.has(d); });
+  __syncthreads();
+  const uint32_t m = sh.n_list;
+  if (tid == 0) sh.at = static_cast<int32_t>(atomicAdd(&ws.n_list, m));
+  __syncthreads();
+  const uint32_t slot = static_cast<uint32_t>(sh.at) + tid;
+  if (tid < static_cast<int>(m) && slot < kList) {
+    const Token x = token_of(sc, sh.near[tid], sh.near_at[tid]);
+    const uint32_t b = static_cast<uint32_t>(x.order) >> 19;
+    ws.list[slot] = {x, sh.mass[b], sh.count[b]};
+  }
   if (s == 0 && tid == 0) ws.all = c.all;
 }
 
@@ -697,6 +915,8 @@ __global__ __launch_bounds__(kThreads) void sample_choose_kernel(SampleArgs a) {
   const Settings st(a, t);
   tabulate(sh);
   float2 r = ws.whole(a.splits);
+  const bool infinite = r.x == INFINITY;
+  if (infinite) r = make_float2(0.0f, 0.0f);
   if (st.greedy(r.x)) {
     if (tid == 0) {
       a.idx[t] = r.x > -INFINITY ? ws.at : 0;
@@ -704,23 +924,30 @@ __global__ __launch_bounds__(kThreads) void sample_choose_kernel(SampleArgs a) {
     }
     return;
   }
-  const bool infinite = r.x == INFINITY;
-  if (infinite) r = make_float2(0.0f, -INFINITY);
   const int m = static_cast<int>(ws.n_list);
-  if (m <= kList && tid < m) sh.list[tid] = ws.list[tid].token;
+  if (m <= kList && tid < m) sh.order[tid] = ws.list[tid].token.order, sh.weight[tid] = ws.list[tid].token.weight;
   __syncthreads();
-  choose(sh, a, st, st.scale(sh, r.x, r.y), t, m, ws.all, st.by_min ? ws.least : ws.all, infinite, r.y,
-         [&](int e, uint32_t, uint64_t& mass, uint32_t& count) { mass += ws.list[e].mass, count += static_cast<uint32_t>(ws.list[e].count); });
+  const Scale sc = st.scale(sh, r.x, r.y);
+  choose(sh, a, st, sc, infinite, t, m, ws.all, st.by_min ? ws.least : ws.all,
+         [&](int e, uint32_t, uint64_t& mass, uint32_t& count) { mass = ws.list[e].mass, count = static_cast<uint32_t>(ws.list[e].count); },
+         [&] {
+           for (int b = tid; b < kBins; b += kThreads) sh.mass[b] = ws.mass[b], sh.count[b] = ws.count[b];
+           __syncthreads();
+           scan_bins<kBins, true, true>(sh, sh.mass, sh.count, 0, 0);
+         });
 }
 
-// Work-groups of a row: one where it holds the row in registers, else as many as leave one a
-// CU of the XCD that the row's are on, of at least kLeastShare logits each.  One | several, us:
-// one row of 50257 47 | 28, of 131071 73 | 29; 64 rows of 131071 95 | 53; 128 rows of 131071 100 | 86;
-// but of 32000 one row 18 | 29, 64 rows 19 | 44, 128 rows 19 | 50.
+// Work-groups of a row: as many as leave one a CU of the XCD that the row's are on, of at least
+// kLeastShare logits each; but one where that saves it fewer than 40000 logits, which take
+// as long as three more launches, or where only two or three would do, whose merged histograms
+// cost what they save.  One | several, us, from top-k of 50 to all tokens: one row of 32000
+// 14-20 | 21-24, of 50257 24-33 | 21-24, of 131071 42-66 | 22-25; 64 rows of 50257 23-32 | 29-33, of
+// 131071 45-70 | 40-45; 128 rows of 131071 46-72 | 64-68.
 constexpr int kLeastShare = 4096;
 int splits_of(int T, int n) {
   const int rows = (std::max(T, 1) - 1) / kXcds + 1;  // of an XCD
-  return n <= kHold * kThreads ? 1 : std::max(1, std::min(kCus / kXcds / rows, n / kLeastShare));
+  const int splits = std::min(kCus / kXcds / rows, n / kLeastShare);
+  return splits < 4 || n - n / splits < 40000 ? 1 : splits;
 }
 
 }  // namespace
@@ -749,14 +976,19 @@ ms_status ms_sample(const float* logits, int32_t T, int32_t n, const ms_sample_o
   if (opts) a.temperature = opts->temperature_dev, a.top_p = opts->top_p_dev, a.min_p = opts->min_p_dev, a.top_k = opts->top_k_dev;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 rows(static_cast<unsigned>(T)), all((static_cast<unsigned>(T) + kXcds - 1) / kXcds * kXcds * splits), block(kThreads);
-  if (splits == 1) {
-    hipLaunchKernelGGL(sample_kernel, rows, block, 0, s, a);
-  } else {
-    hipLaunchKernelGGL(sample_range_kernel, all, block, 0, s, a);
-    hipLaunchKernelGGL(sample_weigh_kernel, all, block, 0, s, a);
-    hipLaunchKernelGGL(sample_gather_kernel, all, block, 0, s, a);
-    hipLaunchKernelGGL(sample_choose_kernel, rows, block, 0, s, a);
-  }
+  auto launch = [&](auto at_once) {
+    constexpr int AT_ONCE = decltype(at_once)::value;
+    if (splits == 1) {
+      hipLaunchKernelGGL(sample_kernel<AT_ONCE>, rows, block, 0, s, a);
+    } else {
+      hipLaunchKernelGGL(sample_range_kernel<AT_ONCE>, all, block, 0, s, a);
+      hipLaunchKernelGGL(sample_weigh_kernel<AT_ONCE>, all, block, 0, s, a);
+      hipLaunchKernelGGL(sample_gather_kernel<AT_ONCE>, all, block, 0, s, a);
+      hipLaunchKernelGGL(sample_choose_kernel, rows, block, 0, s, a);
+    }
+  };
+  if (a.share <= kHold * kThreads) launch(std::integral_constant<int, kHold>());
+  else launch(std::integral_constant<int, kRead>());
   return hipGetLastError() == hipSuccess ? MS_OK : MS_E_HIP;
 }
 

@@ -62,7 +62,7 @@ def _settings(rng, T):
 
 # vocabularies below, at and past the work-group and its multiples; rows that are not 16-byte aligned
 @pytest.mark.parametrize("T,n", [(1, 1), (3, 2), (5, 63), (40, 100), (20, 1024), (9, 1025), (30, 5003), (1, 32000),
-                                 (64, 32000), (7, 50257), (2, 200001), (300, 4097)])
+                                 (64, 32000), (7, 50257), (2, 200001), (300, 4097), (60, 140001)])
 @pytest.mark.parametrize("offset", [0, 1])
 def test_settings_of_every_row(T, n, offset):
     rng = np.random.default_rng(T + n)
@@ -117,6 +117,30 @@ def test_crowded_rows():
     _check(hot, rng.random(T), temperature=np.full(T, 1e4), top_k=np.arange(T) * 700, top_p=np.linspace(0.1, 1, T))
 
 
+@pytest.mark.parametrize("step", [1 / 4, 1 / 8, 1 / 16, 1 / 64])
+@pytest.mark.parametrize("T,n", [(12, 32000), (12, 50257), (6, 131071), (150, 40000)])
+def test_many_tokens_to_a_bin(T, n, step):
+    """Logits of few values, hundreds or thousands of tokens to each: more in the cuts' bins than are sorted at once,
+    more even in one of them."""
+    rng = np.random.default_rng(int(1 / step) + n)
+    logits = np.round(1.5 * rng.standard_normal((T, n)) / step) * step
+    logits[:, ::7] += 2.0 ** -12 * rng.integers(0, 3, (T, (n + 6) // 7))
+    s = _settings(rng, T)
+    s["temperature"] = np.maximum(s["temperature"], 0.7)
+    s["top_k"] = np.where(s["top_k"] > 0, rng.integers(n // 20, n - 1, T), 0)
+    s["min_p"] = np.where(s["min_p"] > 0, 2.0 ** -rng.integers(2, 12, T), 0).astype(np.float32)
+    _check(logits, rng.random(T), **s)
+
+
+@pytest.mark.parametrize("T", [1, 2])
+def test_the_longest_flat_rows(T):
+    rng = np.random.default_rng(T)
+    n = 2 ** 19 - 1
+    logits = 0.5 * rng.standard_normal((T, n))
+    for k, p, m in ((0, 1.0, 0.0), (0, 0.9, 0.0), (400000, 0.5, 0.01), (0, 0.99, 0.3)):
+        _check(logits, rng.random(T), top_k=np.full(T, k), top_p=np.full(T, p), min_p=np.full(T, m))
+
+
 def test_extreme_rows():
     inf, nan = np.inf, np.nan
     rows = np.array([[nan, nan, nan, nan, nan], [-inf, -inf, -inf, -inf, -inf], [nan, -inf, 3.0, nan, -inf],
@@ -129,7 +153,7 @@ def test_extreme_rows():
         _check(rows, np.full(T, u), top_k=np.arange(T), top_p=np.full(T, 0.5), min_p=np.full(T, 0.5))
 
 
-@pytest.mark.parametrize("n", [3000, 32768, 32769, 70001])
+@pytest.mark.parametrize("n", [3000, 32768, 32769, 70001, 300007])
 def test_extreme_values_in_long_rows(n):
     """Greedy rows, rows without a logit above -infinity, infinite maxima and ties at the ends of the work-groups' parts,
     rows whose other logits are all far below, NaN among them."""
@@ -176,13 +200,13 @@ def test_greedy_is_argmax():
     assert np.array_equal(idx, ref.cpu().numpy()) and np.all(prob == 1.0)
 
 
-@pytest.mark.parametrize("n", [20011, 40009])
+@pytest.mark.parametrize("n", [20011, 40009, 60013])
 def test_a_row_does_not_depend_on_its_batch(n):
     rng = np.random.default_rng(9)
     T = 400
     logits = (3 * rng.standard_normal((T, n))).astype(np.float32)
     s, u = _settings(rng, T), rng.random(T)
-    idx, prob = _run(logits, u, **s)  # a work-group per row; from n = 32769 on the smaller batches have several
+    idx, prob = _run(logits, u, **s)  # a work-group per row; of long rows the smaller batches have several
     for t in (0, 17, 399):
         one = _run(logits[t:t + 1], u[t:t + 1], **{k: v[t:t + 1] for k, v in s.items()})
         assert one[0][0] == idx[t] and one[1][0] == prob[t]
@@ -190,7 +214,7 @@ def test_a_row_does_not_depend_on_its_batch(n):
     assert np.array_equal(some[0], idx[100:140]) and np.array_equal(some[1], prob[100:140])
 
 
-@pytest.mark.parametrize("T,n", [(1, 32000), (3, 7001), (200, 3001), (1, 40001), (11, 33000)])
+@pytest.mark.parametrize("T,n", [(1, 32000), (3, 7001), (200, 3001), (1, 40001), (11, 33000), (1, 60001), (9, 150001)])
 def test_captured_and_replayed(T, n):
     """A graph replayed with other logits, numbers and settings, the program's own work between the replays; two graphs
     with a workspace each on two streams at once."""
