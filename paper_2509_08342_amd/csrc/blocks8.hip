@@ -574,32 +574,34 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q_tile_kernel(DenseArgs a,
 // multiplying one, a conversion or two behind every matrix instruction (in a row before them
 // they cost 84 us for 80 below), and a wave takes 64 x 64 to 64 x 96, which has the fewest
 // conversions to a product.
-//   2048 tokens 4096 -> 6144 fp32 79-85 us (1.2-1.3 PFLOP/s; a library product of bf16 matrices
-// 76), bf16 49 (2.1 PFLOP/s; a library product of e4m3 matrices with one scale 43); 4096 tokens
-// 4096 -> 14336 375 and 219 us (1.3 and 2.2 PFLOP/s; 314 and 182); 8192 cubed 905 and 420.  Of
-// the last but one's 1.4 us per stage and CU, the matrix instructions alone take 1.2 and the
+//   2048 tokens 4096 -> 6144 fp32 78-82 us (1.3 PFLOP/s; a library product of bf16 matrices
+// 76), bf16 47 (2.2 PFLOP/s; a library product of e4m3 matrices with one scale 43); 4096 tokens
+// 4096 -> 14336 350-366 and 197-206 us (1.4 and 2.4 PFLOP/s; 314 and 182); 8192 cubed 807 and
+// 405.  Of a bf16 stage's 1.3-1.4 us per CU, the matrix instructions alone take 1.2 and the
 // loads alone 1.1 (15 TB/s from the L2s); a tile's start and end 8 us of 55.  Fetching stages ahead
 // into the L2, without waiting for them, made it slower (259 -> 292 us at the time).
+template <bool EIGHT, int BN>
+struct Pair {
+  static constexpr int BM = 256, WM = EIGHT ? 2 : 4, NWV = 8, WN = NWV / WM;  // tokens, waves
+  static constexpr int TN = BN / WN / 16, EW = TN <= 4 ? 4 : 8;               // bytes of a wave's weight exponents
+  static constexpr int STAGES = 2 * (BM + BN) * kBlock, WE = 2 * EW * WN * (kMostColumns / kBlock);
+};
+// The tile of tokens from t0 on and outputs from o0 on, of those before o_stop.
 template <typename Y, bool EIGHT, int BN>
-__global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m_tiles, int vec) {
-  constexpr int BM = 256, WM = EIGHT ? 2 : 4, NWV = 8, WN = NWV / WM;
-  constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+__device__ __forceinline__ void dense_q_pair(const DenseArgs& a, int t0, int o0, int o_stop, int vec, unsigned char* lds, uint8_t* xe,
+                                             uint8_t* we) {
+  using P = Pair<EIGHT, BN>;
+  constexpr int BM = P::BM, WM = P::WM, NWV = P::NWV, WN = P::WN;
+  constexpr int TM = BM / WM / 16, TN = P::TN, EW = P::EW;
   constexpr int NX = BM / 8 / NWV, NL = (BM + BN) / 8 / NWV;  // loads per wave and stage: tokens', all
   constexpr int SBYTES = (BM + BN) * kBlock;
-  constexpr int EW = TN <= 4 ? 4 : 8;  // bytes of a wave's weight exponents
   static_assert(TM % 4 == 0 && TM <= 8 && TN <= 8 && TN * WN * 16 == BN && BN % (8 * NWV) == 0 && NL <= 8, "tile split");
-  static_assert(2 * SBYTES + kTileExps + 2 * EW * WN * (kMostColumns / kBlock) <= 160 * 1024, "LDS");
+  static_assert(P::STAGES + kTileExps + P::WE <= 160 * 1024, "LDS");
   constexpr auto paired = [](int n) { return sizeof(Y) == 2 && (n | 1) < TN; };
-  __shared__ __align__(16) unsigned char lds[2 * SBYTES];
-  __shared__ __align__(4) uint8_t xe[kTileExps];  // [blocks of columns][WM][16 lanes][TM]
-  __shared__ __align__(4) uint8_t we[2 * EW * WN * (kMostColumns / kBlock)];  // [blocks of columns][WN][lanes' halves][EW]
   const int lane = threadIdx.x & 63, i16 = lane & 15, g4 = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool second = wv >= 4;
   const int wm = wv % WM, wn = wv / WM;
-  const int2 tile = tile_of(blockIdx.x, gridDim.x, m_tiles);
-  // (the divisions are the vector unit's)
-  const int t0 = __builtin_amdgcn_readfirstlane(tile.x) * BM, o0 = __builtin_amdgcn_readfirstlane(tile.y) * BN;
   const uint8_t *x0 = a.x + static_cast<size_t>(t0) * a.n_in, *w0 = a.w + static_cast<size_t>(o0) * a.n_in;
 
   // Staged rows: the tile's tokens, then its outputs, the last of either again.  Piece p of a
@@ -607,7 +609,7 @@ __global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m
   // where r / 8 is odd: so the eight rows that are read together have distinct slots in either
   // order.  A load takes eight rows from a uniform address on; lanes' offsets to them are all
   // alike but where the rows end, and from there on.
-  const int x_end = min(BM, a.T - t0) - 1, w_end = min(BN, a.n_out - o0) - 1;
+  const int x_end = min(BM, a.T - t0) - 1, w_end = min(BN, o_stop - o0) - 1;
   const int lrow = lane >> 3, xk = 16 * ((lane & 7) ^ lrow), wk = xk ^ 64 * (wv & 1);
   const uint32_t x_off = lrow * a.n_in + xk, w_off = lrow * a.n_in + wk;
   const uint32_t x_last = min(lrow, x_end % 8) * a.n_in + xk, w_last = min(lrow, w_end % 8) * a.n_in + wk;
@@ -748,25 +750,31 @@ __global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m
   clear_ends(1);
   __syncthreads();  // two stages and the exponents are there
   auto none = [](int) {};
-  if (second) {
-    change();
-    for (int sl = 0; sl < a.nb; ++sl) {
+  auto turn = [&](int sl, bool first) {  // (stages 0 and 1 are there already: the first turn loads less)
+    if (second) {
       read(sl, none);
       msk::wait_vm<0>();
-      if (sl > 0) clear_ends(sl + 1);
+      if (!first) clear_ends(sl + 1);
       change();
       multiply([&](int j) { issue(sl + 2, j); });
-      change();
-    }
-  } else {
-    for (int sl = 0; sl < a.nb; ++sl) {
-      read(sl, [&](int j) { if (sl > 0) issue(sl + 1, j); });
+    } else {
+      read(sl, [&](int j) { if (!first) issue(sl + 1, j); });
       change();
       multiply(none);
       msk::wait_vm<0>();
-      if (sl > 0) clear_ends(sl + 1);
-      change();
+      if (!first) clear_ends(sl + 1);
     }
+    change();
+  };
+  auto turns = [&]() {  // (the first apart from the loop: 8192 cubed fp32 820 -> 804 us, but bf16 410 -> 445)
+    if (!EIGHT) turn(0, true);
+    for (int sl = EIGHT ? 0 : 1; sl < a.nb; ++sl) turn(sl, EIGHT && sl == 0);
+  };
+  if (second) {
+    change();
+    turns();
+  } else {
+    turns();
     change();
   }
   msk::wait_vm<0>();  // the reloads past the last stage land before the work-group ends
@@ -785,6 +793,24 @@ __global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m
   }
 }
 
+// Tiles of BN outputs, and of REST from output o_split on in the last `rest` work-groups.
+template <typename Y, bool EIGHT, int BN, int REST>
+__global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m_tiles, int vec, int o_split, int rest) {
+  __shared__ __align__(16) unsigned char lds[Pair<EIGHT, BN>::STAGES];
+  __shared__ __align__(4) uint8_t xe[kTileExps];               // [blocks of columns][WM][16 lanes][TM]
+  __shared__ __align__(4) uint8_t we[Pair<EIGHT, BN>::WE];  // [blocks of columns][WN][lanes' halves][EW]
+  static_assert(REST <= BN, "LDS");
+  const int first = static_cast<int>(gridDim.x) - rest, w = blockIdx.x;
+  const bool is_rest = REST != BN && w >= first;
+  const int2 tile = is_rest ? tile_of(w - first, rest, m_tiles) : tile_of(w, first, m_tiles);
+  // (the divisions are the vector unit's)
+  const int t0 = __builtin_amdgcn_readfirstlane(tile.x) * Pair<EIGHT, BN>::BM, at = __builtin_amdgcn_readfirstlane(tile.y);
+  if (is_rest)
+    dense_q_pair<Y, EIGHT, REST>(a, t0, o_split + at * REST, a.n_out, vec, lds, xe, we);
+  else
+    dense_q_pair<Y, EIGHT, BN>(a, t0, at * BN, o_split, vec, lds, xe, we);
+}
+
 // Tile of a launch: the one whose rounds over the CUs cost least, by the times (0.1 us) of
 // one full launch at 4096 columns, fp32 and bf16 results, with one work-group per CU and
 // with two, of which the small tiles' overlap.
@@ -793,27 +819,45 @@ struct Tile {
   int bm, bn, threads;  // tokens, outputs
   int one[2], two[2];   // cost of a round
 };
-constexpr Tile kTiles[] = {{32, 32, 256, {124, 84}, {148, 102}},   {64, 64, 256, {193, 124}, {262, 167}},
-                           {128, 128, 512, {406, 256}, {785, 496}}, {256, 128, 512, {622, 425}, {1187, 824}},
-                           {256, 192, 512, {803, 499}, {1588, 984}}, {256, 256, 512, {0, 589}, {0, 1179}}};
+constexpr Tile kTiles[] = {{32, 32, 256, {125, 85}, {137, 100}},   {64, 64, 256, {190, 120}, {243, 158}},
+                           {128, 128, 512, {390, 238}, {730, 448}}, {256, 128, 512, {587, 391}, {1128, 752}},
+                           {256, 192, 512, {766, 474}, {1492, 914}}, {256, 256, 512, {0, 562}, {0, 1081}}};
+// Whole rounds of one of the two largest tiles, and the outputs that are left in the third: 4096
+// tokens 4096 -> 14336 bf16 205 us with the largest alone and 197 with both, 8192 cubed fp32 850 and
+// 806, 2048 tokens 4096 -> 14336 fp32 212 and 197.
+constexpr int kRest = 3, kFirstMixed = 4;
+static_assert(kTiles[kRest].bm == kTiles[kFirstMixed].bm, "the same tokens");
 
 template <typename Y, bool EIGHT>
 ms_status launch_tiles(const DenseArgs& a, int vec, hipStream_t s) {
-  auto count = [&](const Tile& t) {
-    return ((static_cast<int64_t>(a.T) + t.bm - 1) / t.bm) * ((static_cast<int64_t>(a.n_out) + t.bn - 1) / t.bn);
+  auto count = [&](const Tile& t, int64_t outputs) {
+    return ((static_cast<int64_t>(a.T) + t.bm - 1) / t.bm) * ((outputs + t.bn - 1) / t.bn);
   };
-  int best = -1;
+  auto rounds = [&](const Tile& t, int64_t n) {
+    const int64_t rest = n % (2 * kCus);
+    return n / (2 * kCus) * t.two[EIGHT] + (rest == 0 ? 0 : rest <= kCus ? t.one[EIGHT] : t.two[EIGHT]);
+  };
+  auto fits = [&](const Tile& t, int64_t n) {  // a launch, and the exponents' LDS
+    return n * t.threads <= UINT32_MAX && a.nb * t.bm <= kTileExps;
+  };
+  int best = -1, o_split = a.n_out;
   int64_t best_cost = INT64_MAX;
   for (int i = 0; i < (EIGHT ? 6 : 5); ++i) {
     const Tile& t = kTiles[i];
-    const int64_t n = count(t), rest = n % (2 * kCus);
-    if (n * t.threads > UINT32_MAX || a.nb * t.bm > kTileExps) continue;  // past a launch, or the exponents' LDS
-    const int64_t cost = n / (2 * kCus) * t.two[EIGHT] + (rest == 0 ? 0 : rest <= kCus ? t.one[EIGHT] : t.two[EIGHT]);
-    if (cost < best_cost) best = i, best_cost = cost;
+    const int64_t n = count(t, a.n_out);
+    if (!fits(t, n)) continue;
+    if (const int64_t cost = rounds(t, n); cost < best_cost) best = i, best_cost = cost, o_split = a.n_out;
+    // whole rounds of large tiles, and smaller ones for the outputs that are left
+    if (i < kFirstMixed || n < kCus) continue;
+    const int64_t m = (a.T - 1) / t.bm + 1, wide = n / kCus * kCus / m, left = a.n_out - wide * t.bn;
+    if (wide == 0 || left <= 0 || !fits(t, wide * m + count(kTiles[kRest], left))) continue;
+    const int64_t cost = rounds(t, wide * m) + rounds(kTiles[kRest], count(kTiles[kRest], left));
+    if (cost < best_cost) best = i, best_cost = cost, o_split = static_cast<int>(wide * t.bn);
   }
   if (best < 0) return MS_E_UNSUPPORTED;
   const int m_tiles = (a.T - 1) / kTiles[best].bm + 1;
-  const dim3 grid(static_cast<unsigned>(count(kTiles[best]))), block(kTiles[best].threads);
+  const int rest = static_cast<int>(count(kTiles[kRest], a.n_out - o_split));
+  const dim3 grid(static_cast<unsigned>(count(kTiles[best], o_split) + rest)), block(kTiles[best].threads);
 #define MSK_TILE_CASE(I_, BM_, BN_, WM_, WN_, NST_)                                                                  \
   case I_:                                                                                                           \
     static_assert(kTiles[I_].bm == BM_ && kTiles[I_].bn == BN_ && kTiles[I_].threads == 64 * WM_ * WN_, "tiles");        \
@@ -822,8 +866,12 @@ ms_status launch_tiles(const DenseArgs& a, int vec, hipStream_t s) {
 #define MSK_PAIR_CASE(I_, BN_)                                                                               \
   case I_:                                                                                                   \
     static_assert(kTiles[I_].bm == 256 && kTiles[I_].bn == BN_ && kTiles[I_].threads == 512, "tiles");           \
-    if constexpr (EIGHT || BN_ < 256)                                                                        \
-      hipLaunchKernelGGL((dense_q_pair_kernel<Y, EIGHT, BN_>), grid, block, 0, s, a, m_tiles, vec);      \
+    if constexpr (EIGHT || BN_ < 256) {                                                                      \
+      if (o_split == a.n_out)                                                                            \
+        hipLaunchKernelGGL((dense_q_pair_kernel<Y, EIGHT, BN_, BN_>), grid, block, 0, s, a, m_tiles, vec, o_split, 0); \
+      else                                                                                               \
+        hipLaunchKernelGGL((dense_q_pair_kernel<Y, EIGHT, BN_, 128>), grid, block, 0, s, a, m_tiles, vec, o_split, rest); \
+    }                                                                                                    \
     break;
   switch (best) {
     MSK_TILE_CASE(0, 32, 32, 2, 2, 4)
