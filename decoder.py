@@ -43,7 +43,8 @@ NORM_EPS = 1e-6  # of ms_residual_norm
 
 class Sampling:
     """How the tokens of one sequence are drawn: settings as in ms_sample, random
-    numbers from a seeded generator on the device, n of them made at a time."""
+    numbers from a seeded generator on the device, n of them made at a time.  Draws
+    follow each other, on one stream or on streams that wait for each other."""
 
     def __init__(self, vocab, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, seed=0, n=1024):
         def one(v, dtype):

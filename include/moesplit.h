@@ -649,11 +649,11 @@ ms_status ms_residual_norm_q(const void* h, const void* y, int32_t y_dtype, cons
 
 /* y[t][o] = sum_i x[t][i] w[o][i] (+ add[t][o] if add is not NULL): x [T][n_in] in
  * 8 bits with R = 1, w [n_out][n_in] with R = 128, y and add [T][n_out] y_dtype
- * (add may be y; other overlaps with y are MS_E_INVALID).  Sums in fp32.  An fp32 y is as exact as fp32 products and
- * sums are; a bf16 y may be off, before its rounding, by 2^-12 of the largest of
- * every eight neighbouring products (relative to a result about 2e-5): it is
- * computed on the 8-bit matrix cores where there are many tokens.  A code of NaN
- * makes the results of its row NaN. */
+ * (add may be y; other overlaps with y are MS_E_INVALID).  Sums in fp32.  An fp32
+ * y is as exact as fp32 products and sums are; a bf16 y may be off, before its
+ * rounding, by 2^-12 of the largest of every eight neighbouring products
+ * (relative to a result about 2e-5): it is computed on the 8-bit matrix cores
+ * where there are many tokens.  A code of NaN makes the results of its row NaN. */
 ms_status ms_dense_q(const void* x, const void* x_exp, const void* w, const void* w_exp, int32_t T, int32_t n_in,
                      int32_t n_out, void* y, int32_t y_dtype, const void* add, void* stream);
 
@@ -672,7 +672,7 @@ typedef struct {
 } ms_sample_opts;
 
 /* Device bytes that ms_sample needs at workspace_dev (0: none), whatever the
- * settings; pure host arithmetic. */
+ * settings; fewer rows may need more.  Pure host arithmetic. */
 ms_status ms_sample_workspace(int32_t T, int32_t n, uint64_t* bytes_out);
 
 /* A token per row of logits [T][n] (fp32; n at most 524287, MS_E_UNSUPPORTED beyond;
@@ -686,8 +686,8 @@ ms_status ms_sample_workspace(int32_t T, int32_t n, uint64_t* bytes_out);
  * without a logit above -infinity gives 0.  Weights are whole numbers of 2^-45 of
  * the largest, smaller ones zero: the same inputs give the same token whatever else
  * runs, and whatever T.  opts NULL: temperature 1.
- * workspace_dev: 16-byte aligned, used until the call has finished on `stream`;
- * calls that may overlap in time need one each. */
+ * Outputs overlap nothing (MS_E_INVALID).  workspace_dev: 16-byte aligned, used until
+ * the call has finished on `stream`; calls that may overlap in time need one each. */
 ms_status ms_sample(const float* logits, int32_t T, int32_t n, const ms_sample_opts* opts, const float* u_dev,
                     int32_t* idx_out, float* prob_out, void* workspace_dev, uint64_t workspace_bytes, void* stream);
 

@@ -18,6 +18,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <iterator>
 #include <type_traits>
 
 #include "kernels.h"
@@ -950,6 +951,11 @@ int splits_of(int T, int n) {
   return splits < 4 || n - n / splits < 40000 ? 1 : splits;
 }
 
+bool overlap(const void* p, size_t np, const void* q, size_t nq) {
+  const auto a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return p && q && a < b + nq && b < a + np;
+}
+
 }  // namespace
 
 extern "C" {
@@ -970,10 +976,18 @@ ms_status ms_sample(const float* logits, int32_t T, int32_t n, const ms_sample_o
   if (!logits || !u_dev || !idx_out) return MS_E_INVALID;
   if (need > 0 && (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15u) || workspace_bytes < need))
     return MS_E_INVALID;
+  const size_t values = 4 * static_cast<size_t>(T);
+  const ms_sample_opts given = opts ? *opts : ms_sample_opts{};
+  auto apart = [&](const void* o) {
+    const void* const rows[] = {u_dev, given.temperature_dev, given.top_k_dev, given.top_p_dev, given.min_p_dev};
+    return std::none_of(std::begin(rows), std::end(rows), [&](const void* q) { return overlap(o, values, q, values); }) &&
+           !overlap(o, values, logits, values * n) && !overlap(o, values, workspace_dev, need);
+  };
+  if (!apart(idx_out) || !apart(prob_out) || overlap(idx_out, values, prob_out, values)) return MS_E_INVALID;
   if (T > UINT32_MAX / kThreads) return MS_E_UNSUPPORTED;
   const int splits = splits_of(T, n);
-  SampleArgs a = {logits, u_dev, nullptr, nullptr, nullptr, nullptr, idx_out, prob_out, T, n, splits, (n - 1) / splits + 1, workspace_dev};
-  if (opts) a.temperature = opts->temperature_dev, a.top_p = opts->top_p_dev, a.min_p = opts->min_p_dev, a.top_k = opts->top_k_dev;
+  const SampleArgs a = {logits, u_dev, given.temperature_dev, given.top_p_dev, given.min_p_dev, given.top_k_dev, idx_out, prob_out,
+                        T, n, splits, (n - 1) / splits + 1, workspace_dev};
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 rows(static_cast<unsigned>(T)), all((static_cast<unsigned>(T) + kXcds - 1) / kXcds * kXcds * splits), block(kThreads);
   auto launch = [&](auto at_once) {

@@ -173,6 +173,11 @@ def test_sample_refusals():
             big = [_z(T, n, dtype=torch.float32), _z(T, dtype=torch.float32), _z(T, dtype=torch.int32)]
             for ws in (None, _z(need - 1), _z(need, shift=8)):
                 assert _status(ms.ms_sample, big[0], T, n, None, big[1], big[2], None, ws) == ms.MS_E_INVALID
+    opts, prob = ms.sample_opts(u, i, None, u), _z(2, dtype=torch.float32)
+    for idx, out in ((l.view(-1)[98:].view(torch.int32), prob), (u.view(torch.int32), None), (i, None), (i, u), (prob.view(torch.int32), prob)):
+        assert _status(ms.ms_sample, l, 2, 50, opts, u, idx, out) == ms.MS_E_INVALID  # over the logits, settings, each other
+    ws = _z(ms.ms_sample_workspace(1, 200000))
+    assert _status(ms.ms_sample, _z(1, 200000, dtype=torch.float32), 1, 200000, None, u[:1], ws[:4].view(torch.int32), None, ws) == ms.MS_E_INVALID
     with pytest.raises(ValueError):
         ms.sample_opts(top_k=u)
     with pytest.raises(ValueError):
