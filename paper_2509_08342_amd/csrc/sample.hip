@@ -119,6 +119,7 @@ __device__ __forceinline__ T group_sum(T x, int P) {
 
 // What a row's tokens are weighed with.
 constexpr int kPowers = 256;
+constexpr double kLn2 = 0.69314718055994530942;
 struct Scale {
   double inv;   // kPowers / (ln 2 temperature)
   double top;   // the largest logit (finite)
@@ -134,7 +135,7 @@ struct Scale {
   // rest, |r| <= 1/2, to its fourth power (the next term is 2^-54)
   __device__ __forceinline__ uint64_t weight(float l) const {
     const double y = fmax((l - top) * inv, -kFar - kPowers);  // (NaN, of an endless temperature, too)
-    constexpr double L = 0.69314718055994530942 / kPowers;
+    constexpr double L = kLn2 / kPowers;
     constexpr double kWhole = 6755399441055744.0;  // 1.5 2^52: a sum with it is rounded to whole numbers
     const double z = y + kWhole, r = y - (z - kWhole);
     double s = fma(r, L * L * L * L / 24, L * L * L / 6);
@@ -234,33 +235,40 @@ __device__ __forceinline__ Span scan_bins(Shared& sh, uint64_t* mass, uint32_t* 
   return own;
 }
 
-// Where a prefix ends: at the token that makes it t long, that takes its mass to t, or past t.
+// Where a prefix ends: at the token that makes it t long, that takes its mass to t, or past t.  As
+// whole numbers: the prefix before is short of `length`, or of `mass`.
 enum Cut { kCount, kReach, kPass };
+struct Limit {
+  Cut cut;
+  uint64_t mass;
+  uint32_t length;
 
-// Whether the prefix before `mass` and `count` is still short of the cut.
-__device__ __forceinline__ bool is_short(Cut cut, double t, uint64_t mass, uint32_t count) {
-  return cut == kCount ? count < t : cut == kReach ? static_cast<double>(mass) < t : static_cast<double>(mass) <= t;
+  __device__ __forceinline__ bool is_short(uint64_t m, uint32_t n) const { return cut == kCount ? n < length : m < mass; }
+};
+__device__ __forceinline__ Limit limit(Cut cut, double t) {  // 0 <= t < 2^64
+  const uint64_t m = uniform(static_cast<uint64_t>(cut == kPass ? floor(t) : ceil(t)));
+  return {cut, m + (cut == kPass), static_cast<uint32_t>(min(m, static_cast<uint64_t>(UINT32_MAX)))};
 }
 
-// The bins in which the cuts at t0 and t1 lie, from exclusive sums: of the threads whose bins
+// The bins in which the cuts at l0 and l1 lie, from exclusive sums: of the threads whose bins
 // they may be in exactly one looks (the last where rounding leaves none).
 template <int BINS>  // (found_bin[cut] has to be free)
-__device__ __forceinline__ int2 bins_of(Cut cut, Shared& sh, const uint64_t* mass, const uint32_t* count, const Span& own, double t0, double t1) {
+__device__ __forceinline__ int2 bins_of(Shared& sh, const uint64_t* mass, const uint32_t* count, const Span& own, const Limit& l0, const Limit& l1) {
   constexpr int PER = BINS / kThreads;
   const int tid = threadIdx.x;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const double t = i ? t1 : t0;
-    if ((tid == 0 || is_short(cut, t, own.mass0, own.count0)) && (tid == kThreads - 1 || !is_short(cut, t, own.mass1, own.count1))) {
+    const Limit& l = i ? l1 : l0;
+    if ((tid == 0 || l.is_short(own.mass0, own.count0)) && (tid == kThreads - 1 || !l.is_short(own.mass1, own.count1))) {
       int b = tid * PER;
 #pragma unroll
       for (int j = 1; j < PER; ++j)
-        if (is_short(cut, t, mass[tid * PER + j], count[tid * PER + j])) b = tid * PER + j;
-      sh.found_bin[cut][i] = b;
+        if (l.is_short(mass[tid * PER + j], count[tid * PER + j])) b = tid * PER + j;
+      sh.found_bin[l.cut][i] = b;
     }
   }
   __syncthreads();
-  return make_int2(sh.found_bin[cut][0], sh.found_bin[cut][1]);
+  return make_int2(sh.found_bin[l0.cut][0], sh.found_bin[l0.cut][1]);
 }
 
 struct End {
@@ -384,6 +392,7 @@ __device__ __forceinline__ float2 range_of(RangeShared& sh, L& l) {
 // A row's settings, and the scale that they and its range give.
 struct Settings {
   float temp, drawn, p, min_p;
+  double inv;  // of the scale
   int k;
   bool by_k, by_p, by_min;
   uint64_t least;  // units that min_p asks for
@@ -398,6 +407,7 @@ struct Settings {
         by_p(p < 1.0f),
         by_min(min_p > 0.0f),
         least(0) {
+    inv = uniform(kPowers / kLn2 / temp);
     // (computed once: the compiler would do it again at every use)
     if (by_min) least = uniform(static_cast<uint64_t>(ceil(fmin(static_cast<double>(min_p), 1.0) * kUnit)));
   }
@@ -405,9 +415,8 @@ struct Settings {
   __device__ __forceinline__ double share() const { return fmax(static_cast<double>(p), 0.0); }
   __device__ __forceinline__ bool greedy(float top) const { return !(temp > 0.0f) || top == -INFINITY; }
   __device__ __forceinline__ Scale scale(const Shared& sh, float top, float low) const {
-    constexpr double kLn2 = 0.69314718055994530942;
     Scale sc;
-    sc.inv = uniform(kPowers / kLn2 / temp);
+    sc.inv = inv;
     sc.top = uniform(static_cast<double>(top)), sc.half = uniform(0.5f * top);
     sc.powers = sh.powers;
     const float span = fminf(sc.half - 0.5f * low, static_cast<float>(kFar / kPowers * kLn2 / 2) * temp);
@@ -492,11 +501,12 @@ __device__ __forceinline__ Cuts cuts_of(Shared& sh, const Settings& st, int bk) 
   uint64_t lo = c.all, hi = c.all;
   if (bk >= 0) lo = at(bk), hi = after(bk);
   if (st.by_p) {
-    c.p = bins_of<kBins>(kReach, sh, sh.mass, sh.count, own, share * static_cast<double>(lo), share * static_cast<double>(hi));
+    c.p = bins_of<kBins>(sh, sh.mass, sh.count, own, limit(kReach, share * static_cast<double>(lo)),
+                         limit(kReach, share * static_cast<double>(hi)));
     lo = min(lo, at(c.p.x)), hi = min(hi, after(c.p.y));
   }
   lo = min(lo, c.from_min), hi = min(hi, c.from_min);
-  c.u = bins_of<kBins>(kPass, sh, sh.mass, sh.count, own, u * static_cast<double>(lo), u * static_cast<double>(hi));
+  c.u = bins_of<kBins>(sh, sh.mass, sh.count, own, limit(kPass, u * static_cast<double>(lo)), limit(kPass, u * static_cast<double>(hi)));
   return c;
 }
 
@@ -519,6 +529,7 @@ __device__ __forceinline__ void gather(Shared& sh, const Scale& sc, L& l, uint32
     if ((threadIdx.x & 63) == 0) slot = atomicAdd(n, all);
     slot = uniform(slot) + upto - own;
     l.template steps<8>(from, [&](int g) {
+      if (!__any(mask >> g & 255)) return;
 #pragma unroll
       for (int i = g; i < g + 8; ++i) {
         if (!(mask >> i & 1)) continue;
@@ -532,25 +543,25 @@ __device__ __forceinline__ void gather(Shared& sh, const Scale& sc, L& l, uint32
 // A cut among the tokens of keys kmin to kmax, with base and rank before them, where they are more
 // than the list holds (many equal logits, or an outlier that stretches the bins): the range of keys
 // is divided by 1024 until one is left, then its tokens are counted.
-__device__ End cut_in_range(Cut cut, Shared& sh, Scale sc, const float* row, int n, bool infinite, uint32_t kmin, uint32_t kmax,
-                            uint64_t base, uint32_t rank, double t) {
+__device__ End cut_in_range(const Limit& l, Shared& sh, Scale sc, const float* row, int n, bool infinite, uint32_t kmin, uint32_t kmax,
+                            uint64_t base, uint32_t rank) {
   const int tid = threadIdx.x;
   while (kmax > kmin) {
     const int shift = max(0, 32 - __clz(kmax - kmin) - 10);
     sh.sub.mass[tid] = 0, sh.sub.count[tid] = 0;
     __syncthreads();
     for (int i = tid; i < n; i += kThreads) {
-      const float l = logit(row[i], infinite);
-      const uint32_t key = order_key(l);
-      if (!(l > -INFINITY) || key < kmin || key > kmax) continue;
-      const uint64_t w = sc.weight(l);
+      const float x = logit(row[i], infinite);
+      const uint32_t key = order_key(x);
+      if (!(x > -INFINITY) || key < kmin || key > kmax) continue;
+      const uint64_t w = sc.weight(x);
       if (!w) continue;
       atomicAdd(reinterpret_cast<unsigned long long*>(&sh.sub.mass[(kmax - key) >> shift]), w);
       atomicAdd(&sh.sub.count[(kmax - key) >> shift], 1u);
     }
     __syncthreads();
     const Span own = scan_bins<kSubBins, true, true>(sh, sh.sub.mass, sh.sub.count, base, rank);
-    const uint32_t b = bins_of<kSubBins>(cut, sh, sh.sub.mass, sh.sub.count, own, t, t).x;
+    const uint32_t b = bins_of<kSubBins>(sh, sh.sub.mass, sh.sub.count, own, l, l).x;
     base = sh.sub.mass[b], rank = sh.sub.count[b];
     kmax -= b << shift;
     kmin = max(kmin, kmax - ((1u << shift) - 1));
@@ -558,7 +569,7 @@ __device__ End cut_in_range(Cut cut, Shared& sh, Scale sc, const float* row, int
   }
   // the tokens of one value, by their index: the first with enough before it
   const uint64_t w = sc.weight(key_value(kmax));
-  auto& f = sh.found[cut];
+  auto& f = sh.found[l.cut];
   if (tid == 0) f.at = -1, f.mass = ~0ull;
   __syncthreads();
   for (int i0 = 0; i0 < n; i0 += kThreads) {
@@ -573,7 +584,7 @@ __device__ End cut_in_range(Cut cut, Shared& sh, Scale sc, const float* row, int
       every += sh.wave_count[v];
     }
     const uint64_t mass = base + earlier * w;
-    if (is && !is_short(cut, t, mass + w, rank + earlier + 1) && (is_short(cut, t, mass, rank + earlier) || mass == 0))
+    if (is && !l.is_short(mass + w, rank + earlier + 1) && (l.is_short(mass, rank + earlier) || mass == 0))
       f.mass = mass + w, f.at = i;
     base += every * w, rank += every;
     __syncthreads();
@@ -630,9 +641,9 @@ __device__ __forceinline__ Place sorted(Shared& sh, int m, Earlier earlier) {
 
 // A cut among them: each knows what is before it, and one of them is the end (own is 0 for
 // threads without one).
-__device__ __forceinline__ End cut_in_list(Cut cut, Shared& sh, double t, const Place& p) {
-  auto& f = sh.found[cut];  // as tabulate() left it where none is: all are kept
-  if (p.own && !is_short(cut, t, p.before + p.own, p.rank + 1) && (is_short(cut, t, p.before, p.rank) || p.before == 0))
+__device__ __forceinline__ End cut_in_list(const Limit& l, Shared& sh, const Place& p) {
+  auto& f = sh.found[l.cut];  // as tabulate() left it where none is: all are kept
+  if (p.own && !l.is_short(p.before + p.own, p.rank + 1) && (l.is_short(p.before, p.rank) || p.before == 0))
     f.mass = p.before + p.own, f.weight = p.own, f.at = p.token;
   __syncthreads();
   return {f.mass, f.weight, f.at};
@@ -640,16 +651,16 @@ __device__ __forceinline__ End cut_in_list(Cut cut, Shared& sh, double t, const 
 
 // A cut by the exclusive sums of all bins and the tokens of the one that it lies in.
 template <typename L>
-__device__ __forceinline__ End cut_in_bin(Cut cut, Shared& sh, const Scale& sc, L& l, int n, double t) {
+__device__ __forceinline__ End cut_in_bin(const Limit& limit, Shared& sh, const Scale& sc, L& l, int n) {
   const int tid = threadIdx.x;
   for (int b = tid; b < kBins; b += kThreads) {
-    if ((b == 0 || is_short(cut, t, sh.mass[b], sh.count[b])) &&
-        (b == kBins - 1 || !is_short(cut, t, sh.mass[b + 1], sh.count[b + 1])))
-      sh.found_bin[cut][0] = b;
+    if ((b == 0 || limit.is_short(sh.mass[b], sh.count[b])) &&
+        (b == kBins - 1 || !limit.is_short(sh.mass[b + 1], sh.count[b + 1])))
+      sh.found_bin[limit.cut][0] = b;
   }
   if (tid == 0) sh.n_list = 0, sh.key_low = ~0u, sh.key_top = 0;
   __syncthreads();
-  const int b = sh.found_bin[cut][0];
+  const int b = sh.found_bin[limit.cut][0];
   const uint64_t mass = sh.mass[b];
   const uint32_t count = sh.count[b];
   auto in = [&](float d) { return d >= b && d < b + 1; };
@@ -663,7 +674,7 @@ __device__ __forceinline__ End cut_in_bin(Cut cut, Shared& sh, const Scale& sc, 
     }
     __syncthreads();
     const Place p = sorted(sh, m, [&](int, uint32_t, uint64_t& x, uint32_t& y) { x = mass, y = count; });
-    const End e = cut_in_list(cut, sh, t, p);
+    const End e = cut_in_list(limit, sh, p);
     if (tid == 0) sh.mass[b] = mass, sh.count[b] = count;
     __syncthreads();
     return e;
@@ -675,7 +686,7 @@ __device__ __forceinline__ End cut_in_bin(Cut cut, Shared& sh, const Scale& sc, 
   });
   if (top) atomicMin(&sh.key_low, low), atomicMax(&sh.key_top, top);
   __syncthreads();
-  return cut_in_range(cut, sh, sc, l.row, n, l.infinite, sh.key_low, sh.key_top, mass, count, t);
+  return cut_in_range(limit, sh, sc, l.row, n, l.infinite, sh.key_low, sh.key_top, mass, count);
 }
 
 // The choice among the m gathered tokens of sh.order and sh.weight; where there are more than the
@@ -688,10 +699,10 @@ __device__ __forceinline__ void choose(Shared& sh, const SampleArgs& a, const Se
   End end;
   if (m <= kList) {
     const Place p = sorted(sh, m, earlier);
-    if (st.by_k) M = min(M, cut_in_list(kCount, sh, st.k, p).mass);
-    if (st.by_p) M = min(M, cut_in_list(kReach, sh, share * static_cast<double>(M), p).mass);
+    if (st.by_k) M = min(M, cut_in_list(limit(kCount, st.k), sh, p).mass);
+    if (st.by_p) M = min(M, cut_in_list(limit(kReach, share * static_cast<double>(M)), sh, p).mass);
     M = min(M, from_min);
-    end = cut_in_list(kPass, sh, u * static_cast<double>(M), p);
+    end = cut_in_list(limit(kPass, u * static_cast<double>(M)), sh, p);
   } else {
     all();
     Logits<kRead> l(a.logits + static_cast<size_t>(t) * a.n, 0, a.n);
@@ -700,7 +711,7 @@ __device__ __forceinline__ void choose(Shared& sh, const SampleArgs& a, const Se
     for (int c = st.by_k ? kCount : st.by_p ? kReach : kPass; c <= kPass; ++c) {
       if (c == kReach && !st.by_p) continue;
       if (c == kPass) M = min(M, from_min);
-      end = cut_in_bin(static_cast<Cut>(c), sh, sc, l, a.n, c == kCount ? st.k : (c == kReach ? share : u) * static_cast<double>(M));
+      end = cut_in_bin(limit(static_cast<Cut>(c), c == kCount ? st.k : (c == kReach ? share : u) * static_cast<double>(M)), sh, sc, l, a.n);
       if (c < kPass) M = min(M, end.mass);
     }
   }
@@ -745,7 +756,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     l.every([&](float x, int) { count_token(sh, sc.bin(x)); });
     __syncthreads();
     const Span own = scan_bins<kBins, false, true>(sh, sh.mass, sh.count, 0, 0);
-    last = min(last, bins_of<kBins>(kCount, sh, sh.mass, sh.count, own, st.k, st.k).x);
+    last = min(last, bins_of<kBins>(sh, sh.mass, sh.count, own, limit(kCount, st.k), limit(kCount, st.k)).x);
   }
   bool few = last < kBins - 1 && !(st.by_k && sh.count[last + 1] > kList);
   if (few) {
@@ -892,7 +903,7 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs a) {
   int bk = -2;
   if (st.by_k) {
     const Span own = scan_bins<kBins, false, true>(sh, sh.mass, sh.count, 0, 0);
-    bk = bins_of<kBins>(kCount, sh, sh.mass, sh.count, own, st.k, st.k).x;
+    bk = bins_of<kBins>(sh, sh.mass, sh.count, own, limit(kCount, st.k), limit(kCount, st.k)).x;
   }
   const Cuts c = cuts_of(sh, st, bk);
   gather(sh, sc, l, &sh.n_list, [&](float d) { return c.has(d); });
