@@ -268,6 +268,52 @@ def test_dense_nan_stays_in_its_row(T, n_in, n_out, dtype):
     assert np.array_equal(nan, want)
 
 
+def test_rows_past_32_bits():
+    """Rows whose values lie past 2^32 of a matrix, its codes or its results, as the same rows alone."""
+    ms = _ms()
+    R, n, tail = 2049 * 128, 16384, 128
+    s = torch.cuda.current_stream()
+    torch.manual_seed(3)
+    x = torch.zeros(R, n, dtype=torch.bfloat16, device="cuda")
+    x[-tail:] = 3 * torch.randn(tail, n, device="cuda")
+    last = x[-tail:].clone()
+    for block_rows in (1, 128):
+        codes, exps = ms.new_matrix_q(R, n, block_rows)
+        c, e = ms.new_matrix_q(tail, n, block_rows)
+        ms.ms_quant_q(x, R, n, block_rows, codes, exps, s)
+        ms.ms_quant_q(last, tail, n, block_rows, c, e, s)
+        assert torch.equal(codes[-tail:], c) and torch.equal(exps[-len(e):], e) and not codes[:-tail].any()
+    y, mags = {}, None
+    for T in (3, 70, 300):  # weights: the last one's codes and exponents
+        a, ae = ms.new_matrix_q(T, n)
+        ms.ms_quant_q(last[:1].expand(T, n).contiguous() if T > tail else last[:T].clone(), T, n, 1, a, ae, s)
+        out = torch.empty(T, R, dtype=torch.float32, device="cuda")
+        ms.ms_dense_q(a, ae, codes, exps, T, n, R, out, stream=s)
+        ref, mags = b8.dense(b8.values(a[:3].cpu().numpy(), ae[:3].cpu().numpy()), b8.values(c.cpu().numpy(), e.cpu().numpy(), 128), None)
+        assert np.all(np.abs(out[:3, -tail:].cpu().numpy() - ref) <= (n / 32 + 8) * 2.0 ** -23 * mags) and not out[:, :-tail].any()
+    del codes, out
+    total, out = torch.empty_like(x), torch.empty_like(x)
+    codes, exps = ms.new_matrix_q(R, n)
+    ms.ms_residual_norm_q(x, None, None, 1e-6, R, n, total, out, codes, exps, s)
+    alone = [torch.empty_like(last), torch.empty_like(last), *ms.new_matrix_q(tail, n)]
+    ms.ms_residual_norm_q(last, None, None, 1e-6, tail, n, *alone, s)
+    for got, want in zip((total, out, codes, exps), alone):
+        assert torch.equal(got[-tail:], want)
+    del x, total, out, codes
+    T, n_in, n_out = 40000, 16, 110000
+    a, ae = ms.new_matrix_q(T, n_in)
+    w, we = ms.new_matrix_q(n_out, n_in, 128)
+    ms.ms_quant_q(torch.randn(T, n_in, device="cuda"), T, n_in, 1, a, ae, s)
+    ms.ms_quant_q(torch.randn(n_out, n_in, device="cuda"), n_out, n_in, 128, w, we, s)
+    y = torch.empty(T, n_out, dtype=torch.bfloat16, device="cuda")
+    ms.ms_dense_q(a, ae, w, we, T, n_in, n_out, y, stream=s)
+    ref, mags = b8.dense(b8.values(a.cpu().numpy(), ae.cpu().numpy())[-300:], b8.values(w.cpu().numpy(), we.cpu().numpy(), 128)[-300:], None)
+    bad = np.abs(y[-300:, -300:].float().cpu().numpy() - ref) > 1.01 * (2.0 ** -9 * mags + 2.0 ** -8 * np.abs(ref)) + 2.0 ** -19 * mags
+    assert not bad.any()
+    del y
+    torch.cuda.empty_cache()
+
+
 def test_a_run_of_them():
     """norm -> product -> norm -> ..., eager and as a captured graph with other inputs, on a side stream: every call
     against the oracle on what the call before left."""

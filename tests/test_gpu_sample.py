@@ -141,6 +141,27 @@ def test_the_longest_flat_rows(T):
         _check(logits, rng.random(T), top_k=np.full(T, k), top_p=np.full(T, p), min_p=np.full(T, m))
 
 
+def test_rows_past_32_bits():
+    ms = _ms()
+    T, n = 8200, 2 ** 19 - 1
+    rng = np.random.default_rng(1)
+    logits = torch.zeros(T, n, device="cuda")
+    last = (2 * rng.standard_normal((3, n))).astype(np.float32)
+    logits[-3:] = torch.from_numpy(last).cuda()
+    u = rng.random(T).astype(np.float32)
+    idx, prob = torch.empty(T, dtype=torch.int32, device="cuda"), torch.empty(T, device="cuda")
+    assert ms.ms_sample_workspace(T, n) == 0
+    ms.ms_sample(logits, T, n, None, _dev(u, np.float32), idx, prob, None, torch.cuda.current_stream())
+    idx, prob = idx.cpu().numpy(), prob.cpu().numpy()
+    assert np.all(np.abs(idx[:-3] - np.floor(u[:-3].astype(np.float64) * n)) <= 1) and np.all(np.abs(prob[:-3] * n - 1) < 1e-6)
+    for t in range(3):
+        want, share, near = osm.draw(last[t], u[T - 3 + t])
+        if near > 1e-9:
+            assert idx[T - 3 + t] == want and abs(prob[T - 3 + t] - share) <= 2.0 ** -23 * share + 2.0 ** -45
+    del logits
+    torch.cuda.empty_cache()
+
+
 def test_extreme_rows():
     inf, nan = np.inf, np.nan
     rows = np.array([[nan, nan, nan, nan, nan], [-inf, -inf, -inf, -inf, -inf], [nan, -inf, 3.0, nan, -inf],
