@@ -78,6 +78,7 @@ class ms_attn_opts(ctypes.Structure):
 
 class ms_sample_opts(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("temperature_dev", "top_k_dev", "top_p_dev", "min_p_dev")]
+    rows = None  # of the tensors
 
 
 MS_CACHE_STATIC, MS_CACHE_LCP, MS_CACHE_LRU, MS_CACHE_LFU, MS_CACHE_RND = range(5)
@@ -559,10 +560,13 @@ def ms_quant_q(x, rows, n, block_rows, codes, exps, stream=None):
 
 def ms_residual_norm_q(h, y, weight, eps, T, d, sum_out=None, out=None, codes=None, exps=None, stream=None):
     dtype, size = (MS_F32, 4) if y is None else _value_type(y, "y")
-    opt = lambda x, name, size, n: None if x is None else _rows(x, name, size, n)  # noqa: E731
-    st = lib.ms_residual_norm_q(_rows(h, "h", 2, T * d), opt(y, "y", size, T * d), dtype, opt(weight, "weight", 2, d), eps, T, d,
-                                opt(sum_out, "sum_out", 2, T * d), opt(out, "out", 2, T * d), opt(codes, "codes", 1, T * d),
-                                opt(exps, "exps", 1, T * _blocks(d)), _stream(stream))
+    n = T * d
+    st = lib.ms_residual_norm_q(_rows(h, "h", 2, n), None if y is None else _rows(y, "y", size, n), dtype,
+                                None if weight is None else _rows(weight, "weight", 2, d), eps, T, d,
+                                None if sum_out is None else _rows(sum_out, "sum_out", 2, n),
+                                None if out is None else _rows(out, "out", 2, n),
+                                None if codes is None else _rows(codes, "codes", 1, n),
+                                None if exps is None else _rows(exps, "exps", 1, T * _blocks(d)), _stream(stream))
     if st:
         _check(st, what="ms_residual_norm_q")
 
@@ -587,7 +591,12 @@ def sample_opts(temperature=None, top_k=None, top_p=None, min_p=None):
     for x, name in zip(ts, ("torch.float32", "torch.int32", "torch.float32", "torch.float32")):
         if x is not None and str(getattr(x, "dtype", name)) != name:
             raise ValueError("sample_opts: %s expected" % name)
+    shapes = {tuple(x.shape) for x in ts if hasattr(x, "shape")}
+    if len(shapes) > 1 or any(len(x) != 1 for x in shapes):
+        raise ValueError("sample_opts: a value per row expected")
     o = ms_sample_opts(*[_ptr(x) for x in ts])
+    for rows, in shapes:
+        o.rows = rows
     o.tensors = ts
     return o
 
@@ -600,10 +609,8 @@ def ms_sample_workspace(T, n):
 
 def ms_sample(logits, T, n, opts, u, idx_out, prob_out=None, workspace=None, stream=None):
     """workspace: a device tensor of at least ms_sample_workspace bytes."""
-    if opts is not None:
-        for x in getattr(opts, "tensors", ()):
-            if x is not None and getattr(x, "shape", None) not in (None, (T,)):
-                raise ValueError("sample_opts: [%d] expected" % T)
+    if opts is not None and opts.rows not in (None, T):
+        raise ValueError("sample_opts: [%d] expected" % T)
     st = lib.ms_sample(_rows(logits, "logits", 4, T * n), T, n, opts, _rows(u, "u", 4, T), _rows(idx_out, "idx_out", 4, T),
                        None if prob_out is None else _rows(prob_out, "prob_out", 4, T), _ptr(workspace),
                        0 if workspace is None else workspace.nbytes, _stream(stream))

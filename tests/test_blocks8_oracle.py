@@ -182,6 +182,9 @@ def test_sample_refusals():
         ms.sample_opts(top_k=u)
     with pytest.raises(ValueError):
         ms.sample_opts(temperature=i)
+    for shapes in ((u, u[:1]), (u.view(1, 2), u.view(1, 2)), (u[0], None)):
+        with pytest.raises(ValueError):
+            ms.sample_opts(temperature=shapes[0], top_p=shapes[1])
     with pytest.raises(ValueError):
         ms.ms_sample(l, 2, 50, ms.sample_opts(temperature=u[:1]), u, i)
     for bad in ((l[:1], u, i), (l, u[:1], i), (l, u, i[:1]), (l.half(), u, i)):
