@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <iterator>
 
 #include "device.h"
 #include "kernels.h"
@@ -331,8 +332,8 @@ __device__ __forceinline__ void store8(const DenseArgs& a, int t, int o, msk::f3
 }
 
 // Few tokens: MO blocks of 16 outputs x NT of 16 tokens (the last one repeated) per
-// work-group, its KW waves every KW-th 128 columns.  Codes go from memory to registers: lane l has pieces l / 16 and 4 + l / 16 of sixteen
-// codes of row l % 16.
+// work-group, its KW waves every KW-th 128 columns.  Codes go from memory to registers: lane l has
+// pieces l / 16 and 4 + l / 16 of sixteen codes of row l % 16.
 template <typename Y, int KW, int MO, int NT>
 __global__ __launch_bounds__(64 * KW) void dense_q_few_kernel(DenseArgs a, int vec) {
   __shared__ __align__(16) float red[KW][MO * NT][64][4];
@@ -400,15 +401,19 @@ __global__ __launch_bounds__(64 * KW) void dense_q_few_kernel(DenseArgs a, int v
 // Some tokens: y^T = W x^T, a work-group takes BM tokens x BN outputs; both operands go to LDS as
 // codes by direct loads (a row's 128 columns of a stage are a cache line; piece p of sixteen
 // codes of row r sits in slot p ^ (r % 8), so the lanes that an LDS read serves together hit
-// distinct banks), in a ring of NST stages.  WM x WN waves split the tile.
+// distinct banks), in a ring of NST stages.  WM x WN waves split the tile, and KS times as many
+// the stages, each part with a ring of its own; the parts' sums are added in LDS in the end.
 //   An fp32 result: codes become bf16, times their scale, as operands are read; every
 // product is exact and sums are fp32.  A bf16 result (EIGHT): the matrix cores take the codes
 // and the scales as they are, at twice the rate; they align the products of eight neighbouring
 // columns to about 2^-13 of the largest before they add them in fp32, which leaves 2e-5 of a
 // result, a hundredth of what its rounding to bf16 takes and too much for an fp32 one.
 //   Bound by the latency of a stage (loads, a barrier, LDS reads, then few matrix instructions
-// of a wave): 100 tokens 4096 -> 4096 15 us with fp32 results, 10.5 with bf16 ones; 512 tokens 4096
-// -> 6144 38 and 25 us.
+// of a wave), so one that has the CU to itself takes its stages several at a time: with 1, 2 and 4
+// parts a round of tiles of 32 x 32 at 4096 columns takes 12.4, 9.6 and 8.8 us with fp32 results and
+// 8.8, 7.3 and 6.8 with bf16 ones, of 64 x 64 18.9, 15.5 and 14.1, and 12.3, 10.7 and 10.6; two
+// rounds of 32 x 32 14.2, 12.6 and 15.8.  64 tokens 4096 -> 4096 8.7 and 6.7 us, 512 tokens 4096 ->
+// 6144 35 and 22.5.
 constexpr int kStageLoad = 64 * 16;      // one load: 8 rows
 constexpr int kRows16 = 16 * kBlock;     // bytes of 16 staged rows
 constexpr int kTileExps = 16384;         // exponents of a tile's tokens that fit: blocks of columns x BM
@@ -440,8 +445,8 @@ __device__ __forceinline__ void stage_exponents(const DenseArgs& a, int t0, Put 
   }
 }
 
-template <typename Y, bool EIGHT, int BM, int BN, int WM, int WN, int NST>
-__global__ __launch_bounds__(64 * WM * WN) void dense_q_tile_kernel(DenseArgs a, int m_tiles, int vec) {
+template <typename Y, bool EIGHT, int BM, int BN, int WM, int WN, int NST, int KS>
+__global__ __launch_bounds__(64 * WM * WN * KS) void dense_q_tile_kernel(DenseArgs a, int m_tiles, int vec) {
   constexpr int NWV = WM * WN;
   constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // 16-wide blocks per wave
   constexpr int NL = (BM + BN) / 8 / NWV;              // loads per wave and stage
@@ -449,11 +454,12 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q_tile_kernel(DenseArgs a,
   constexpr int WB = (BN + kBlock - 1) / kBlock + 1;   // weights' scales that a tile may touch
   constexpr int EXPS = BM * (kMostColumns / kBlock) < kTileExps ? BM * (kMostColumns / kBlock) : kTileExps;
   static_assert(TM * WM * 16 == BM && TN * WN * 16 == BN && NL * 8 * NWV == BM + BN, "tile split");
-  static_assert(NST >= 2 && NST * SBYTES + EXPS + WB * (kMostColumns / kBlock) <= 160 * 1024 && (NST - 2) * NL < 64, "ring");
-  __shared__ __align__(16) unsigned char lds[NST * SBYTES];
+  static_assert(NST >= 2 && KS * NST * SBYTES + EXPS + WB * (kMostColumns / kBlock) <= 160 * 1024 && (NST - 2) * NL < 64, "ring");
+  __shared__ __align__(16) unsigned char lds[KS * NST * SBYTES];
   __shared__ uint8_t xe[EXPS], we[WB * (kMostColumns / kBlock)];  // [blocks of columns][BM], [WB][blocks of columns]
   const int lane = threadIdx.x & 63;
-  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wv = wave % NWV, part = wave / NWV;  // of the waves that take stages part, part + KS, ...
   const int wm = wv % WM, wn = wv / WM;
   const int2 tile = tile_of(blockIdx.x, gridDim.x, m_tiles);
   const int t0 = tile.x * BM, o0 = tile.y * BN;
@@ -465,9 +471,10 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q_tile_kernel(DenseArgs a,
     src[j] = (r < BM ? a.x + static_cast<size_t>(min(t0 + r, a.T - 1)) * a.n_in
                      : a.w + static_cast<size_t>(min(o0 + r - BM, a.n_out - 1)) * a.n_in) + lk;
   }
-  const uint32_t lbase = msk::lds_address(lds) + wv * kStageLoad;
-  auto issue = [&](int sl, int buf) {  // stages past the last reload it (in bounds, never read)
-    const int k0 = min(sl, a.nb - 1) * kBlock;
+  unsigned char* const ring = lds + part * NST * SBYTES;
+  const uint32_t lbase = msk::lds_address(lds) + part * NST * SBYTES + wv * kStageLoad;
+  auto issue = [&](int turn, int buf) {  // stages past the last reload it (in bounds, never read)
+    const int k0 = min(turn * KS + part, a.nb - 1) * kBlock;
     if (k0 + kBlock <= a.n_in) {
 #pragma unroll
       for (int j = 0; j < NL; ++j) msk::lds_load16(src[j] + k0, lbase + buf * SBYTES + NWV * j * kStageLoad);
@@ -480,9 +487,9 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q_tile_kernel(DenseArgs a,
   };
 #pragma unroll
   for (int p = 0; p < NST - 1; ++p) issue(p, p);
-  stage_exponents<BM, 64 * NWV>(a, t0, [&](int r, int b, uint8_t e) { xe[b * BM + r] = e; });
+  stage_exponents<BM, 64 * NWV * KS>(a, t0, [&](int r, int b, uint8_t e) { xe[b * BM + r] = e; });
   const int wb0 = o0 / kBlock, wbn = (a.n_out - 1) / kBlock;
-  for (int i = threadIdx.x; i < WB * a.nb; i += 64 * NWV)
+  for (int i = threadIdx.x; i < WB * a.nb; i += 64 * NWV * KS)
     we[i] = static_cast<uint8_t>(exponent_in_range(a.w_exp[static_cast<size_t>(min(wb0 + i / a.nb, wbn)) * a.nb + i % a.nb]));
   int fo[2];
 #pragma unroll
@@ -497,8 +504,8 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q_tile_kernel(DenseArgs a,
 #pragma unroll
     for (int m = 0; m < TM; ++m) acc[n][m] = msk::f32x4_t{0.f, 0.f, 0.f, 0.f};
   auto compute = [&](int sl, int buf) {
-    const unsigned char* sx = lds + buf * SBYTES + wm * TM * kRows16;
-    const unsigned char* sw = lds + buf * SBYTES + BM * kBlock + wn * TN * kRows16;
+    const unsigned char* sx = ring + buf * SBYTES + wm * TM * kRows16;
+    const unsigned char* sw = ring + buf * SBYTES + BM * kBlock + wn * TN * kRows16;
     if constexpr (EIGHT) {
       auto codes = [&](const unsigned char* p) {
         const uint4 lo = *reinterpret_cast<const uint4*>(p + fo[0]), hi = *reinterpret_cast<const uint4*>(p + fo[1]);
@@ -542,15 +549,34 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q_tile_kernel(DenseArgs a,
   };
   __syncthreads();  // the exponents are there
   int cur = 0, nxt = NST - 1;
-  for (int sl = 0; sl < a.nb; ++sl) {
+  for (int turn = 0; turn * KS < a.nb; ++turn) {
     msk::wait_vm<(NST - 2) * NL>();
     msk::bare_barrier();
-    issue(sl + NST - 1, nxt);
-    compute(sl, cur);
+    issue(turn + NST - 1, nxt);
+    if (KS == 1 || turn * KS + part < a.nb) compute(turn * KS + part, cur);
     cur = cur + 1 == NST ? 0 : cur + 1;
     nxt = nxt + 1 == NST ? 0 : nxt + 1;
   }
-  msk::wait_vm<0>();  // the reloads past the last stage land before the work-group ends
+  msk::wait_vm<0>();  // the reloads past the last stage land before the work-group ends, or its LDS is used again
+  if constexpr (KS > 1) {  // the parts' sums, in their order
+    static_assert((KS - 1) * TN * TM * NWV * 1024 <= KS * NST * SBYTES, "sums");
+    auto* sums = reinterpret_cast<msk::f32x4_t*>(lds) + (wv * 64 + lane);
+    __syncthreads();
+    if (part > 0) {
+#pragma unroll
+      for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int m = 0; m < TM; ++m) sums[(((part - 1) * TN + n) * TM + m) * NWV * 64] = acc[n][m];
+    }
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int p = 1; p < KS; ++p)
+#pragma unroll
+      for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int m = 0; m < TM; ++m) acc[n][m] += sums[(((p - 1) * TN + n) * TM + m) * NWV * 64];
+  }
 #pragma unroll
   for (int m = 0; m < TM; ++m) {
     const int t = t0 + (wm * TM + m) * 16 + (lane & 15);
@@ -816,16 +842,17 @@ __global__ __launch_bounds__(512, 2) void dense_q_pair_kernel(DenseArgs a, int m
 // with two, of which the small tiles' overlap.
 constexpr int kCus = 256;
 struct Tile {
-  int bm, bn, threads;  // tokens, outputs
-  int one[2], two[2];   // cost of a round
+  int bm, bn, parts;   // tokens, outputs; waves that divide the columns
+  int one[2], two[2];  // cost of a round
 };
-constexpr Tile kTiles[] = {{32, 32, 256, {125, 85}, {137, 100}},   {64, 64, 256, {190, 120}, {243, 158}},
-                           {128, 128, 512, {390, 238}, {730, 448}}, {256, 128, 512, {587, 391}, {1128, 752}},
-                           {256, 192, 512, {766, 474}, {1492, 914}}, {256, 256, 512, {0, 562}, {0, 1081}}};
+constexpr Tile kTiles[] = {{32, 32, 4, {88, 68}, {157, 120}},    {32, 32, 2, {96, 73}, {126, 94}},
+                           {64, 64, 4, {141, 106}, {262, 221}},  {64, 64, 2, {155, 107}, {231, 161}},
+                           {128, 128, 2, {364, 230}, {691, 439}}, {256, 128, 1, {587, 391}, {1128, 752}},
+                           {256, 192, 1, {766, 474}, {1492, 914}}, {256, 256, 1, {0, 562}, {0, 1081}}};
 // Whole rounds of one of the two largest tiles, and the outputs that are left in the third: 4096
 // tokens 4096 -> 14336 bf16 205 us with the largest alone and 197 with both, 8192 cubed fp32 850 and
 // 806, 2048 tokens 4096 -> 14336 fp32 212 and 197.
-constexpr int kRest = 3, kFirstMixed = 4;
+constexpr int kNTiles = std::size(kTiles), kRest = kNTiles - 3, kFirstMixed = kNTiles - 2;
 static_assert(kTiles[kRest].bm == kTiles[kFirstMixed].bm, "the same tokens");
 
 template <typename Y, bool EIGHT>
@@ -838,11 +865,11 @@ ms_status launch_tiles(const DenseArgs& a, int vec, hipStream_t s) {
     return n / (2 * kCus) * t.two[EIGHT] + (rest == 0 ? 0 : rest <= kCus ? t.one[EIGHT] : t.two[EIGHT]);
   };
   auto fits = [&](const Tile& t, int64_t n) {  // a launch, and the exponents' LDS
-    return n * t.threads <= UINT32_MAX && a.nb * t.bm <= kTileExps;
+    return n <= UINT32_MAX / 1024 && a.nb * t.bm <= kTileExps;
   };
   int best = -1, o_split = a.n_out;
   int64_t best_cost = INT64_MAX;
-  for (int i = 0; i < (EIGHT ? 6 : 5); ++i) {
+  for (int i = 0; i < kNTiles - !EIGHT; ++i) {
     const Tile& t = kTiles[i];
     const int64_t n = count(t, a.n_out);
     if (!fits(t, n)) continue;
@@ -857,29 +884,32 @@ ms_status launch_tiles(const DenseArgs& a, int vec, hipStream_t s) {
   if (best < 0) return MS_E_UNSUPPORTED;
   const int m_tiles = (a.T - 1) / kTiles[best].bm + 1;
   const int rest = static_cast<int>(count(kTiles[kRest], a.n_out - o_split));
-  const dim3 grid(static_cast<unsigned>(count(kTiles[best], o_split) + rest)), block(kTiles[best].threads);
-#define MSK_TILE_CASE(I_, BM_, BN_, WM_, WN_, NST_)                                                                  \
-  case I_:                                                                                                           \
-    static_assert(kTiles[I_].bm == BM_ && kTiles[I_].bn == BN_ && kTiles[I_].threads == 64 * WM_ * WN_, "tiles");        \
-    hipLaunchKernelGGL((dense_q_tile_kernel<Y, EIGHT, BM_, BN_, WM_, WN_, NST_>), grid, block, 0, s, a, m_tiles, vec); \
+  const dim3 grid(static_cast<unsigned>(count(kTiles[best], o_split) + rest));
+#define MSK_TILE_CASE(I_, BM_, BN_, WM_, WN_, NST_, KS_)                                                                  \
+  case I_:                                                                                                                \
+    static_assert(kTiles[I_].bm == BM_ && kTiles[I_].bn == BN_ && kTiles[I_].parts == KS_, "tiles");                      \
+    hipLaunchKernelGGL((dense_q_tile_kernel<Y, EIGHT, BM_, BN_, WM_, WN_, NST_, KS_>), grid, dim3(64 * WM_ * WN_ * KS_), 0, s, \
+                       a, m_tiles, vec);                                                                                  \
     break;
-#define MSK_PAIR_CASE(I_, BN_)                                                                               \
-  case I_:                                                                                                   \
-    static_assert(kTiles[I_].bm == 256 && kTiles[I_].bn == BN_ && kTiles[I_].threads == 512, "tiles");           \
-    if constexpr (EIGHT || BN_ < 256) {                                                                      \
-      if (o_split == a.n_out)                                                                            \
-        hipLaunchKernelGGL((dense_q_pair_kernel<Y, EIGHT, BN_, BN_>), grid, block, 0, s, a, m_tiles, vec, o_split, 0); \
-      else                                                                                               \
-        hipLaunchKernelGGL((dense_q_pair_kernel<Y, EIGHT, BN_, 128>), grid, block, 0, s, a, m_tiles, vec, o_split, rest); \
-    }                                                                                                    \
+#define MSK_PAIR_CASE(I_, BN_)                                                                                                     \
+  case I_:                                                                                                                         \
+    static_assert(kTiles[I_].bm == 256 && kTiles[I_].bn == BN_, "tiles");                                                          \
+    if constexpr (EIGHT || BN_ < 256) {                                                                                            \
+      if (o_split == a.n_out)                                                                                                      \
+        hipLaunchKernelGGL((dense_q_pair_kernel<Y, EIGHT, BN_, BN_>), grid, dim3(512), 0, s, a, m_tiles, vec, o_split, 0);    \
+      else                                                                                                                         \
+        hipLaunchKernelGGL((dense_q_pair_kernel<Y, EIGHT, BN_, 128>), grid, dim3(512), 0, s, a, m_tiles, vec, o_split, rest); \
+    }                                                                                                                              \
     break;
   switch (best) {
-    MSK_TILE_CASE(0, 32, 32, 2, 2, 4)
-    MSK_TILE_CASE(1, 64, 64, 2, 2, 3)
-    MSK_TILE_CASE(2, 128, 128, 2, 4, 4)
-    MSK_PAIR_CASE(3, 128)
-    MSK_PAIR_CASE(4, 192)
-    MSK_PAIR_CASE(5, 256)
+    MSK_TILE_CASE(0, 32, 32, 2, 2, 3, 4)
+    MSK_TILE_CASE(1, 32, 32, 2, 2, 3, 2)
+    MSK_TILE_CASE(2, 64, 64, 2, 2, 2, 4)
+    MSK_TILE_CASE(3, 64, 64, 2, 2, 2, 2)
+    MSK_TILE_CASE(4, 128, 128, 2, 4, 2, 2)
+    MSK_PAIR_CASE(5, 128)
+    MSK_PAIR_CASE(6, 192)
+    MSK_PAIR_CASE(7, 256)
   }
 #undef MSK_TILE_CASE
 #undef MSK_PAIR_CASE
@@ -891,8 +921,7 @@ ms_status launch_tiles(const DenseArgs& a, int vec, hipStream_t s) {
 // 7.9 | 12.3, 4096 -> 14336 15.1 | 14.3 | 13.3 | 14.5, 4096 -> 32000 30.3 | 26.6 | 24.5 | 29.7, 1024 ->
 // 32000 7.6 | 7.6 | 9.6 | 8.2; 16 tokens 4096 -> 6144 12.4 | 9.2 | 9.5 | 13.2, -> 32000 40.0 | 32.0 | 31.0 |
 // 31.4.  Long rows of one token want one block and sixteen waves, 8192 -> 8192 14.2 for 18.1
-// with 2 x 16, and of 16 tokens not, 21.1 for 18.1.  32 tokens 4096 -> 32000 46.4 with 2 x 8, 34.5
-// with 4 x 8; 64 tokens 2048 -> 32000 30.5 and 25.9 (4 x 4).
+// with 2 x 16, and of 16 tokens not, 21.1 for 18.1.
 template <typename Y, int NT>
 void launch_few(const DenseArgs& a, int vec, hipStream_t s) {
   const unsigned blocks = (a.n_out - 1) / 16 + 1;
@@ -908,30 +937,36 @@ void launch_few(const DenseArgs& a, int vec, hipStream_t s) {
       MSK_FEW(16, 2);
     else
       MSK_FEW(8, 2);
-  } else if (blocks <= 2 * kCus) {
-    MSK_FEW(8, 2);
   } else {
-    MSK_FEW(NT == 2 ? 8 : 4, 4);
+    MSK_FEW(8, 2);
   }
 #undef MSK_FEW
 }
 
-// Which calls dense_q_few_kernel takes: up to 16 tokens all, up to 64 those of short rows, and
-// up to 32 with fp32 results, us of it | tiles, fp32 and bf16 results: 16 tokens 4096 -> 4096 6.8 |
-// 11.8, 6.8 | 8.4; 32 tokens 4096 -> 6144 11.2 | 12.0, 11.2 | 8.5, 2048 -> 2048 5.1 | 7.8, 5.1 | 6.2;
-// 61 tokens 2000 -> 5003 6.8 | 9.2, 6.6 | 7.2; 64 tokens 4096 -> 4096 15.2 | 12.5, 15.9 | 8.7.
-bool takes_few(int T, int n_in, bool eight) { return T <= 16 || (T <= 64 && n_in <= 2048) || (T <= 32 && !eight); }
+// Which calls dense_q_few_kernel takes: up to 16 tokens all; up to 32 those of short rows, and of
+// longer ones that do not start every 512 bytes on few memory channels (its waves read a row
+// in pieces, tiles whole rows); with fp32 results up to 64 those of rows shorter still.  us of
+// it | tiles, weights not in the caches: 16 tokens 4096 -> 6144 fp32 8.9 | 8.9, 4096 -> 4096 7.2 |
+// 8.7; 32 tokens 2048 -> 4096 fp32 5.9 | 6.7, bf16 5.9 | 6.1, 2048 -> 32000 18.0 | 16.5, 3008 -> 4096 fp32
+// 7.0 | 8.6, 4096 -> 4096 10.5 | 9.3; 64 tokens 1520 -> 6144 fp32 8.3 | 8.9, bf16 8.3 | 8.4, 2048 ->
+// 6144 fp32 9.8 | 9.0, 4096 -> 4096 (cached) 14.7 | 8.9.
+bool takes_few(const DenseArgs& a, bool eight) {
+  if (a.T <= 16) return true;
+  if (a.n_out > 32 * kCus) return false;
+  if (a.T <= 32) return a.n_in <= 2048 || (a.n_in <= 4096 && a.n_in % 512 != 0 && a.n_out <= 16 * kCus);
+  return a.T <= 64 && !eight && a.n_in < 2048;
+}
 
 template <typename Y, bool EIGHT>
 ms_status launch_dense_q(const DenseArgs& a, hipStream_t s) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.add);
   const int vec = a.n_out % 4 == 0 && (at & (4 * sizeof(Y) - 1)) == 0;
-  if (!takes_few(a.T, a.n_in, EIGHT)) return launch_tiles<Y, EIGHT>(a, vec, s);
+  if (!takes_few(a, EIGHT)) return launch_tiles<Y, EIGHT>(a, vec, s);
   if (a.T <= 16)
     launch_few<Y, 1>(a, vec, s);
   else if (a.T <= 32)
     launch_few<Y, 2>(a, vec, s);
-  else
+  else if constexpr (!EIGHT)
     launch_few<Y, 4>(a, vec, s);
   return hipGetLastError() == hipSuccess ? MS_OK : MS_E_HIP;
 }

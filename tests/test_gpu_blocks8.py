@@ -218,7 +218,7 @@ def _dense(T, n_in, n_out, dtype, add=None, shift=0, seed=0, spread=4):
 
 # few tokens: every number of blocks of 16 outputs and of waves (outputs up to 4096, 8192 and more, by rows of up to
 # 2048 and 4096 columns and longer ones), 1, 2 and 4 blocks of tokens; then tiles of 32 x 32 to 256 x 256 with
-# remainders, and two sizes of them in a launch; widths that end inside a block of 128; the longest row
+# remainders, of fewer stages than parts of waves, and two sizes of them in a launch; widths that end inside a block of 128; the longest row
 @pytest.mark.parametrize("T,n_in,n_out", [(1, 16, 1), (1, 4096, 6144), (1, 16384, 33), (2, 144, 100), (15, 2000, 129),
                                           (1, 4112, 4099), (16, 4112, 4099), (3, 2064, 8200), (16, 80, 8211),
                                           (16, 1024, 300), (17, 512, 70), (32, 144, 4101), (20, 272, 8210), (33, 448, 30),
@@ -226,7 +226,8 @@ def _dense(T, n_in, n_out, dtype, add=None, shift=0, seed=0, spread=4):
                                           (65, 80, 2500), (130, 8192, 200), (129, 1104, 257), (250, 128, 6144),
                                           (511, 272, 6100), (1000, 256, 4099), (2047, 144, 6140), (300, 16384, 150),
                                           (1500, 80, 6200), (2000, 144, 8190), (1030, 272, 16400), (1300, 400, 11001),
-                                          (1300, 80, 11500), (1800, 144, 18504)])
+                                          (1300, 80, 11500), (1800, 144, 18504), (60, 2000, 8200), (500, 1200, 6100),
+                                          (1030, 1104, 1030), (33, 16384, 40)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_dense(T, n_in, n_out, dtype):
     _dense(T, n_in, n_out, dtype)
