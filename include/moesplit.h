@@ -650,10 +650,16 @@ ms_status ms_residual_norm_q(const void* h, const void* y, int32_t y_dtype, cons
 /* y[t][o] = sum_i x[t][i] w[o][i] (+ add[t][o] if add is not NULL): x [T][n_in] in
  * 8 bits with R = 1, w [n_out][n_in] with R = 128, y and add [T][n_out] y_dtype
  * (add may be y; other overlaps with y are MS_E_INVALID).  Sums in fp32.  An fp32
- * y is as exact as fp32 products and sums are; a bf16 y may be off, before its
- * rounding, by 2^-12 of the largest of every eight neighbouring products
- * (relative to a result about 2e-5): it is computed on the 8-bit matrix cores
- * where there are many tokens.  A code of NaN makes the results of its row NaN. */
+ * y is as exact as fp32 products and sums are, and so is a bf16 y of up to 16 tokens
+ * before its one rounding.  Of more tokens a bf16 y may be computed on the 8-bit
+ * matrix cores: of every eight neighbouring columns the products are first cut to
+ * multiples of 2^(E - 13), E the largest sum of the exponents of two codes (at least
+ * -6 each) and their scales whose product is not zero.  Without subnormal codes that
+ * takes less than 2^-13 of the largest product from each of the others, 2^-10 from
+ * all, and with them (of one factor) up to eight times that: some 2e-5 of a result of
+ * products of both signs and like sizes, more of one that cancels or of a sum of many
+ * small products beside a large one.  So a token's bf16 results may depend on how many
+ * others there are.  A code of NaN makes the results of its row NaN. */
 ms_status ms_dense_q(const void* x, const void* x_exp, const void* w, const void* w_exp, int32_t T, int32_t n_in,
                      int32_t n_out, void* y, int32_t y_dtype, const void* add, void* stream);
 
