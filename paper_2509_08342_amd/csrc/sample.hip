@@ -750,8 +750,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   }
   const Scale sc = st.scale(sh, r.x, r.y);
   int last = kBins - 1;  // the last bin that matters
-  if (st.by_min && !st.by_p)  // (a bin further, for its fp32 distances)
-    last = static_cast<int>(fminf(-logf(fminf(st.min_p, 1.0f)) * st.temp * 0.500005f * sc.bins, kBins - 2)) + 1;
+  if (st.by_min && !st.by_p) {  // of the least weight that rounds up to min_p's units (a bin further, for its fp32 distances)
+    const double w = (static_cast<double>(st.least) - 0.5) / kUnit;
+    const float far = fmaxf(-logf(static_cast<float>(w)), static_cast<float>(1.0 - w));  // (next to 1 the logarithm gives 0)
+    last = static_cast<int>(fminf(far * st.temp * 0.500005f * sc.bins, kBins - 2)) + 1;
+  }
   if (st.by_k) {
     l.every([&](float x, int) { count_token(sh, sc.bin(x)); });
     __syncthreads();

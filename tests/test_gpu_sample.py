@@ -271,3 +271,38 @@ def test_captured_and_replayed(T, n):
             idx, prob = _run(x, u, **v)
             assert np.array_equal(s["idx"].cpu().numpy(), idx) and np.array_equal(s["prob"].cpu().numpy(), prob)
         _check(*new[0][:2], **new[0][2])
+
+
+@pytest.mark.parametrize("min_p,temperature", [(2.0 ** -44, 1.0), (2.0 ** -45, 0.7), (1e-14, 1.0), (2.5e-13, 2.0), (1.0, 3e38)])
+def test_a_small_min_p_does_not_depend_on_the_batch(min_p, temperature):
+    """Weights that only rounding to whole units of 2^-45 brings up to min_p's are kept, by one work-group a row and by
+    several: 20000 tokens of 0.4 units less than it asks for, whose mass moves the drawn token by many of the 900 above them."""
+    n, T = 60013, 400
+    least = int(np.ceil(np.float32(min_p).astype(np.float64) * 2.0 ** 45))
+    rng = np.random.default_rng(least)
+    units = np.zeros(n)  # in 2^-45 of the largest
+    if min_p < 1:
+        units[1:901] = 2500 + 3 * np.arange(900)
+        units[901:20901] = least - 0.4
+    else:  # all of them round to the largest
+        units[1:20901] = 2.0 ** 45 - np.linspace(0, 0.4, 20900)
+    units[0] = 2.0 ** 45
+    row = np.full(n, -200.0 * temperature if min_p < 1 else -np.inf, np.float64)
+    row[:20901] = temperature * np.log(units[:20901] / 2.0 ** 45) if min_p < 1 else -np.linspace(0, 20900, 20901)
+    row = rng.permutation(row).astype(np.float32)
+    T32 = np.float32(temperature).astype(np.float64)
+    w = [int(v) for v in np.rint(2.0 ** 45 * np.exp((row.astype(np.float64) - row.max()) / T32))]
+    order = np.lexsort((np.arange(n), -row))
+    u = np.float32(1 - 2.0 ** -24)
+    kept = [i for i in order if w[i] >= least]
+    assert len(kept) == 20901
+    M, c = sum(w[i] for i in kept), 0
+    for i in kept:
+        c += w[i]
+        if c * 2 ** 24 > M * (2 ** 24 - 1):
+            break
+    for rows in (1, T):
+        s = dict(temperature=np.full(rows, temperature), min_p=np.full(rows, min_p))
+        idx, prob = _run(np.tile(row, (rows, 1)), np.full(rows, u), **s)
+        assert (idx == i).all(), (rows, idx[:4], i)
+        assert np.all(np.abs(prob - w[i] / M) <= 2.0 ** -23 * w[i] / M)
