@@ -692,7 +692,8 @@ ms_status ms_sample_workspace(int32_t T, int32_t n, uint64_t* bytes_out);
  * without a logit above -infinity gives 0.  Weights are whole numbers of 2^-45 of
  * the largest, smaller ones zero: the same inputs give the same token whatever else
  * runs, and whatever T.  opts NULL: temperature 1.
- * Outputs overlap nothing (MS_E_INVALID).  workspace_dev: 16-byte aligned, used until
+ * Outputs and, where it is used, the workspace overlap nothing (MS_E_INVALID).
+ * workspace_dev: 16-byte aligned, used until
  * the call has finished on `stream`; calls that may overlap in time need one each. */
 ms_status ms_sample(const float* logits, int32_t T, int32_t n, const ms_sample_opts* opts, const float* u_dev,
                     int32_t* idx_out, float* prob_out, void* workspace_dev, uint64_t workspace_bytes, void* stream);

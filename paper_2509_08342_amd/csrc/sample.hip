@@ -992,12 +992,16 @@ ms_status ms_sample(const float* logits, int32_t T, int32_t n, const ms_sample_o
     return MS_E_INVALID;
   const size_t values = 4 * static_cast<size_t>(T);
   const ms_sample_opts given = opts ? *opts : ms_sample_opts{};
-  auto apart = [&](const void* o) {
+  auto apart = [&](const void* o, size_t bytes) {  // from all inputs
     const void* const rows[] = {u_dev, given.temperature_dev, given.top_k_dev, given.top_p_dev, given.min_p_dev};
-    return std::none_of(std::begin(rows), std::end(rows), [&](const void* q) { return overlap(o, values, q, values); }) &&
-           !overlap(o, values, logits, values * n) && !overlap(o, values, workspace_dev, need);
+    return std::none_of(std::begin(rows), std::end(rows), [&](const void* q) { return overlap(o, bytes, q, values); }) &&
+           !overlap(o, bytes, logits, values * n);
   };
-  if (!apart(idx_out) || !apart(prob_out) || overlap(idx_out, values, prob_out, values)) return MS_E_INVALID;
+  if (!apart(idx_out, values) || !apart(prob_out, values) || overlap(idx_out, values, prob_out, values)) return MS_E_INVALID;
+  // (the workspace is written before inputs are read for the last time)
+  if (need > 0 && (!apart(workspace_dev, need) || overlap(workspace_dev, need, idx_out, values) ||
+                   overlap(workspace_dev, need, prob_out, values)))
+    return MS_E_INVALID;
   if (T > UINT32_MAX / kThreads) return MS_E_UNSUPPORTED;
   const int splits = splits_of(T, n);
   const SampleArgs a = {logits, u_dev, given.temperature_dev, given.top_p_dev, given.min_p_dev, given.top_k_dev, idx_out, prob_out,

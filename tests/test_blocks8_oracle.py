@@ -190,3 +190,24 @@ def test_sample_refusals():
     for bad in ((l[:1], u, i), (l, u[:1], i), (l, u, i[:1]), (l.half(), u, i)):
         with pytest.raises(ValueError):
             ms.ms_sample(bad[0], 2, 50, None, *bad[1:])
+
+
+def test_sample_workspace_over_inputs():
+    """A workspace is written before the last look at logits, numbers and settings: it overlaps none of them."""
+    ms = _ms()
+    T, n = 1, 200000
+    need = ms.ms_sample_workspace(T, n)
+    assert need > 0
+    room = torch.zeros(4 * n + need + 64, dtype=torch.uint8)
+    u, i, idx = torch.zeros(T), torch.zeros(T, dtype=torch.int32), torch.zeros(T, dtype=torch.int32)
+    logits = torch.zeros(T, n)
+    over = [room[:need], room[4 * n - 16:4 * n - 16 + need]]  # the first logits, and the last four
+    for ws in over:
+        assert _status(ms.ms_sample, room[:4 * n].view(torch.float32), T, n, None, u, idx, None, ws) == ms.MS_E_INVALID
+    ws = room[:need]
+    at = lambda t: room[need - 4:need].view(t)  # noqa: E731  (in the workspace's last bytes)
+    assert _status(ms.ms_sample, logits, T, n, None, at(torch.float32), idx, None, ws) == ms.MS_E_INVALID
+    for name, t in (("temperature", torch.float32), ("top_k", torch.int32), ("top_p", torch.float32), ("min_p", torch.float32)):
+        assert _status(ms.ms_sample, logits, T, n, ms.sample_opts(**{name: at(t)}), u, idx, None, ws) == ms.MS_E_INVALID
+    # unused, it may lie anywhere
+    ms.ms_sample(torch.zeros(0, 50), 0, 50, None, u[:0], i[:0], None, room[:16])
