@@ -474,27 +474,45 @@ def _span(x, cache):
     return _ptr(x)
 
 
-def _rows(x, name, size, values):
-    """x's address; a tensor is contiguous and holds at least `values` numbers of `size` bytes, in whatever shape."""
+class _Values(dict):
+    """Bytes of a value by the type of the tensor that holds it; without end for types that hold other values (a type's
+    name is looked at once)."""
+
+    def __init__(self, size, *names):
+        super().__init__()
+        self.size, self.names = size, names
+
+    def __missing__(self, dtype):
+        self[dtype] = size = self.size if str(dtype) in self.names else float("inf")
+        return size
+
+
+_F32, _BF16, _I32 = _Values(4, "torch.float32"), _Values(2, "torch.bfloat16"), _Values(4, "torch.int32")
+_CODES = _Values(1, "torch.uint8", "torch.int8", "torch.float8_e4m3fn")
+_EXPONENTS = _Values(1, "torch.uint8", "torch.float8_e8m0fnu")
+
+
+def _rows(x, name, kind, values):
+    """x's address; a tensor is contiguous and holds at least `values` of a kind (_Values), in whatever shape."""
     try:
-        if x.nbytes >= values * size and x.itemsize == size and x.is_contiguous():
+        if x.is_contiguous() and x.nbytes >= values * kind[x.dtype]:  # (none of a size without end: NaN)
             return x.data_ptr()
     except AttributeError:  # an address
         return _ptr(x)
-    raise ValueError("%s: %d contiguous values of %d bytes expected" % (name, values, size))
+    raise ValueError("%s: %d contiguous values of %s expected" % (name, values, " or ".join(kind.names)))
 
 
 def ms_rope_kv_q(cache, rope, qkv, T, Hq, pos0, q_out, span=None, stream=None):
     n, kv = (cache.n_seqs * T * cache.head_dim, 2 * cache.n_kv_heads) if cache is not None else (0, 0)
-    st = lib.ms_rope_kv_q(cache, rope, _rows(qkv, "qkv", 4, n * (Hq + kv)), T, Hq, pos0,
-                          None if span is None else _span(span, cache), _rows(q_out, "q_out", 2, n * Hq), _stream(stream))
+    st = lib.ms_rope_kv_q(cache, rope, _rows(qkv, "qkv", _F32, n * (Hq + kv)), T, Hq, pos0,
+                          None if span is None else _span(span, cache), _rows(q_out, "q_out", _BF16, n * Hq), _stream(stream))
     if st:
         _check(st, what="ms_rope_kv_q")
 
 
 def ms_kv_read_q(cache, pos0, n, k_out, v_out, stream=None):
     values = cache.n_seqs * n * cache.head_dim * cache.n_kv_heads if cache is not None else 0
-    st = lib.ms_kv_read_q(cache, pos0, n, _rows(k_out, "k_out", 2, values), _rows(v_out, "v_out", 2, values), _stream(stream))
+    st = lib.ms_kv_read_q(cache, pos0, n, _rows(k_out, "k_out", _BF16, values), _rows(v_out, "v_out", _BF16, values), _stream(stream))
     if st:
         _check(st, what="ms_kv_read_q")
 
@@ -514,8 +532,8 @@ def ms_attention_q(cache, q, T, Hq, pos0, out, workspace=None, opts=None, span=N
             raise ValueError("attn_opts: slopes of %r expected" % ((Hq,),))
         if doc is not None and getattr(doc, "shape", None) not in (None, (cache.n_seqs, cache.max_ctx)):
             raise ValueError("attn_opts: doc of %r expected" % ((cache.n_seqs, cache.max_ctx),))
-    st = lib.ms_attention_q(cache, _rows(q, "q", 2, n), T, Hq, pos0, None if span is None else _span(span, cache), opts,
-                            _rows(out, "out", 2, n), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
+    st = lib.ms_attention_q(cache, _rows(q, "q", _BF16, n), T, Hq, pos0, None if span is None else _span(span, cache), opts,
+                            _rows(out, "out", _BF16, n), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
                             _stream(stream))
     if st:
         _check(st, what="ms_attention_q")
@@ -525,11 +543,11 @@ def ms_attention_q(cache, q, T, Hq, pos0, out, workspace=None, opts=None, span=N
 
 BLOCK_Q = 128  # columns that share a scale, and rows of a weight's block
 
-_VALUE_TYPES = {"torch.float32": (MS_F32, 4), "torch.bfloat16": (MS_BF16, 2)}
+_VALUE_TYPES = {"torch.float32": (MS_F32, _F32), "torch.bfloat16": (MS_BF16, _BF16)}
 
 
 def _value_type(x, name):
-    """(MS_F32 or MS_BF16, its size) of a tensor."""
+    """(MS_F32 or MS_BF16, its kind) of a tensor."""
     try:
         t = _VALUE_TYPES.get(x.dtype)
         if t is None:  # the first of its type
@@ -551,34 +569,34 @@ def _blocks(n):
 
 
 def ms_quant_q(x, rows, n, block_rows, codes, exps, stream=None):
-    dtype, size = _value_type(x, "x")
-    st = lib.ms_quant_q(_rows(x, "x", size, rows * n), dtype, rows, n, block_rows, _rows(codes, "codes", 1, rows * n),
-                        _rows(exps, "exps", 1, -(-rows // max(block_rows, 1)) * _blocks(n)), _stream(stream))
+    dtype, kind = _value_type(x, "x")
+    st = lib.ms_quant_q(_rows(x, "x", kind, rows * n), dtype, rows, n, block_rows, _rows(codes, "codes", _CODES, rows * n),
+                        _rows(exps, "exps", _EXPONENTS, -(-rows // max(block_rows, 1)) * _blocks(n)), _stream(stream))
     if st:
         _check(st, what="ms_quant_q")
 
 
 def ms_residual_norm_q(h, y, weight, eps, T, d, sum_out=None, out=None, codes=None, exps=None, stream=None):
-    dtype, size = (MS_F32, 4) if y is None else _value_type(y, "y")
+    dtype, kind = (MS_F32, _F32) if y is None else _value_type(y, "y")
     n = T * d
-    st = lib.ms_residual_norm_q(_rows(h, "h", 2, n), None if y is None else _rows(y, "y", size, n), dtype,
-                                None if weight is None else _rows(weight, "weight", 2, d), eps, T, d,
-                                None if sum_out is None else _rows(sum_out, "sum_out", 2, n),
-                                None if out is None else _rows(out, "out", 2, n),
-                                None if codes is None else _rows(codes, "codes", 1, n),
-                                None if exps is None else _rows(exps, "exps", 1, T * _blocks(d)), _stream(stream))
+    st = lib.ms_residual_norm_q(_rows(h, "h", _BF16, n), None if y is None else _rows(y, "y", kind, n), dtype,
+                                None if weight is None else _rows(weight, "weight", _BF16, d), eps, T, d,
+                                None if sum_out is None else _rows(sum_out, "sum_out", _BF16, n),
+                                None if out is None else _rows(out, "out", _BF16, n),
+                                None if codes is None else _rows(codes, "codes", _CODES, n),
+                                None if exps is None else _rows(exps, "exps", _EXPONENTS, T * _blocks(d)), _stream(stream))
     if st:
         _check(st, what="ms_residual_norm_q")
 
 
 def ms_dense_q(x, x_exp, w, w_exp, T, n_in, n_out, y, add=None, stream=None):
     """y (and add): float32 or bfloat16."""
-    dtype, size = _value_type(y, "y")
+    dtype, kind = _value_type(y, "y")
     if add is not None and add.dtype != y.dtype:
         raise ValueError("add: the type of y expected")
-    st = lib.ms_dense_q(_rows(x, "x", 1, T * n_in), _rows(x_exp, "x_exp", 1, T * _blocks(n_in)), _rows(w, "w", 1, n_out * n_in),
-                        _rows(w_exp, "w_exp", 1, _blocks(n_out) * _blocks(n_in)), T, n_in, n_out, _rows(y, "y", size, T * n_out),
-                        dtype, None if add is None else _rows(add, "add", size, T * n_out), _stream(stream))
+    st = lib.ms_dense_q(_rows(x, "x", _CODES, T * n_in), _rows(x_exp, "x_exp", _EXPONENTS, T * _blocks(n_in)), _rows(w, "w", _CODES, n_out * n_in),
+                        _rows(w_exp, "w_exp", _EXPONENTS, _blocks(n_out) * _blocks(n_in)), T, n_in, n_out, _rows(y, "y", kind, T * n_out),
+                        dtype, None if add is None else _rows(add, "add", kind, T * n_out), _stream(stream))
     if st:
         _check(st, what="ms_dense_q")
 
@@ -611,8 +629,8 @@ def ms_sample(logits, T, n, opts, u, idx_out, prob_out=None, workspace=None, str
     """workspace: a device tensor of at least ms_sample_workspace bytes."""
     if opts is not None and opts.rows not in (None, T):
         raise ValueError("sample_opts: [%d] expected" % T)
-    st = lib.ms_sample(_rows(logits, "logits", 4, T * n), T, n, opts, _rows(u, "u", 4, T), _rows(idx_out, "idx_out", 4, T),
-                       None if prob_out is None else _rows(prob_out, "prob_out", 4, T), _ptr(workspace),
+    st = lib.ms_sample(_rows(logits, "logits", _F32, T * n), T, n, opts, _rows(u, "u", _F32, T), _rows(idx_out, "idx_out", _I32, T),
+                       None if prob_out is None else _rows(prob_out, "prob_out", _F32, T), _ptr(workspace),
                        0 if workspace is None else workspace.nbytes, _stream(stream))
     if st:
         _check(st, what="ms_sample")

@@ -211,3 +211,56 @@ def test_sample_workspace_over_inputs():
         assert _status(ms.ms_sample, logits, T, n, ms.sample_opts(**{name: at(t)}), u, idx, None, ws) == ms.MS_E_INVALID
     # unused, it may lie anywhere
     ms.ms_sample(torch.zeros(0, 50), 0, 50, None, u[:0], i[:0], None, room[:16])
+
+
+def test_tensors_of_another_type_are_refused():
+    """Every tensor of the calls as a type of the same size that holds other values."""
+    ms = _ms()
+    T, d = 3, 256
+    z = lambda *shape, dtype: torch.zeros(*shape, dtype=dtype)  # noqa: E731
+    bf, f32, u8 = torch.bfloat16, torch.float32, torch.uint8
+    ok = dict(h=z(T, d, dtype=bf), y=z(T, d, dtype=bf), weight=z(d, dtype=bf), sum_out=z(T, d, dtype=bf), out=z(T, d, dtype=bf),
+              codes=z(T, d, dtype=u8), exps=z(T, 2, dtype=u8))
+
+    def norm(**a):
+        a = {**ok, **a}
+        ms.ms_residual_norm_q(a.pop("h"), a.pop("y"), a.pop("weight"), 1e-6, T, d, **a)
+    for name in ("h", "y", "weight", "sum_out", "out"):
+        for other in (torch.float16, torch.int16):
+            with pytest.raises(ValueError):
+                norm(**{name: ok[name].view(other)})
+    for name, others in (("codes", (torch.bool, torch.float8_e5m2, torch.float8_e4m3fnuz)), ("exps", (torch.int8, torch.bool, torch.float8_e4m3fn))):
+        for other in others:
+            with pytest.raises(ValueError):
+                norm(**{name: ok[name].view(other)})
+            with pytest.raises(ValueError):
+                ms.ms_quant_q(ok["h"], T, d, 1, **{**{k: ok[k] for k in ("codes", "exps")}, name: ok[name].view(other)})
+    x, xe, y = ok["codes"], ok["exps"], z(T, T, dtype=f32)
+    w, we = z(T, d, dtype=u8), z(1, 2, dtype=u8)
+    for bad in ((x.view(torch.float8_e5m2), xe, w, we), (x, xe.view(torch.int8), w, we), (x, xe, w.view(torch.bool), we),
+                (x, xe, w, we.view(torch.float8_e5m2))):
+        with pytest.raises(ValueError):
+            ms.ms_dense_q(*bad, T, d, T, y)
+    n = 50
+    ok = dict(logits=z(T, n, dtype=f32), u=z(T, dtype=f32), idx=z(T, dtype=torch.int32), prob=z(T, dtype=f32))
+    for name, other in (("logits", torch.int32), ("u", torch.int32), ("idx", f32), ("idx", torch.uint32), ("prob", torch.int32)):
+        a = {**ok, name: ok[name].view(other)}
+        with pytest.raises(ValueError):
+            ms.ms_sample(a["logits"], T, n, None, a["u"], a["idx"], a["prob"])
+    # nothing to do, of every type that there is
+    for c, e in ((u8, u8), (torch.int8, u8), (torch.float8_e4m3fn, torch.float8_e8m0fnu)):
+        ms.ms_quant_q(z(0, d, dtype=bf), 0, d, 1, z(0, d, dtype=c), z(0, 2, dtype=e))
+
+
+def test_cache_tensors_of_another_type_are_refused():
+    ms = _ms()
+    T, Hq, Hkv, D = 3, 4, 2, 64
+    c = ms.new_kv_cache_q(1, Hkv, D, 64, device="cpu")
+    rope = ms.rope_desc(D, 1e4)
+    half, qkv = torch.zeros(T * Hq * D, dtype=torch.float16), torch.zeros(T * (Hq + 2 * Hkv) * D)
+    q = torch.zeros(T * Hq * D, dtype=torch.bfloat16)
+    for call in (lambda: ms.ms_rope_kv_q(c, rope, qkv.view(torch.int32), T, Hq, 0, q), lambda: ms.ms_rope_kv_q(c, rope, qkv, T, Hq, 0, half),
+                 lambda: ms.ms_attention_q(c, half, T, Hq, 0, q), lambda: ms.ms_attention_q(c, q, T, Hq, 0, half),
+                 lambda: ms.ms_kv_read_q(c, 0, T, half, q), lambda: ms.ms_kv_read_q(c, 0, T, q, half)):
+        with pytest.raises(ValueError):
+            call()
