@@ -995,7 +995,8 @@ void launch_norm(const NormArgs& a, hipStream_t s) {
   const unsigned T = static_cast<unsigned>(a.T);
   const dim3 block(kNormThreads), rows(T), twos((T + 1) / 2), fours((T + 3) / 4);
   const int d = a.d;
-#define MSK_NORM(GRID_, WAVES_, PER_) hipLaunchKernelGGL((residual_norm_q_kernel<Y, WAVES_, PER_>), GRID_, block, 0, s, a)
+#define MSK_NORM(GRID_, WAVES_, PER_) /* (of one wave, rows have no LDS of their own) */ \
+  hipLaunchKernelGGL((residual_norm_q_kernel<Y, WAVES_, PER_>), GRID_, block, msk::kGuardLds, s, a)
   if (d <= 512)
     MSK_NORM(fours, 1, 1);
   else if (d <= 1024)

@@ -264,3 +264,30 @@ def test_cache_tensors_of_another_type_are_refused():
                  lambda: ms.ms_kv_read_q(c, 0, T, half, q), lambda: ms.ms_kv_read_q(c, 0, T, q, half)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_every_launch_asks_for_lds():
+    """A work-group without LDS may land on the compute units that copies of experts hold, and waits behind their reads: a
+    kernel has LDS in each of its forms, or is launched with some."""
+    import os
+    import re
+    import paper_2509_08342_amd
+    has_lds = {"quant_blocks_kernel", "dense_q_tile_kernel", "dense_q_pair_kernel", "dense_q_few_kernel", "sample_kernel",
+               "sample_range_kernel", "sample_weigh_kernel", "sample_gather_kernel", "sample_choose_kernel"}
+    launched = set()
+    for name in ("blocks8.hip", "sample.hip"):
+        text = open(os.path.join(os.path.dirname(paper_2509_08342_amd.__file__), "csrc", name)).read().replace("\\\n", " ")
+        for m in re.finditer(r"hipLaunchKernelGGL\(", text):
+            args, depth, at = [""], 0, m.end()
+            while depth >= 0 and len(args) < 5:
+                c = text[at]
+                depth += (c == "(") - (c == ")")
+                args = args + [""] if c == "," and depth == 0 else args[:-1] + [args[-1] + c]
+                at += 1
+            kernel = re.search(r"\w+_kernel", args[0]).group()
+            launched.add(kernel)
+            if args[3].strip() != "msk::kGuardLds":
+                assert args[3].strip() == "0" and kernel in has_lds, (name, args[:4])
+                body = text[text.index("void %s(" % kernel):]
+                assert "__shared__" in body[:body.index("\n}\n")], kernel
+    assert has_lds < launched and len(launched) == len(has_lds) + 2
