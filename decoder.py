@@ -132,6 +132,7 @@ class Decoder:
         self.ids = torch.zeros(max(T, 1), dtype=torch.int32, device=dev)
         self.prob = torch.ones(1, dtype=torch.float32, device=dev)
         self.pos = 0
+        torch.cuda.current_stream().synchronize()  # the codes and cleared caches: steps may be on another stream
 
     def weights(self, raw):
         """A host matrix [n_out][n_in] as the device keeps it: bf16, or codes and exponents."""

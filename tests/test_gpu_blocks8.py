@@ -470,3 +470,19 @@ def test_decoder_in_8_bits_allocates_nothing_and_repeats():
             dec.step(x, 1, stream=stream, sampling=draw)
         stream.synchronize()
         assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
+
+
+@pytest.mark.parametrize("kv_bits", [16, 8])
+def test_a_decoder_is_ready_for_every_stream(kv_bits, monkeypatch):
+    """What its constructor enqueues (codes of the weights, cleared caches) has finished when it returns: the first step may
+    be on another stream."""
+    from workload import SplitRig
+    outputs = SplitRig.outputs
+
+    def late(rig, T):  # among the last things that a decoder makes
+        torch.cuda._sleep(200_000_000)
+        return outputs(rig, T)
+    monkeypatch.setattr(SplitRig, "outputs", late)
+    _, _, dec = _decoder(40, kv_bits=kv_bits, keep_f32=False)
+    with dec:
+        assert torch.cuda.current_stream().query()
