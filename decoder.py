@@ -22,7 +22,8 @@ dense_bits=8 keeps the projections' and the head's weights in 8 bits
 (ms_quant_q, once) and multiplies them with activations in 8 bits
 (ms_dense_q): half the resident bytes again.  The norms between the modules
 hand on what the next product reads (ms_residual_norm_q); the attention's
-output is made 8 bits by ms_quant_q.  What goes into the residual stays bf16.
+output is made 8 bits by ms_quant_q.  Products' results are fp32, as with
+bf16 weights, and the residual stays bf16.
 
 Tokens are the arg max of the logits, or drawn from them (ms_sample):
 Sampling."""
@@ -121,8 +122,7 @@ class Decoder:
         self.qkv = torch.empty(T, self.n_qkv, dtype=torch.float32, device=dev)
         self.q = torch.empty(T, Hq, D, dtype=bf, device=dev)
         self.o = torch.empty(T, Hq * D, dtype=bf, device=dev)
-        # 8 bits: what goes into the residual is rounded to bf16 anyway, and such results are the faster ones
-        self.att = torch.empty(T, d, dtype=torch.float32 if dense_bits == 16 else bf, device=dev)
+        self.att = torch.empty(T, d, dtype=torch.float32, device=dev)
         if dense_bits == 8:
             self.xq, self.oq = ms.new_matrix_q(T, d), ms.new_matrix_q(T, Hq * D)
         self.x = [torch.empty(T, d, dtype=bf, device=dev) for _ in range(2)]

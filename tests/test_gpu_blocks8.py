@@ -486,3 +486,26 @@ def test_a_decoder_is_ready_for_every_stream(kv_bits, monkeypatch):
     _, _, dec = _decoder(40, kv_bits=kv_bits, keep_f32=False)
     with dec:
         assert torch.cuda.current_stream().query()
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_the_residual_sum_takes_the_attention_as_it_is(T):
+    """h of the last layer, from its input and the attention's codes left by the step: rounded once, to half a step of bf16,
+    with no rounding of the attention's result before the sum."""
+    _, attn, dec = _decoder(40)
+    with dec:
+        _ready(dec)
+        x = torch.randn(T, 256, device="cuda").to(torch.bfloat16)
+        torch.cuda.synchronize()
+        cap = dec.step(x, T, capture=(1,))
+        torch.cuda.synchronize()
+        o = b8.values(*[t[:T].cpu().numpy() for t in dec.oq])
+        w = b8.values(*[t.cpu().numpy() for t in dec.layer_weights(1)[1]], 128)
+        att, mags = b8.dense(o, w)
+        xin = cap[1]["x"].astype(np.float64)
+        total, h = b8.residual_norm(xin, att)
+        half = np.exp2(np.floor(np.log2(np.abs(h))) - 8)
+        sums = 16 * 2.0 ** -23 * mags * np.abs(h / total)
+        bad = np.abs(cap[1]["h"] - h) > half * (1 + 2.0 ** -20) + sums
+        assert not bad.any(), (bad.sum(), bad.size)
+        assert np.median(np.abs(att / total)) > 2.0 ** -6  # (rounded before the sum, it would show)
