@@ -628,7 +628,10 @@ ms_status ms_attention_q(const ms_kv_cache_q* cache, const void* q, int32_t T, i
  * exponent of a block is the least in [-40, 40] with the largest finite magnitude
  * at most 448 * 2^e, codes are rounded to the nearest, ties to even; larger finite
  * values become the largest code, infinities and NaN the code of NaN.  Stored
- * exponents outside that range count as its ends. */
+ * exponents outside that range count as its ends.
+ *   A launch holds at most 2^28 - 16 blocks of one row, 2^24 - 1 of 128 rows, 2^24 - 1
+ * rows of a norm, 2^25 outputs of a product and, of more than 16 tokens, 2^22 - 1 blocks
+ * of 128 x 128 results (of some shapes more): MS_E_UNSUPPORTED beyond. */
 
 /* x [rows][n] (dtype MS_F32 or MS_BF16, 16-byte aligned) as a matrix in 8 bits,
  * block_rows = R (1 or 128): weights once, activations such as the attention's
@@ -681,20 +684,20 @@ typedef struct {
  * settings; fewer rows may need more.  Pure host arithmetic. */
 ms_status ms_sample_workspace(int32_t T, int32_t n, uint64_t* bytes_out);
 
-/* A token per row of logits [T][n] (fp32; n at most 524287, MS_E_UNSUPPORTED beyond;
- * NaN counts as -infinity).  Tokens in descending order of their logits, ties to the
- * lower index, weigh exp((l - max) / temperature); of them are kept the first top_k,
- * of those the fewest whose weights reach top_p of theirs (at least one), and of all
- * those with at least min_p of the largest weight.  idx_out[t] is the first kept
- * token at which the running weight passes u_dev[t] (fp32 in [0, 1): others count as
- * the nearest, NaN as 0) times the kept weight, prob_out[t] (or NULL) its share of
- * the kept weight; the arg max has 1.  Infinite maxima share the weight; a row
- * without a logit above -infinity gives 0.  Weights are whole numbers of 2^-45 of
- * the largest, smaller ones zero: the same inputs give the same token whatever else
- * runs, and whatever T.  opts NULL: temperature 1.
+/* A token per row of logits [T][n] (fp32; n at most 524287 and T at most 2^22 - 1,
+ * MS_E_UNSUPPORTED beyond; NaN counts as -infinity).  Tokens in descending order of
+ * their logits, ties to the lower index, weigh exp((l - max) / temperature); of them
+ * are kept the first top_k, of those the fewest whose weights reach top_p of theirs
+ * (at least one), and of all those with at least min_p of the largest weight.
+ * idx_out[t] is the first kept token at which the running weight passes u_dev[t] (fp32
+ * in [0, 1): others count as the nearest, NaN as 0) times the kept weight, prob_out[t]
+ * (or NULL) its share of the kept weight; the arg max has 1.  Infinite maxima share the
+ * weight; a row without a logit above -infinity gives 0.  Weights are whole numbers of
+ * 2^-45 of the largest, smaller ones zero: the same inputs give the same token whatever
+ * else runs, and whatever T.  opts NULL: temperature 1.
  * Outputs and, where it is used, the workspace overlap nothing (MS_E_INVALID).
- * workspace_dev: 16-byte aligned, used until
- * the call has finished on `stream`; calls that may overlap in time need one each. */
+ * workspace_dev: 16-byte aligned, used until the call has finished on `stream`; calls
+ * that may overlap in time need one each. */
 ms_status ms_sample(const float* logits, int32_t T, int32_t n, const ms_sample_opts* opts, const float* u_dev,
                     int32_t* idx_out, float* prob_out, void* workspace_dev, uint64_t workspace_bytes, void* stream);
 

@@ -291,3 +291,18 @@ def test_every_launch_asks_for_lds():
                 body = text[text.index("void %s(" % kernel):]
                 assert "__shared__" in body[:body.index("\n}\n")], kernel
     assert has_lds < launched and len(launched) == len(has_lds) + 2
+
+
+def test_calls_larger_than_a_launch_are_refused():
+    """One past each limit that the header states (addresses far apart, never read)."""
+    ms = _ms()
+    a, b, c, d, e = (k << 50 for k in range(1, 6))
+    quant = lambda rows, n, R: ms.lib.ms_quant_q(a, ms.MS_BF16, rows, n, R, b, c, None)  # noqa: E731
+    assert quant(2 ** 28 - 15, 16, 1) == ms.MS_E_UNSUPPORTED and quant(2 ** 21, 16384, 1) == ms.MS_E_UNSUPPORTED
+    assert quant(2 ** 31 - 1, 16, 128) == ms.MS_E_UNSUPPORTED and quant(2 ** 24, 16384, 128) == ms.MS_E_UNSUPPORTED
+    assert ms.lib.ms_residual_norm_q(a, None, ms.MS_F32, None, 1e-6, 2 ** 24, 16, b, None, None, None, None) == ms.MS_E_UNSUPPORTED
+    dense = lambda T, n_in, n_out: ms.lib.ms_dense_q(a, b, c, d, T, n_in, n_out, e, ms.MS_F32, None, None)  # noqa: E731
+    assert dense(1, 16, 2 ** 25 + 1) == ms.MS_E_UNSUPPORTED
+    # 2^22 blocks of 128 x 128 of rows that only such tiles take; of shorter ones as many of the largest tiles
+    assert dense(2 ** 18, 16384, 2 ** 18) == ms.MS_E_UNSUPPORTED and dense(2 ** 26, 128, 128 * 192) == ms.MS_E_UNSUPPORTED
+    assert ms.lib.ms_sample(a, 2 ** 22, 50, None, b, c, d, None, 0, None) == ms.MS_E_UNSUPPORTED
