@@ -22,6 +22,8 @@
 
 namespace {
 
+using msk::overlap;
+
 constexpr int kBlock = 128;  // columns that share a scale, and rows of a weight's block
 constexpr int kExpBias = 127;
 constexpr int kExpMin = -40, kExpMax = 40;
@@ -982,11 +984,6 @@ ms_status check_columns(int32_t n) {
   if (n <= 0) return MS_E_INVALID;
   return n % 16 == 0 && n <= kMostColumns ? MS_OK : MS_E_UNSUPPORTED;
 }
-bool overlap(const void* p, size_t np, const void* q, size_t nq) {
-  const auto a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return p && q && a < b + nq && b < a + np;
-}
-
 // A row by four waves, a short one by two or one: 4096 rows of 1024 15.4 us with four and
 // 12.3 with two, of 256 7.2 with four and 6.7 with one; 4096 rows of 2048 19.7 with four and
 // 21.8 with one.

@@ -10,6 +10,12 @@
 
 namespace msk {
 
+// whether two ranges of bytes of a caller's share any (NULL: none)
+inline bool overlap(const void* p, size_t np, const void* q, size_t nq) {
+  const auto a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return p && q && a < b + nq && b < a + np;
+}
+
 constexpr int kChunkUnits = 64;    // FFN intermediate units per chunk
 constexpr int kMaxTasks = 200;     // tasks passed by value in one FFN launch (3.3 KiB of kernel arguments)
 static_assert(kMaxTasks <= 256, "find_task_of reads at most 256 task starts");

@@ -26,6 +26,8 @@
 
 namespace {
 
+using msk::overlap;
+
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;  // as many as a row of lanes
 // (8192 bins sort fewer tokens and take longer to scan and merge: 64 rows of 131071 logits 44-50 us
@@ -963,11 +965,6 @@ int splits_of(int T, int n) {
   const int rows = (std::max(T, 1) - 1) / kXcds + 1;  // of an XCD
   const int splits = std::min(kCus / kXcds / rows, n / kLeastShare);
   return splits < 4 || n - n / splits < 40000 ? 1 : splits;
-}
-
-bool overlap(const void* p, size_t np, const void* q, size_t nq) {
-  const auto a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return p && q && a < b + nq && b < a + np;
 }
 
 }  // namespace
