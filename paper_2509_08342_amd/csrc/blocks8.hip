@@ -336,6 +336,9 @@ __device__ __forceinline__ void store8(const DenseArgs& a, int t, int o, msk::f3
 // Few tokens: MO blocks of 16 outputs x NT of 16 tokens (the last one repeated) per
 // work-group, its KW waves every KW-th 128 columns.  Codes go from memory to registers: lane l has
 // pieces l / 16 and 4 + l / 16 of sixteen codes of row l % 16.
+//   Bound by latency: a turn's loads are all waited for before they are converted, so a wave makes as
+// many trips to memory as it has turns (4096 columns, eight waves: four).  One token 4096 -> 6144 7.5
+// us, 3.4 TB/s; 4096 -> 32000 24.5, 5.3 TB/s; 61 tokens 2000 -> 5003 8.4-9.1.
 template <typename Y, int KW, int MO, int NT>
 __global__ __launch_bounds__(64 * KW) void dense_q_few_kernel(DenseArgs a, int vec) {
   __shared__ __align__(16) float red[KW][MO * NT][64][4];
@@ -417,8 +420,8 @@ __global__ __launch_bounds__(64 * KW) void dense_q_few_kernel(DenseArgs a, int v
 // of a wave), so one that has the CU to itself takes its stages several at a time: with 1, 2 and 4
 // parts a round of tiles of 32 x 32 at 4096 columns takes 12.4, 9.6 and 8.8 us with fp32 results and
 // 8.8, 7.3 and 6.8 with bf16 ones, of 64 x 64 18.9, 15.5 and 14.1, and 12.3, 10.7 and 10.6; two
-// rounds of 32 x 32 14.2, 12.6 and 15.8.  64 tokens 4096 -> 4096 8.7 and 6.7 us, 512 tokens 4096 ->
-// 6144 35 and 22.5.
+// rounds of 32 x 32 14.2, 12.6 and 15.8 (the same inputs again and again).  64 tokens 4096 -> 4096 8.9
+// and 7.3 us, 512 tokens 4096 -> 6144 35 and 22.6 (three sets of inputs in turn).
 constexpr int kStageLoad = 64 * 16;      // one load: 8 rows
 constexpr int kRows16 = 16 * kBlock;     // bytes of 16 staged rows
 constexpr int kTileExps = 16384;         // exponents of a tile's tokens that fit: blocks of columns x BM
@@ -605,12 +608,16 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void dense_q_tile_kernel(DenseAr
 // multiplying one, a conversion or two behind every matrix instruction (in a row before them
 // they cost 84 us for 80 below), and a wave takes 64 x 64 to 64 x 96, which has the fewest
 // conversions to a product.
-//   2048 tokens 4096 -> 6144 fp32 78-82 us (1.3 PFLOP/s; a library product of bf16 matrices
-// 76), bf16 47 (2.2 PFLOP/s; a library product of e4m3 matrices with one scale 43); 4096 tokens
-// 4096 -> 14336 350-366 and 197-206 us (1.4 and 2.4 PFLOP/s; 314 and 182); 8192 cubed 807 and
-// 405.  Of a bf16 stage's 1.3-1.4 us per CU, the matrix instructions alone take 1.2 and the
-// loads alone 1.1 (15 TB/s from the L2s); a tile's start and end 8 us of 55.  Fetching stages ahead
-// into the L2, without waiting for them, made it slower (259 -> 292 us at the time).
+//   Launches after each other on three sets of inputs in turn, so that weights are not in the
+// caches: 2048 tokens 4096 -> 6144 fp32 79 us (1.3 PFLOP/s; a library product of bf16 matrices
+// 82), bf16 48 (2.1 PFLOP/s; a library product of e4m3 matrices with one scale 46); 4096 tokens
+// 4096 -> 14336 370-384 and 222-229 us (1.3 and 2.1 PFLOP/s; 345 and 172); 8192 cubed 813 and
+// 435-448 (705 and 356).  On the same inputs again and again the second is 360-371 and 203-212, the
+// third 810 and 416-424, and the library's hardly less: the first loads of a tile wait longer here.
+//   On the same inputs: of a bf16 stage's 1.3-1.4 us per CU, the matrix instructions alone take 1.2
+// and the loads alone 1.1 (15 TB/s from the L2s); a tile's start and end 8 us of 55, the matrix
+// cores idle.  Fetching stages ahead into the L2, without waiting for them, made it slower (259 -> 292
+// us at the time).
 template <bool EIGHT, int BN>
 struct Pair {
   static constexpr int BM = 256, WM = EIGHT ? 2 : 4, NWV = 8, WN = NWV / WM;  // tokens, waves
@@ -797,7 +804,7 @@ __device__ __forceinline__ void dense_q_pair(const DenseArgs& a, int t0, int o0,
     }
     change();
   };
-  auto turns = [&]() {  // (the first apart from the loop: 8192 cubed fp32 820 -> 804 us, but bf16 410 -> 445)
+  auto turns = [&]() {  // (the first apart from the loop: 8192 cubed fp32 820 -> 804 us, but bf16 410 -> 445, the same inputs)
     if (!EIGHT) turn(0, true);
     for (int sl = EIGHT ? 0 : 1; sl < a.nb; ++sl) turn(sl, EIGHT && sl == 0);
   };
@@ -855,8 +862,8 @@ constexpr Tile kTiles[] = {{32, 32, 4, {88, 68}, {157, 120}},    {32, 32, 2, {96
                            {128, 128, 2, {364, 230}, {691, 439}}, {256, 128, 1, {587, 391}, {1128, 752}},
                            {256, 192, 1, {766, 474}, {1492, 914}}, {256, 256, 1, {0, 562}, {0, 1081}}};
 // Whole rounds of one of the two largest tiles, and the outputs that are left in the third: 4096
-// tokens 4096 -> 14336 bf16 205 us with the largest alone and 197 with both, 8192 cubed fp32 850 and
-// 806, 2048 tokens 4096 -> 14336 fp32 212 and 197.
+// tokens 4096 -> 14336 bf16 230 us with the largest alone and 228 with both, 8192 cubed fp32 828 and
+// 814, 2048 tokens 4096 -> 14336 fp32 234 and 209 (three sets of inputs in turn).
 constexpr int kNTiles = std::size(kTiles), kRest = kNTiles - 3, kFirstMixed = kNTiles - 2;
 static_assert(kTiles[kRest].bm == kTiles[kFirstMixed].bm, "the same tokens");
 

@@ -726,8 +726,8 @@ __device__ __forceinline__ void choose(Shared& sh, const SampleArgs& a, const Se
 // A work-group per row, its logits in registers up to 32768.  Bound by the instructions of the
 // weights, some thirty a token of which half are in double precision, and by a chain of scans and
 // barriers: with top-k, or min-p alone, only the tokens down to a cut's bin are weighed, from a
-// list.  One row of 32000: 13.6 us with top-k of 50, 18 with all tokens (8 of them weights);
-// 500 rows with min-p: 27 us, 2.4 TB/s, in two rounds of work-groups.
+// list.  One row of 32000: 13.3 us with top-k of 50, 18 with all tokens (8 of them weights);
+// 500 rows with min-p: 26.5 us, 2.4 TB/s, in two rounds of work-groups (128 registers: one a CU).
 template <int AT_ONCE>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   __shared__ Shared sh;
@@ -800,8 +800,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
 }
 
 // The same by several work-groups a row, in four launches: the range of each, one histogram of
-// them all, the tokens of the cuts' bins, and the choice.  64 rows of 131071 logits: 5.9, 18.8, 13.5
-// and 5.8 us.  (A histogram for each work-group, summed by the next launch, instead of atomics: the
+// them all, the tokens of the cuts' bins, and the choice.  64 rows of 131071 logits: 7.4, 18.2, 12.9
+// and 5.2 us.  (A histogram for each work-group, summed by the next launch, instead of atomics: the
 // same; the last of a row's work-groups to choose instead of a fourth launch: as long, as its fence
 // waits for the L2.)
 struct Gathered {
